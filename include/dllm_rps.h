@@ -245,6 +245,126 @@ dllm_status vocab_entropy_topk_noalloc(const void* hidden, const void* w_lm, int
                                        int32_t dtype, const float* row_scale, float scale, int32_t mask_id,
                                        const dllm_stats* out, dllm_stream stream);
 
+/* ------------------------------------------------- paged key/value cache
+ *
+ * Keys and values of many sequences in pages of page_len positions, shared
+ * between sequences by reference: the form of the prefix cache for batches of
+ * requests and for searches, where sequences have lengths of their own and
+ * lookahead branches start from one another.  Lengths, tables and reference
+ * counts live on the device, so no call waits for the GPU.
+ *
+ *   k      [n_layers][n_pages][n_kv_heads][page_len][head_dim], post-RoPE
+ *   vt     [n_layers][n_pages][n_kv_heads][head_dim][page_len] (values
+ *          transposed); types as in dllm_kv_cache.
+ *   refs   [n_pages] sequences that hold the page; 0: free.
+ *   table  [max_seqs][max_blocks] page of positions j * page_len .. of a
+ *          sequence; -1 past its last page.
+ *   len    [max_seqs] positions a sequence holds; 0: an empty one.
+ * The caller allocates the arrays (k and vt 16-byte aligned) and calls
+ * kv_pages_init once.  A page that is not full is held by one sequence only.
+ * Requirements: head_dim in {64, 128}, page_len in {16, 32, 64, 128, 256},
+ * n_pages <= KV_MAX_PAGES, max_seqs <= KV_MAX_SEQS, n_kv_heads <= 1024,
+ * max_blocks * page_len <= KV_MAX_POSITIONS.
+ *
+ * Sequence lists are device arrays.  The calls that change tables check them
+ * on the device: `status` (device int32) receives KV_PAGES_OK, or the lowest
+ * code that applies and nothing is changed. */
+#define KV_MAX_PAGES (1 << 20)
+#define KV_MAX_SEQS 1024
+#define KV_MAX_POSITIONS (1 << 30)
+enum {
+    KV_PAGES_OK = 0,
+    KV_PAGES_ESEQ = 1,      /* a sequence outside 0 .. max_seqs-1, listed twice, or a fork's target not empty */
+    KV_PAGES_ELEN = 2,      /* a negative count, more than max_blocks pages, or more positions than are held */
+    KV_PAGES_ESHARED = 3,   /* a cut inside a page that another sequence holds too */
+    KV_PAGES_EFULL = 4      /* fewer free pages than needed */
+};
+
+typedef struct {
+    void* k;
+    void* vt;
+    int32_t* refs;
+    int32_t* table;
+    int32_t* len;
+    int32_t n_layers, n_pages, n_kv_heads, head_dim, page_len, max_seqs, max_blocks;
+    int32_t dtype;          /* dllm_dtype of the model */
+} dllm_kv_pages;
+
+/* Rows of a batch: row i of entry b and head h starts at element
+ * b * seq + i * row + h * head of p and holds head_dim contiguous elements.
+ * p and the strides (in bytes) are multiples of 16; strides are >= 0. */
+typedef struct {
+    void* p;
+    int64_t seq, row, head;
+} dllm_rows;
+
+/* Every page free, every sequence empty. */
+dllm_status kv_pages_init(const dllm_kv_pages* pages, dllm_stream stream);
+
+/* Sequence seqs[i] grows by add[i] positions (1 <= n <= KV_MAX_SEQS): it gets
+ * the pages they need, lowest free ids first in call order.  Their contents
+ * are written by kv_pages_write. */
+dllm_status kv_pages_grow(const dllm_kv_pages* pages, const int32_t* seqs, const int32_t* add, int32_t n,
+                          int32_t* status, dllm_stream stream);
+
+/* The empty sequence dst[i] becomes the first keep[i] positions of src[i]
+ * (keep NULL: all of them).  Whole pages are shared; a page that keep cuts is
+ * copied, in every layer, to the lowest free id (in call order).  A source may
+ * be listed any number of times; sources are taken as before the call. */
+dllm_status kv_pages_fork(const dllm_kv_pages* pages, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                          int32_t n, int32_t* status, dllm_stream stream);
+
+/* Sequence seqs[i] keeps its first keep[i] positions (keep NULL: none) and
+ * gives back the pages past them; a page is free when its last holder has.
+ * A cut inside a page that is held more than once before the call is refused
+ * (KV_PAGES_ESHARED); kv_pages_fork with keep copies it instead. */
+dllm_status kv_pages_free(const dllm_kv_pages* pages, const int32_t* seqs, const int32_t* keep, int32_t n,
+                          int32_t* status, dllm_stream stream);
+
+/* Pages in use move to ids 0 .. n_used-1, in every layer: the r-th used page
+ * with an id of n_used or more to the r-th free id below, the others stay.
+ * Tables and references follow; n_used (device int32) receives the number of
+ * pages in use, so that pages from there on may be released by the caller. */
+size_t kv_pages_compact_workspace_bytes(const dllm_kv_pages* pages);
+dllm_status kv_pages_compact(const dllm_kv_pages* pages, int32_t* n_used, void* ws, size_t ws_bytes,
+                             dllm_stream stream);
+
+/* Keys and values of the last n_rows[b] positions of sequence seqs[b] into
+ * their pages of one layer (n_rows NULL: max_rows each; outside 0 .. max_rows:
+ * clamped), 1 <= n <= KV_MAX_SEQS.  k (post-RoPE) and v have n_kv_heads heads
+ * and the model's type.  Row i is position len - n_rows[b] + i.  Not written:
+ * rows of a sequence outside 0 .. max_seqs-1, rows before position 0 and rows
+ * whose page another sequence holds too.  Of a sequence listed twice the last
+ * entry is written. */
+dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                           int32_t max_rows, const int32_t* n_rows, const dllm_rows* k, const dllm_rows* v,
+                           dllm_stream stream);
+
+/* Attention of a batch over one layer of its pages, the prefix that the batch
+ * shares computed once for all: softmax(scale q k^T) v for n_rows[b] rows of
+ * entry b (n_rows as in kv_pages_write) over the positions of sequence
+ * seqs[b]; 1 <= n <= KV_MAX_SEQS, 1 <= max_rows.
+ *   q, out       rows of n_heads heads, a multiple of n_kv_heads: head h reads
+ *                key head h / (n_heads / n_kv_heads).  out rows from n_rows[b]
+ *                on are left as they were; out and q do not overlap.
+ *   prefix_seq, shared_len   the whole pages among the first min(shared_len,
+ *                len[prefix_seq]) positions of sequence prefix_seq (a host
+ *                value) are read from its table for every entry, once for the
+ *                batch; the entries' own tables are read from there on.
+ *                shared_len 0: nothing is shared.
+ *   max_len      the longest sequence among the entries, as far as the caller
+ *                knows (it sets how the work is divided, not what is computed).
+ *   causal       0: every row sees all positions of its sequence; 1: row i
+ *                sees positions 0 .. len - n_rows[b] + i.
+ * A row that sees no position is 0, and so are the rows of a sequence outside
+ * 0 .. max_seqs-1.  Table entries outside the pool are clamped.  Positions past
+ * a row's last are never used, whatever they hold. */
+size_t kv_pages_attention_workspace_bytes(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads);
+dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                               int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
+                               const dllm_rows* out, int32_t prefix_seq, int32_t shared_len, int32_t max_len,
+                               int32_t causal, float scale, void* ws, size_t ws_bytes, dllm_stream stream);
+
 /* Kernel timing for benchmarks.  Between dllm_profile_begin and
  * dllm_profile_end every kernel that dllm_forward launches is bracketed by
  * HIP events on the launch stream (for at most max_launches launches).

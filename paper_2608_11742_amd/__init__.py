@@ -12,6 +12,8 @@ from .binding import (  # noqa: F401
     dllm_workspace_bytes_packed,
     rps_lookahead_score, rps_commit, sched_commit, params, new_plan, new_decision, read_plan, read_decision, lib,
     dllm_profile_begin, dllm_profile_end, dllm_mfma_ceiling,
+    KvPages, kv_pages_init, kv_pages_grow, kv_pages_fork, kv_pages_free, kv_pages_compact,
+    kv_pages_compact_workspace_bytes, kv_pages_write, kv_pages_attention, kv_pages_attention_workspace_bytes,
 )
 from .model import Model  # noqa: F401
 from .step import RpsStep, rps_decode, baseline_decode  # noqa: F401

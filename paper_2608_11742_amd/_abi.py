@@ -48,6 +48,16 @@ class KvCache(C.Structure):
     _fields_ = [("k", vp), ("vt", vp), ("len", i32), ("cap", i32)]
 
 
+class KvPagesC(C.Structure):
+    _fields_ = [("k", vp), ("vt", vp), ("refs", vp), ("table", vp), ("len", vp), ("n_layers", i32),
+                ("n_pages", i32), ("n_kv_heads", i32), ("head_dim", i32), ("page_len", i32), ("max_seqs", i32),
+                ("max_blocks", i32), ("dtype", i32)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("p", vp), ("seq", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
 class Probe(C.Structure):
     _fields_ = [("row", vp), ("token", vp), ("logit", vp), ("n", i32)]
 
@@ -86,6 +96,16 @@ SIGNATURES = {
     "vocab_entropy_topk_workspace_bytes": (sz, [i32, i32]),
     "vocab_entropy_topk": (i32, [vp, vp, i32, i32, i32, i32, vp, f32, i32, C.POINTER(StatsC), vp, sz, vp]),
     "vocab_entropy_topk_noalloc": (i32, [vp, vp, i32, i32, i32, i32, vp, f32, i32, C.POINTER(StatsC), vp]),
+    "kv_pages_init": (i32, [C.POINTER(KvPagesC), vp]),
+    "kv_pages_grow": (i32, [C.POINTER(KvPagesC), vp, vp, i32, vp, vp]),
+    "kv_pages_fork": (i32, [C.POINTER(KvPagesC), vp, vp, vp, i32, vp, vp]),
+    "kv_pages_free": (i32, [C.POINTER(KvPagesC), vp, vp, i32, vp, vp]),
+    "kv_pages_compact_workspace_bytes": (sz, [C.POINTER(KvPagesC)]),
+    "kv_pages_compact": (i32, [C.POINTER(KvPagesC), vp, vp, sz, vp]),
+    "kv_pages_write": (i32, [C.POINTER(KvPagesC), i32, vp, i32, i32, vp, C.POINTER(Rows), C.POINTER(Rows), vp]),
+    "kv_pages_attention_workspace_bytes": (sz, [C.POINTER(KvPagesC), i32, i32, i32]),
+    "kv_pages_attention": (i32, [C.POINTER(KvPagesC), i32, vp, i32, i32, vp, i32, C.POINTER(Rows), C.POINTER(Rows),
+                                 i32, i32, i32, i32, f32, vp, sz, vp]),
     "dllm_profile_begin": (i32, [vp, i32]),
     "dllm_profile_begin_classes": (i32, [vp, i32, C.c_uint32]),
     "dllm_profile_end": (i32, [vp, C.POINTER(f32), C.POINTER(i32)]),
@@ -100,6 +120,8 @@ SIGNATURES = {
 }
 
 SCHED_TOP_CONFIDENCE, SCHED_LOW_ENTROPY = 0, 1
+KV_PAGES_OK, KV_PAGES_ESEQ, KV_PAGES_ELEN, KV_PAGES_ESHARED, KV_PAGES_EFULL = 0, 1, 2, 3, 4
+KV_MAX_PAGES, KV_MAX_SEQS, KV_MAX_POSITIONS = 1 << 20, 1024, 1 << 30
 
 
 def load(path: str = LIB_PATH):

@@ -220,6 +220,139 @@ def vocab_entropy_topk_noalloc(hidden, w_lm, out: Stats, row_scale=None, scale: 
                                             C.byref(out.c()), _stream(stream)))
 
 
+# ---------------------------------------------------------------- paged key/value cache
+
+class KvPages:
+    """Device arrays of a paged key/value cache (dllm_kv_pages).
+
+    k [layers, pages, kv heads, page_len, head_dim] bf16 or fp32; vt [layers,
+    pages, kv heads, head_dim, page_len] float16 for bf16 keys, else fp32;
+    refs [pages], table [max_seqs, max_blocks], len [max_seqs] int32.
+    """
+
+    def __init__(self, k, vt, refs, table, len):
+        L, n_pages, heads, page_len, hd = k.shape
+        v_dtype = {torch.bfloat16: torch.float16, torch.float32: torch.float32}.get(k.dtype)
+        if v_dtype is None or vt.dtype != v_dtype or tuple(vt.shape) != (L, n_pages, heads, hd, page_len):
+            raise ValueError("k must be bf16 with float16 vt, or fp32 with fp32 vt, vt transposed within the pages")
+        if any(t.dtype != torch.int32 for t in (refs, table, len)):
+            raise ValueError("refs, table and len must be int32")
+        if refs.shape != (n_pages,) or table.dim() != 2 or len.shape != table.shape[:1]:
+            raise ValueError("refs [pages], table [max_seqs, max_blocks], len [max_seqs]")
+        if any(t.device != k.device or not t.is_contiguous() for t in (k, vt, refs, table, len)):
+            raise ValueError("the arrays must be contiguous tensors of one device")
+        self.k, self.vt, self.refs, self.table, self.len = k, vt, refs, table, len
+        self.page_len, self.head_dim, self.n_kv_heads, self.device = page_len, hd, heads, k.device
+        self._c = _abi.KvPagesC(k.data_ptr(), vt.data_ptr(), refs.data_ptr(), table.data_ptr(), len.data_ptr(), L,
+                                n_pages, heads, hd, page_len, table.shape[0], table.shape[1],
+                                DLLM_BF16 if k.dtype == torch.bfloat16 else DLLM_F32)
+        self._ref = C.byref(self._c)
+
+    @classmethod
+    def empty(cls, n_layers: int, n_pages: int, n_kv_heads: int, page_len: int, head_dim: int, max_seqs: int,
+              max_blocks: int, dtype=torch.bfloat16, device="cuda"):
+        """New arrays, every page free and every sequence empty (kv_pages_init)."""
+        i = dict(dtype=torch.int32, device=device)
+        v_dtype = torch.float16 if dtype == torch.bfloat16 else dtype
+        pages = cls(torch.empty(n_layers, n_pages, n_kv_heads, page_len, head_dim, dtype=dtype, device=device),
+                    torch.empty(n_layers, n_pages, n_kv_heads, head_dim, page_len, dtype=v_dtype, device=device),
+                    torch.empty(n_pages, **i), torch.empty(max_seqs, max_blocks, **i), torch.empty(max_seqs, **i))
+        kv_pages_init(pages)
+        return pages
+
+
+def _ids(pages: KvPages, t, n: int | None = None):
+    """Address of an int32 list of n entries beside the pages' arrays."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.device != pages.device or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError("sequence lists, counts and status are contiguous int32 tensors, one value an entry, beside the pages")
+    return t.data_ptr()
+
+
+def _rows(pages: KvPages, t, heads: int, name: str):
+    """t [entries, rows, heads, head_dim], any strides over contiguous head_dim, as dllm_rows."""
+    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != pages.head_dim or t.stride(3) != 1:
+        raise ValueError(f"{name} must be [entries, rows, {heads}, {pages.head_dim}] with contiguous rows")
+    if t.dtype != pages.k.dtype or t.device != pages.device:
+        raise ValueError(f"{name} must have the type and device of the pages' keys")
+    # a dimension of one has no stride to speak of
+    st = [0 if n == 1 else step for n, step in zip(t.shape, t.stride())]
+    return C.byref(_abi.Rows(t.data_ptr(), st[0], st[1], st[2]))
+
+
+def _page_stream(pages: KvPages, stream):
+    if stream is None and pages.device.index != torch.cuda.current_device():
+        raise ValueError("the pages are on another device than the current one")
+    return _stream(stream)
+
+
+def kv_pages_init(pages: KvPages, stream=None):
+    _check(lib().kv_pages_init(pages._ref, _page_stream(pages, stream)))
+
+
+def kv_pages_grow(pages: KvPages, seqs, add, status, stream=None):
+    """Sequences seqs[i] grow by add[i] positions; status (int32, device) receives a KV_PAGES_ code."""
+    n = seqs.numel()
+    _check(lib().kv_pages_grow(pages._ref, _ids(pages, seqs), _ids(pages, add, n), n, _ids(pages, status, 1),
+                               _page_stream(pages, stream)))
+
+
+def kv_pages_fork(pages: KvPages, src, dst, status, keep=None, stream=None):
+    """Empty sequences dst[i] become the first keep[i] positions of src[i] (all of them without keep)."""
+    n = src.numel()
+    _check(lib().kv_pages_fork(pages._ref, _ids(pages, src), _ids(pages, dst, n), _ids(pages, keep, n), n,
+                               _ids(pages, status, 1), _page_stream(pages, stream)))
+
+
+def kv_pages_free(pages: KvPages, seqs, status, keep=None, stream=None):
+    """Sequences seqs[i] keep their first keep[i] positions (none without keep)."""
+    n = seqs.numel()
+    _check(lib().kv_pages_free(pages._ref, _ids(pages, seqs), _ids(pages, keep, n), n, _ids(pages, status, 1),
+                               _page_stream(pages, stream)))
+
+
+def kv_pages_compact_workspace_bytes(pages: KvPages) -> int:
+    return lib().kv_pages_compact_workspace_bytes(pages._ref)
+
+
+def kv_pages_compact(pages: KvPages, n_used, ws, stream=None):
+    """Pages in use move to ids 0 .. n_used-1 (n_used: int32, device)."""
+    _check(lib().kv_pages_compact(pages._ref, _ids(pages, n_used, 1), _p(ws), ws.numel() * ws.element_size(),
+                                  _page_stream(pages, stream)))
+
+
+def kv_pages_write(pages: KvPages, layer: int, seqs, k, v, n_rows=None, stream=None):
+    """k, v [entries, rows, kv heads, head_dim]: the last n_rows[b] (or all rows) positions of sequence seqs[b]."""
+    n = seqs.numel()
+    if k.shape[0] != n or v.shape[:2] != k.shape[:2]:
+        raise ValueError("k and v need one batch entry per sequence and the same rows")
+    _check(lib().kv_pages_write(pages._ref, layer, _ids(pages, seqs), n, k.shape[1], _ids(pages, n_rows, n),
+                                _rows(pages, k, pages.n_kv_heads, "k"), _rows(pages, v, pages.n_kv_heads, "v"),
+                                _page_stream(pages, stream)))
+
+
+def kv_pages_attention_workspace_bytes(pages: KvPages, n: int, max_rows: int, n_heads: int) -> int:
+    return lib().kv_pages_attention_workspace_bytes(pages._ref, n, max_rows, n_heads)
+
+
+def kv_pages_attention(pages: KvPages, layer: int, seqs, q, out, ws, n_rows=None, prefix_seq: int = 0,
+                       shared_len: int = 0, max_len: int | None = None, causal: bool = False,
+                       scale: float | None = None, stream=None):
+    """q, out [entries, rows, heads, head_dim]; see kv_pages_attention in dllm_rps.h.
+
+    max_len defaults to the tables' length, scale to 1 / sqrt(head_dim)."""
+    n, rows, heads, hd = q.shape
+    if seqs.numel() != n or out.shape != q.shape:
+        raise ValueError("q and out need one batch entry per sequence and the same shape")
+    if max_len is None:
+        max_len = pages.table.shape[1] * pages.page_len
+    _check(lib().kv_pages_attention(pages._ref, layer, _ids(pages, seqs), n, rows, _ids(pages, n_rows, n), heads,
+                                    _rows(pages, q, heads, "q"), _rows(pages, out, heads, "out"), prefix_seq,
+                                    shared_len, max_len, int(causal), hd ** -0.5 if scale is None else scale, _p(ws),
+                                    ws.numel() * ws.element_size(), _page_stream(pages, stream)))
+
+
 # ---------------------------------------------------------------- scheduler
 
 def rps_select_pivots(base: Stats, m_pos, n_m: int, prm: RpsParams, plan, stream=None):

@@ -760,4 +760,170 @@ dllm_status sched_commit(int32_t* tokens, int32_t seq, int32_t* m_pos, int32_t n
                    "sched_commit");
 }
 
+// ---------------------------------------------------------------- paged key/value cache
+
+namespace {
+
+dllm_status check_pages(const dllm_kv_pages* p, const char* who) {
+  if (!p) return fail(DLLM_EINVAL, "%s: NULL pages", who);
+  if (!p->k || !p->vt || !p->refs || !p->table || !p->len) return fail(DLLM_EINVAL, "%s: pages has a NULL array", who);
+  if (p->dtype != DLLM_F32 && p->dtype != DLLM_BF16) return fail(DLLM_EDTYPE, "%s: dtype %d", who, p->dtype);
+  if (p->head_dim != 64 && p->head_dim != 128)
+    return fail(DLLM_ESHAPE, "%s: head_dim %d not in {64, 128}", who, p->head_dim);
+  if (p->page_len < 16 || p->page_len > 256 || (p->page_len & (p->page_len - 1)))
+    return fail(DLLM_ESHAPE, "%s: page_len %d not in {16, 32, 64, 128, 256}", who, p->page_len);
+  if (p->n_layers < 1 || p->n_layers > 65536 || p->n_kv_heads < 1 || p->n_kv_heads > 1024 || p->n_pages < 1 ||
+      p->n_pages > KV_MAX_PAGES || p->max_seqs < 1 || p->max_seqs > KV_MAX_SEQS || p->max_blocks < 1 ||
+      p->max_blocks > KV_MAX_POSITIONS / p->page_len)
+    return fail(DLLM_ESHAPE, "%s: %d layers, %d pages, %d heads, %d sequences of %d pages", who, p->n_layers,
+                p->n_pages, p->n_kv_heads, p->max_seqs, p->max_blocks);
+  if ((reinterpret_cast<uintptr_t>(p->k) | reinterpret_cast<uintptr_t>(p->vt)) % 16)
+    return fail(DLLM_EINVAL, "%s: k and vt need 16-byte alignment", who);
+  return DLLM_OK;
+}
+
+dllm_status check_entries(const void* seqs, int32_t n, const char* who) {
+  if (!seqs) return fail(DLLM_EINVAL, "%s: NULL sequences", who);
+  if (n < 1 || n > KV_MAX_SEQS) return fail(DLLM_ESHAPE, "%s: %d entries outside 1..%d", who, n, KV_MAX_SEQS);
+  return DLLM_OK;
+}
+
+dllm_status check_rows(const dllm_rows* r, int dtype, const char* who, const char* name) {
+  if (!r || !r->p) return fail(DLLM_EINVAL, "%s: NULL %s", who, name);
+  const int64_t T = elem_bytes(dtype);
+  const int64_t most = int64_t(1) << 40;   // of a stride; products with 2^24 rows stay inside 64 bits
+  if (r->seq < 0 || r->row < 0 || r->head < 0 || r->seq > most || r->row > most || r->head > most)
+    return fail(DLLM_ESHAPE, "%s: strides of %s outside 0..2^40", who, name);
+  if (reinterpret_cast<uintptr_t>(r->p) % 16 || r->seq * T % 16 || r->row * T % 16 || r->head * T % 16)
+    return fail(DLLM_EINVAL, "%s: %s needs 16-byte aligned rows", who, name);
+  return DLLM_OK;
+}
+
+constexpr int kMaxBatchRows = 1 << 20;   // rows of one entry
+
+}  // namespace
+
+dllm_status kv_pages_init(const dllm_kv_pages* pages, dllm_stream stream) {
+  dllm_status st = check_pages(pages, "kv_pages_init");
+  if (st != DLLM_OK) return st;
+  return hip_check(pages_init(*pages, static_cast<hipStream_t>(stream)), "kv_pages_init");
+}
+
+dllm_status kv_pages_grow(const dllm_kv_pages* pages, const int32_t* seqs, const int32_t* add, int32_t n,
+                          int32_t* status, dllm_stream stream) {
+  dllm_status st = check_pages(pages, "kv_pages_grow");
+  if (st == DLLM_OK) st = check_entries(seqs, n, "kv_pages_grow");
+  if (st != DLLM_OK) return st;
+  if (!add || !status) return fail(DLLM_EINVAL, "kv_pages_grow: NULL add or status");
+  return hip_check(pages_grow(*pages, seqs, add, n, status, static_cast<hipStream_t>(stream)), "kv_pages_grow");
+}
+
+dllm_status kv_pages_fork(const dllm_kv_pages* pages, const int32_t* src, const int32_t* dst, const int32_t* keep,
+                          int32_t n, int32_t* status, dllm_stream stream) {
+  dllm_status st = check_pages(pages, "kv_pages_fork");
+  if (st == DLLM_OK) st = check_entries(src, n, "kv_pages_fork");
+  if (st == DLLM_OK) st = check_entries(dst, n, "kv_pages_fork");
+  if (st != DLLM_OK) return st;
+  if (!status) return fail(DLLM_EINVAL, "kv_pages_fork: NULL status");
+  return hip_check(pages_fork(*pages, src, dst, keep, n, status, static_cast<hipStream_t>(stream)), "kv_pages_fork");
+}
+
+dllm_status kv_pages_free(const dllm_kv_pages* pages, const int32_t* seqs, const int32_t* keep, int32_t n,
+                          int32_t* status, dllm_stream stream) {
+  dllm_status st = check_pages(pages, "kv_pages_free");
+  if (st == DLLM_OK) st = check_entries(seqs, n, "kv_pages_free");
+  if (st != DLLM_OK) return st;
+  if (!status) return fail(DLLM_EINVAL, "kv_pages_free: NULL status");
+  return hip_check(pages_free(*pages, seqs, keep, n, status, static_cast<hipStream_t>(stream)), "kv_pages_free");
+}
+
+size_t kv_pages_compact_workspace_bytes(const dllm_kv_pages* pages) {
+  return check_pages(pages, "kv_pages_compact_workspace_bytes") == DLLM_OK ? pages_compact_workspace(pages->n_pages) : 0;
+}
+
+dllm_status kv_pages_compact(const dllm_kv_pages* pages, int32_t* n_used, void* ws, size_t ws_bytes,
+                             dllm_stream stream) {
+  dllm_status st = check_pages(pages, "kv_pages_compact");
+  if (st != DLLM_OK) return st;
+  if (!n_used || !ws) return fail(DLLM_EINVAL, "kv_pages_compact: NULL n_used or ws");
+  const size_t need = pages_compact_workspace(pages->n_pages);
+  if (ws_bytes < need) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, need);
+  return hip_check(pages_compact(*pages, n_used, ws, static_cast<hipStream_t>(stream)), "kv_pages_compact");
+}
+
+dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                           int32_t max_rows, const int32_t* n_rows, const dllm_rows* k, const dllm_rows* v,
+                           dllm_stream stream) {
+  dllm_status st = check_pages(pages, "kv_pages_write");
+  if (st == DLLM_OK) st = check_entries(seqs, n, "kv_pages_write");
+  if (st == DLLM_OK) st = check_rows(k, pages->dtype, "kv_pages_write", "k");
+  if (st == DLLM_OK) st = check_rows(v, pages->dtype, "kv_pages_write", "v");
+  if (st != DLLM_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers) return fail(DLLM_ESHAPE, "kv_pages_write: layer %d", layer);
+  if (max_rows < 1 || max_rows > kMaxBatchRows) return fail(DLLM_ESHAPE, "kv_pages_write: max_rows %d", max_rows);
+  return hip_check(pages_write(*pages, layer, seqs, n, max_rows, n_rows, *k, *v, static_cast<hipStream_t>(stream)),
+                   "kv_pages_write");
+}
+
+namespace {
+
+dllm_status check_attention(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
+                            const char* who) {
+  dllm_status st = check_pages(pages, who);
+  if (st != DLLM_OK) return st;
+  if (n < 1 || n > KV_MAX_SEQS) return fail(DLLM_ESHAPE, "%s: %d entries outside 1..%d", who, n, KV_MAX_SEQS);
+  if (max_rows < 1 || max_rows > kMaxBatchRows) return fail(DLLM_ESHAPE, "%s: max_rows %d", who, max_rows);
+  if (n_heads < 1 || n_heads > 1024 || n_heads % pages->n_kv_heads)
+    return fail(DLLM_ESHAPE, "%s: %d heads over %d key heads", who, n_heads, pages->n_kv_heads);
+  if (int64_t(n) * max_rows * n_heads > (int64_t(1) << 26))
+    return fail(DLLM_ESHAPE, "%s: %d x %d rows of %d heads", who, n, max_rows, n_heads);
+  return DLLM_OK;
+}
+
+}  // namespace
+
+size_t kv_pages_attention_workspace_bytes(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads) {
+  if (check_attention(pages, n, max_rows, n_heads, "kv_pages_attention_workspace_bytes") != DLLM_OK) return 0;
+  return paged_attention_workspace(*pages, n, max_rows, n_heads);
+}
+
+dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                               int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
+                               const dllm_rows* out, int32_t prefix_seq, int32_t shared_len, int32_t max_len,
+                               int32_t causal, float scale, void* ws, size_t ws_bytes, dllm_stream stream) {
+  dllm_status st = check_attention(pages, n, max_rows, n_heads, "kv_pages_attention");
+  if (st == DLLM_OK) st = check_entries(seqs, n, "kv_pages_attention");
+  if (st == DLLM_OK) st = check_rows(q, pages->dtype, "kv_pages_attention", "q");
+  if (st == DLLM_OK) st = check_rows(out, pages->dtype, "kv_pages_attention", "out");
+  if (st != DLLM_OK) return st;
+  const int64_t hd = pages->head_dim;
+  if ((n > 1 && out->seq < hd) || (max_rows > 1 && out->row < hd) || (n_heads > 1 && out->head < hd))
+    return fail(DLLM_ESHAPE, "kv_pages_attention: rows of out overlap");
+  if (layer < 0 || layer >= pages->n_layers) return fail(DLLM_ESHAPE, "kv_pages_attention: layer %d", layer);
+  if (shared_len < 0 || max_len < 0) return fail(DLLM_ESHAPE, "kv_pages_attention: shared_len %d max_len %d", shared_len, max_len);
+  if (shared_len > 0 && (prefix_seq < 0 || prefix_seq >= pages->max_seqs))
+    return fail(DLLM_EINVAL, "kv_pages_attention: prefix_seq %d outside 0..%d", prefix_seq, pages->max_seqs - 1);
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(DLLM_EINVAL, "kv_pages_attention: scale must be finite and > 0");
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "kv_pages_attention: ws NULL or not 16-byte aligned");
+  const size_t need = paged_attention_workspace(*pages, n, max_rows, n_heads);
+  if (ws_bytes < need) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, need);
+  PagedAttn a{};
+  a.p = *pages;
+  a.layer = layer;
+  a.seqs = seqs;
+  a.n_rows = n_rows;
+  a.n = n;
+  a.max_rows = max_rows;
+  a.heads = n_heads;
+  a.q = *q;
+  a.out = *out;
+  a.prefix_seq = prefix_seq;
+  a.shared_len = shared_len;
+  a.max_len = max_len;
+  a.causal = causal != 0;
+  a.scale = scale;
+  a.part = static_cast<float*>(ws);
+  return hip_check(paged_attention(a, static_cast<hipStream_t>(stream)), "kv_pages_attention");
+}
+
 }  // extern "C"

@@ -134,6 +134,36 @@ hipError_t rps_commit_step(int32_t* tokens, int seq, int32_t* m_pos, int n_m, co
 hipError_t sched_commit_step(int32_t* tokens, int seq, int32_t* m_pos, int n_m, const StatsOut& st, int rule, int k,
                             int32_t* n_m_out, int32_t* committed, int32_t* n_committed, hipStream_t s);
 
+// paged key/value cache: tables and data (pages.hip).  fork and free take a
+// host-side bound on the table entries of a call, n * max_blocks.
+hipError_t pages_init(const dllm_kv_pages& p, hipStream_t s);
+hipError_t pages_grow(const dllm_kv_pages& p, const int32_t* seqs, const int32_t* add, int n, int32_t* status,
+                      hipStream_t s);
+hipError_t pages_fork(const dllm_kv_pages& p, const int32_t* src, const int32_t* dst, const int32_t* keep, int n,
+                      int32_t* status, hipStream_t s);
+hipError_t pages_free(const dllm_kv_pages& p, const int32_t* seqs, const int32_t* keep, int n, int32_t* status,
+                      hipStream_t s);
+size_t pages_compact_workspace(int n_pages);
+hipError_t pages_compact(const dllm_kv_pages& p, int32_t* n_used, void* ws, hipStream_t s);
+hipError_t pages_write(const dllm_kv_pages& p, int layer, const int32_t* seqs, int n, int max_rows,
+                       const int32_t* n_rows, const dllm_rows& k, const dllm_rows& v, hipStream_t s);
+
+// attention over the pages of one layer (paged_attention.hip)
+struct PagedAttn {
+  dllm_kv_pages p;
+  int layer;
+  const int32_t* seqs;
+  const int32_t* n_rows;   // nullable: max_rows each
+  int n, max_rows, heads;
+  dllm_rows q, out;
+  int prefix_seq, shared_len, max_len;
+  bool causal;
+  float scale;
+  float* part;             // workspace of paged_attention_workspace bytes
+};
+size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads);
+hipError_t paged_attention(const PagedAttn& a, hipStream_t s);
+
 // register-only bf16 MFMA loop (benchmark calibration); *flop: the launch's MFMA work
 hipError_t mfma_calibration(bool random_operands, int iters, int workgroups, double* flop, hipStream_t s);
 
