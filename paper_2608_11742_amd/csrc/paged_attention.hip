@@ -1,87 +1,748 @@
 // Attention over the pages of one layer: softmax(scale q k^T) v for the rows
-// of a batch of sequences, one pass over the keys with a running maximum m,
-// sum l and output o per row.
+// of a batch of sequences.
 //
-// One wave a row and head: a lane takes one key of 64 (its score), then one
-// or two dims (its part of o).
+// softmax over a set of keys is carried as (m, l, o): an exponent reference,
+// the sum of 2^(x - m) and the unnormalised output; two disjoint sets join as
+// m = max(m1, m2), l = l1 2^(m1 - m) + l2 2^(m2 - m), o alike.  So the keys of
+// a row may be divided freely:
+//   prefix   the positions that the whole batch shares.  The rows of all
+//            entries (and of the query heads of one key head) are stacked, so
+//            that a key tile is read once for all of them.
+//   tail     each entry's own positions after them, for its own rows.
+// and each of the two over workgroups by ranges of keys, where there are few
+// rows.  Every range leaves a record per row, and a merge joins them in order;
+// with one range in all the workgroup writes the output itself.
+//
+// Two kernels, by the number of stacked rows:
+//   narrow   up to 32 rows: bound by the keys and values it streams.  Four
+//            waves share the rows and take every fourth key step; a step's
+//            fragments come straight from memory into registers, K of the
+//            next step while the softmax runs, V after it (no LDS, no
+//            barrier), and the waves' states are joined through LDS at the end.
+//   wide     128 rows, 32 a wave: bound by MFMAs and the softmax's vector
+//            instructions.  Tiles of 64 keys go through a two-slot LDS ring,
+//            copied one tile ahead, on 32 x 32 MFMAs.
+// Scores are computed transposed (S^T = K Q^T): a lane then holds one row's
+// scores, and with the key order below its probabilities are, as they lie in
+// its registers, the operand of o^T += V^T P^T.  The exponent reference moves
+// only when a score passes it by 8 (log2 units), so o is rescaled rarely.
+// Probabilities of bf16 models are rounded to binary16 (below 2^8, 11
+// significant bits) for the product with binary16 values; the sums l take them
+// unrounded.
 #include <algorithm>
 
 #include "common.h"
 #include "kernels.h"
+#include "mainloop.h"
 
 namespace dllm {
 
 namespace {
 
-constexpr int kRowWaves = 4;
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kTile = 64;       // keys of a wide tile; ranges are whole tiles
+constexpr int kWideRows = 128;
+constexpr int kNarrowRows = 32;
+// floats per record: HD output values, m, l, padding to 16 bytes
+constexpr int record(int hd) { return hd + 4; }
 
-__device__ __forceinline__ float load_v(const float* p) { return *p; }
-__device__ __forceinline__ float load_v(const bf16_t* p) { return f16_lo(p->bits); }
+// How a part's keys and rows are divided: row tiles, key ranges and keys per range
+struct Part {
+  int row_tiles, ranges, range;
+};
 
-template <typename T, int HD>
-__global__ __launch_bounds__(kRowWaves * kWave) void row_attn_kernel(PagedAttn a) {
-  __shared__ float sq[kRowWaves][HD], sp[kRowWaves][kWave];
-  const dllm_kv_pages& p = a.p;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int h = blockIdx.y, b = blockIdx.z, i = blockIdx.x * kRowWaves + wave;
+// what a call's kernels share
+struct Job {
+  PagedAttn a;
+  float scale_log2;   // scale * log2(e)
+  int group;          // query heads per key head
+  Part prefix, tail;
+  bool direct;        // one range in all: the output itself
+};
+
+__device__ __forceinline__ int most_positions(const PagedAttn& a) { return a.p.max_blocks * a.p.page_len; }
+
+// whole pages of the prefix (0: none)
+__device__ __forceinline__ int shared_of(const PagedAttn& a) {
+  if (a.shared_len <= 0) return 0;
+  const int held = min(max(a.p.len[a.prefix_seq], 0), most_positions(a));
+  return min(a.shared_len, held) & ~(a.p.page_len - 1);
+}
+
+struct Entry {
+  int seq, held, rows;   // sequence (-1: none), its positions, rows of the entry
+};
+__device__ __forceinline__ Entry entry_of(const PagedAttn& a, int b) {
+  Entry e;
   const int s = a.seqs[b];
-  const int rows = a.n_rows ? min(max(a.n_rows[b], 0), a.max_rows) : a.max_rows;
-  if (i >= rows) return;
-  const bool known = s >= 0 && s < p.max_seqs;
-  const int most = p.max_blocks * p.page_len;
-  const int held = known ? min(max(p.len[s], 0), most) : 0;
-  const int limit = a.causal ? max(0, min(held, held - rows + i + 1)) : held;
-  const bool has_prefix = a.shared_len > 0 && a.prefix_seq >= 0 && a.prefix_seq < p.max_seqs;
-  const int shared = has_prefix ? min(a.shared_len, min(max(p.len[a.prefix_seq], 0), most)) / p.page_len * p.page_len : 0;
-  const size_t layer = size_t(a.layer) * p.n_pages;
-  const int kvh = h / (a.heads / p.n_kv_heads);
-  auto page_of = [&](int pos) {
-    const int32_t* t = p.table + size_t(pos < shared ? a.prefix_seq : s) * p.max_blocks;
-    return (layer + min(max(t[pos / p.page_len], 0), p.n_pages - 1)) * p.n_kv_heads + kvh;
-  };
-  const T* q = static_cast<const T*>(a.q.p) + b * a.q.seq + i * a.q.row + h * a.q.head;
-  for (int d = lane; d < HD; d += kWave) sq[wave][d] = load_f(q + d);
-  __builtin_amdgcn_wave_barrier();
-  float m = -INFINITY, l = 0.f, o[HD / kWave] = {};
-  for (int t = 0; t < limit; t += kWave) {
-    float x = -INFINITY;
-    if (t + lane < limit) {
-      const T* k = static_cast<const T*>(p.k) + (page_of(t + lane) * p.page_len + (t + lane) % p.page_len) * HD;
-      float dot = 0.f;
-      for (int d = 0; d < HD; ++d) dot = fmaf(sq[wave][d], load_f(k + d), dot);
-      x = dot * a.scale;
-    }
-    const float top = fmaxf(m, wave_max(x)), ref = top == -INFINITY ? 0.f : top;
-    const float e = expf(x - ref), alpha = expf(m - ref);
-    m = top;
-    l = l * alpha + wave_sum(e);
-    sp[wave][lane] = e;
-    __builtin_amdgcn_wave_barrier();
-    for (int c = 0; c < HD / kWave; ++c) o[c] *= alpha;
-    for (int j = 0; j < min(kWave, limit - t); ++j) {
-      const T* v = static_cast<const T*>(p.vt) + page_of(t + j) * HD * p.page_len + (t + j) % p.page_len;
-      for (int c = 0; c < HD / kWave; ++c)
-        o[c] = fmaf(sp[wave][j], load_v(v + (c * kWave + lane) * p.page_len), o[c]);
-    }
-    __builtin_amdgcn_wave_barrier();
+  e.seq = s >= 0 && s < a.p.max_seqs ? s : -1;
+  e.held = e.seq >= 0 ? min(max(a.p.len[e.seq], 0), most_positions(a)) : 0;
+  e.rows = a.n_rows ? min(max(a.n_rows[b], 0), a.max_rows) : a.max_rows;
+  return e;
+}
+// positions that row i of the entry sees
+__device__ __forceinline__ int limit_of(const PagedAttn& a, const Entry& e, int i) {
+  return a.causal ? max(0, min(e.held, e.held - e.rows + i + 1)) : e.held;
+}
+
+// A workgroup's share: rows row0 .. (stacked as ((entry * max_rows) + row) *
+// group + query head), keys k0 .. k1 - 1 of the table, record index.
+struct Share {
+  int row0, row_end, k0, k1, part;
+  const int32_t* table;
+};
+
+// False if the share is empty.
+__device__ __forceinline__ bool share_of(const Job& j, int item, bool in_prefix, int tile_rows, Share& w) {
+  const PagedAttn& a = j.a;
+  const int per = a.max_rows * j.group;   // stacked rows of one entry
+  const int s = shared_of(a);
+  if (in_prefix) {
+    const int r = item / j.prefix.row_tiles;
+    w.row0 = item % j.prefix.row_tiles * tile_rows;
+    w.row_end = a.n * per;
+    w.k0 = r * j.prefix.range;
+    w.k1 = min(w.k0 + j.prefix.range, s);
+    w.part = r;
+    w.table = a.p.table + size_t(a.prefix_seq) * a.p.max_blocks;
+    return w.k0 < w.k1;
   }
-  T* out = static_cast<T*>(a.out.p) + b * a.out.seq + i * a.out.row + h * a.out.head;
-  for (int c = 0; c < HD / kWave; ++c) store_f(out + c * kWave + lane, limit > 0 ? o[c] / l : 0.f);
+  const int b = item / (j.tail.row_tiles * j.tail.ranges), i = item % (j.tail.row_tiles * j.tail.ranges);
+  const int r = i / j.tail.row_tiles;
+  const Entry e = entry_of(a, b);
+  w.row0 = b * per + i % j.tail.row_tiles * tile_rows;
+  w.row_end = (b + 1) * per;
+  w.k0 = s + r * j.tail.range;
+  w.k1 = r + 1 == j.tail.ranges ? e.held : min(w.k0 + j.tail.range, e.held);
+  w.part = j.prefix.ranges + r;
+  w.table = a.p.table + size_t(max(e.seq, 0)) * a.p.max_blocks;
+  // an entry without positions still has its rows set to 0 where nothing is joined
+  return w.row0 < b * per + e.rows * j.group && (w.k0 < w.k1 || j.direct);
+}
+
+// a stacked row's place
+struct RowAt {
+  int b, i, g;
+};
+__device__ __forceinline__ RowAt row_at(const Job& j, int row) {
+  RowAt r;
+  r.g = row % j.group;
+  const int t = row / j.group;
+  r.b = t / j.a.max_rows;
+  r.i = t % j.a.max_rows;
+  return r;
+}
+
+__device__ __forceinline__ float* record_of(const Job& j, int part, const RowAt& r, int kvh, int hd) {
+  const size_t row = (size_t(r.b) * j.a.max_rows + r.i) * j.a.heads + kvh * j.group + r.g;
+  return j.a.part + (size_t(part) * j.a.n * j.a.max_rows * j.a.heads + row) * record(hd);
+}
+
+// lane l's value of lanes l, l ^ 32 joined
+__device__ __forceinline__ float pair_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+// of lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float quad_max(float x) {
+  const float m = pair_max(x);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  const float m = pair_sum(x);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// smallest / largest of a value over the wave, as a scalar
+__device__ __forceinline__ int wave_min_int(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o, kWave));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// ---------------------------------------------------------------- narrow
+
+// NQB blocks of 16 rows.  A key step is KS keys in blocks of 16; bf16 keys of
+// a 32-key half are gathered so that output element i of lane group g in
+// block kk is key 8 g + 4 kk + i: the lane's 8 probabilities of the half are 8
+// consecutive keys, one 16-byte chunk of a V^T row.
+template <typename T, int HD, int NQB>
+struct Narrow {
+  static constexpr bool kHalf = sizeof(T) == 2;
+  static constexpr int E = 16 / int(sizeof(T));             // elements per chunk
+  static constexpr int CK = HD / E;                         // chunks per key row
+  // a step's K takes 64 registers at most, its V as many; half of that beside the state of two row blocks
+  static constexpr int KS = (NQB == 1 ? 16 : 8) * 1024 / (HD * int(sizeof(T))) < 64
+                                ? (NQB == 1 ? 16 : 8) * 1024 / (HD * int(sizeof(T))) : 64;
+  static constexpr int NB = KS / 16;                        // 16-key blocks of a step
+  static constexpr int QS = CK / 4;                         // MFMA steps over head_dim
+  static constexpr int NDB = HD / 16;
+  static constexpr int NV = KS / (4 * E);                   // V chunks per dim row and lane
+  static constexpr int STATE = NDB * 4 + 2;                 // floats a lane hands over per 16 rows
+
+  __device__ __forceinline__ static int key_of(int kb, int r) {
+    if constexpr (kHalf) return 32 * (kb >> 1) + 8 * (r >> 2) + 4 * (kb & 1) + (r & 3);
+    else return 16 * kb + r;
+  }
+
+  __device__ static void run(const Job& j, const Share& w, int kvh, float* smem) {
+    const PagedAttn& a = j.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int fr = lane & 15, g = lane >> 4;
+    const int shift = 31 - __builtin_clz(a.p.page_len), pmask = a.p.page_len - 1;
+    const size_t head_stride = size_t(a.p.page_len) * HD;
+    const size_t page_stride = head_stride * a.p.n_kv_heads;
+    const size_t base = (size_t(a.layer) * a.p.n_pages * a.p.n_kv_heads + kvh) * head_stride;
+    const T* K = static_cast<const T*>(a.p.k) + base;
+    const T* V = static_cast<const T*>(a.p.vt) + base;
+    const int last_block = max(w.k1 - 1, 0) >> shift;
+
+    RowAt at[NQB];
+    u32x4 qf[NQB][QS];
+    int lim[NQB], lim_min = 1 << 30;
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      at[qb] = row_at(j, min(w.row0 + 16 * qb + fr, w.row_end - 1));
+      const T* q = static_cast<const T*>(a.q.p) + at[qb].b * a.q.seq + at[qb].i * a.q.row +
+                   (kvh * j.group + at[qb].g) * a.q.head;
+#pragma unroll
+      for (int st = 0; st < QS; ++st) qf[qb][st] = *reinterpret_cast<const u32x4*>(q + (4 * st + g) * E);
+      lim[qb] = min(limit_of(a, entry_of(a, at[qb].b), at[qb].i), w.k1);
+      lim_min = min(lim_min, lim[qb]);
+    }
+    lim_min = wave_min_int(lim_min);
+
+    // page ids of a step's 16-key groups (past the last key: its page again)
+    auto pages_at = [&](int k0, int (&id)[NB]) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int p = w.table[min((k0 + 16 * i) >> shift, last_block)];
+        id[i] = min(max(p, 0), a.p.n_pages - 1);
+      }
+    };
+    u32x4 kf[NB][QS], vf[NDB][NV];
+    auto load_k = [&](int k0, const int (&id)[NB]) {
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb) {
+        const int key = key_of(kb, fr);
+        const int page = kHalf ? (fr < 8 ? id[kb & ~1] : id[kb | 1]) : id[kb];
+        const T* row = K + page * page_stride + ((k0 + key) & pmask) * HD;
+#pragma unroll
+        for (int st = 0; st < QS; ++st) kf[kb][st] = *reinterpret_cast<const u32x4*>(row + (4 * st + g) * E);
+      }
+    };
+    auto load_v = [&](int k0, const int (&id)[NB]) {
+#pragma unroll
+      for (int c = 0; c < NV; ++c) {
+        const int key = (4 * c + g) * E;   // first of this lane's chunk
+        const int page = kHalf ? (g < 2 ? id[2 * c] : id[2 * c + 1]) : id[c];
+        const T* row = V + page * page_stride + size_t(fr) * a.p.page_len + ((k0 + key) & pmask);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+          vf[db][c] = *reinterpret_cast<const u32x4*>(row + 16 * db * a.p.page_len);
+      }
+    };
+
+    f32x4 o[NDB][NQB];
+    float m[NQB], l[NQB];
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      m[qb] = -INFINITY;
+      l[qb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[db][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    int k0 = w.k0 + wave * KS;
+    int id[NB];
+    if (k0 < w.k1) {
+      pages_at(k0, id);
+      load_k(k0, id);
+      load_v(k0, id);
+    }
+    for (; k0 < w.k1; k0 += kWaves * KS) {
+      const int next = k0 + kWaves * KS;
+      const bool more = next < w.k1;
+      if (more) pages_at(next, id);
+      f32x4 sc[NB][NQB];
+#pragma unroll
+      for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          sc[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int st = 0; st < QS; ++st) Mfma<T>::run(sc[kb][qb], kf[kb][st], qf[qb][st]);
+        }
+      if (more) load_k(next, id);
+      if (k0 + KS > lim_min) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (k0 + key_of(kb, 4 * g + i) >= lim[qb]) sc[kb][qb][i] = -INFINITY;
+      }
+      bool moved = false;
+      float alpha[NQB];
+#pragma unroll
+      for (int qb = 0; qb < NQB; ++qb) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[kb][qb][i]);
+        top = quad_max(top) * j.scale_log2;
+        const float mn = top > m[qb] + 8.f ? top : m[qb];
+        const float ref = mn == -INFINITY ? 0.f : mn;   // a row that has seen no key yet: exponents 2^-inf
+        alpha[qb] = __builtin_amdgcn_exp2f(m[qb] - ref);
+        moved = moved || mn != m[qb];
+        m[qb] = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc[kb][qb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][qb][i], j.scale_log2, -ref));
+            sum += sc[kb][qb][i];
+          }
+        l[qb] = l[qb] * alpha[qb] + sum;
+      }
+      if (__any(moved)) {
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) o[db][qb] *= alpha[qb];
+      }
+      if (k0 + KS > w.k1) {   // values past the last key: whatever they are, times 0
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          const int left = w.k1 - (k0 + (4 * c + g) * E);   // valid elements of this lane's chunks
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t keep = kHalf ? (left > 2 * x + 1 ? ~0u : left > 2 * x ? 0xffffu : 0u) : (left > x ? ~0u : 0u);
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) vf[db][c][x] &= keep;
+          }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NV; ++c)
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          u32x4 pf;
+          if constexpr (kHalf) {
+            pf = u32x4{pack_f16x2(sc[2 * c][qb][0], sc[2 * c][qb][1]), pack_f16x2(sc[2 * c][qb][2], sc[2 * c][qb][3]),
+                       pack_f16x2(sc[2 * c + 1][qb][0], sc[2 * c + 1][qb][1]),
+                       pack_f16x2(sc[2 * c + 1][qb][2], sc[2 * c + 1][qb][3])};
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pf[i] = __float_as_uint(sc[c][qb][i]);
+          }
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            if constexpr (kHalf) MfmaF16::run(o[db][qb], vf[db][c], pf);
+            else Mfma<float>::run(o[db][qb], vf[db][c], pf);
+          }
+        }
+      if (more) load_v(next, id);
+    }
+
+    // join the waves' states, 16 rows at a time: wave w sums dim blocks w, w + 4, ..
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      float* mine = smem + wave * STATE * kWave + lane;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[(4 * db + i) * kWave] = o[db][qb][i];
+      mine[(STATE - 2) * kWave] = m[qb];
+      mine[(STATE - 1) * kWave] = quad_sum(l[qb]);
+      __syncthreads();
+      float mw[kWaves], top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        mw[v] = smem[(v * STATE + STATE - 2) * kWave + lane];
+        top = fmaxf(top, mw[v]);
+      }
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        mw[v] = __builtin_amdgcn_exp2f(mw[v] - ref);
+        sum += smem[(v * STATE + STATE - 1) * kWave + lane] * mw[v];
+      }
+      const int row = w.row0 + 16 * qb + fr;
+      const bool live = row < w.row_end && at[qb].i < entry_of(a, at[qb].b).rows;
+      const float inv = lim[qb] > 0 ? 1.f / sum : 0.f;
+      T* out = static_cast<T*>(a.out.p) + at[qb].b * a.out.seq + at[qb].i * a.out.row +
+               (kvh * j.group + at[qb].g) * a.out.head;
+      float* rec = record_of(j, w.part, at[qb], kvh, HD);
+      for (int db = wave; db < NDB; db += kWaves) {
+        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] += smem[(v * STATE + 4 * db + i) * kWave + lane] * mw[v];
+        if (!live) continue;
+        if (j.direct) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) store_f(out + 16 * db + 4 * g + i, lim[qb] > 0 ? x[i] * inv : 0.f);
+        } else {
+          *reinterpret_cast<f32x4*>(rec + 16 * db + 4 * g) = x;
+        }
+      }
+      if (live && !j.direct && wave == 0 && g == 0) {
+        rec[HD] = top;
+        rec[HD + 1] = sum;
+      }
+      if (qb + 1 < NQB) __syncthreads();
+    }
+  }
+};
+
+// grid: prefix items, then tail items; blockIdx.y the key head
+template <typename T, int HD, int NQB>
+__global__ __launch_bounds__(kThreads, 2) void narrow_kernel(Job j, int prefix_items) {
+  __shared__ __attribute__((aligned(16))) float smem[kWaves * Narrow<T, HD, NQB>::STATE * kWave];
+  const bool in_prefix = int(blockIdx.x) < prefix_items;
+  Share w;
+  if (!share_of(j, in_prefix ? int(blockIdx.x) : int(blockIdx.x) - prefix_items, in_prefix, 16 * NQB, w)) return;
+  Narrow<T, HD, NQB>::run(j, w, blockIdx.y, smem);
+}
+
+// ---------------------------------------------------------------- wide
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+
+// 16 bytes per lane from global memory straight into LDS (lane l: lds + 16 l)
+__device__ __forceinline__ void copy16(const void* src, uint32_t lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),
+                                   reinterpret_cast<__attribute__((address_space(3))) void*>(static_cast<uintptr_t>(lds)),
+                                   16, 0, 0);
+}
+
+// bf16 models.  MFMA row r of a 32-key half is key r with bits 2 and 3
+// exchanged: output registers 8 s .. 8 s + 7 of lane half f are then keys
+// 16 s + 8 f .. + 7, the chunk of V^T that this lane half multiplies in step s.
+template <int HD>
+struct Wide {
+  static constexpr int RB = HD * 2;                 // bytes of a key row
+  static constexpr int CK = RB / 16;                // chunks of a key row
+  static constexpr int KB = kTile * RB;             // K tile; V^T tile: HD rows of 128 bytes
+  static constexpr int SLOT = 2 * KB;
+  static constexpr int SMEM = 2 * SLOT;
+  static constexpr int KROWS = kWave / CK;          // key rows of one 1 KB copy
+  static constexpr int IC = KB / 1024 / kWaves;     // copies a wave issues for K, and for V
+  static constexpr int QS = HD / 16;                // MFMA steps over head_dim
+  static constexpr int NDB = HD / 32;
+
+  // chunk slots: rows read together by 8 lanes fall on different banks
+  __device__ __forceinline__ static int kswz(int r) { return (r & 3) | ((r >> 1) & 4); }
+
+  __device__ static void run(const Job& j, const Share& w, int kvh, uint8_t* smem) {
+    const PagedAttn& a = j.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int fr = lane & 31, f = lane >> 5;
+    const int shift = 31 - __builtin_clz(a.p.page_len), pmask = a.p.page_len - 1;
+    const size_t head_bytes = size_t(a.p.page_len) * RB, page_bytes = head_bytes * a.p.n_kv_heads;
+    const size_t base = (size_t(a.layer) * a.p.n_pages * a.p.n_kv_heads + kvh) * head_bytes;
+    const uint8_t* K = static_cast<const uint8_t*>(a.p.k) + base;
+    const uint8_t* V = static_cast<const uint8_t*>(a.p.vt) + base;
+    const int last_block = max(w.k1 - 1, 0) >> shift;
+    const uint32_t lds0 = lds_address(smem);
+
+    const RowAt at = row_at(j, min(w.row0 + 32 * wave + fr, w.row_end - 1));
+    u32x4 qf[QS];
+    const bf16_t* q = static_cast<const bf16_t*>(a.q.p) + at.b * a.q.seq + at.i * a.q.row +
+                      (kvh * j.group + at.g) * a.q.head;
+#pragma unroll
+    for (int st = 0; st < QS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(q + (2 * st + f) * 8);
+    const Entry entry = entry_of(a, at.b);
+    const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
+    const int lim_min = wave_min_int(lim);
+
+    auto pages_at = [&](int k0, int (&id)[4]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int p = w.table[min((k0 + 16 * i) >> shift, last_block)];
+        id[i] = min(max(p, 0), a.p.n_pages - 1);
+      }
+    };
+    // this lane's source of each copy: a key row's chunk, a dim row's chunk
+    const int kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vd;
+    auto issue = [&](int k0, const int (&id)[4], int slot) {
+      const uint32_t dst = lds0 + slot * SLOT;
+#pragma unroll
+      for (int i = 0; i < IC; ++i) {
+        const int grp = wave * IC + i, r = grp * KROWS + kr;
+        const int sub = grp * KROWS / 16;   // the wave's copies of one i share a 16-key group
+        const int page = sub == 0 ? id[0] : sub == 1 ? id[1] : sub == 2 ? id[2] : id[3];
+        const uint8_t* src = K + page * page_bytes + ((k0 + sub * 16) & pmask) * RB;
+        copy16(src + (r & 15) * RB + ((lane % CK) ^ kswz(r)) * 16, dst + grp * 1024);
+      }
+      const int page = vc < 4 ? (vc < 2 ? id[0] : id[1]) : (vc < 6 ? id[2] : id[3]);
+      const uint8_t* src = V + page * page_bytes + size_t(vd) * (a.p.page_len * 2) + ((k0 + 8 * vc) & pmask) * 2;
+#pragma unroll
+      for (int i = 0; i < IC; ++i) {
+        const int grp = wave * IC + i;
+        copy16(src + size_t(grp) * 8 * (a.p.page_len * 2), dst + KB + grp * 1024);
+      }
+    };
+
+    f32x16 o[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    int id[4];
+    pages_at(w.k0, id);
+    if (w.k0 < w.k1) issue(w.k0, id, 0);
+    pages_at(w.k0 + kTile, id);
+    int slot = 0;
+    for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
+      wait_vmcnt<0>();
+      __syncthreads();   // tile k0 has landed; the other slot has been read
+      const uint8_t* sk = smem + slot * SLOT;
+      uint8_t* sv = smem + slot * SLOT + KB;
+      if (k0 + kTile > w.k1) {   // values past the last key: whatever they are, times 0
+        for (int c = tid; c < HD * 8; c += kThreads) {
+          const int d = c >> 3, left = w.k1 - k0 - 8 * (c & 7);
+          if (left >= 8) continue;
+          u32x4* p = reinterpret_cast<u32x4*>(sv + d * 128 + (((c & 7) ^ (d & 7)) << 4));
+          u32x4 x = *p;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] &= left > 2 * i + 1 ? ~0u : left > 2 * i ? 0xffffu : 0u;
+          *p = x;
+        }
+        __syncthreads();
+      } else if (k0 + kTile < w.k1) {
+        issue(k0 + kTile, id, slot ^ 1);
+        pages_at(k0 + 2 * kTile, id);
+      }
+      f32x16 sc[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[h][i] = 0.f;
+#pragma unroll
+      for (int st = 0; st < QS; ++st)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = 32 * h + ((fr & 0x13) | ((fr & 4) << 1) | ((fr & 8) >> 1));
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(sk + r * RB + (((2 * st + f) ^ kswz(r)) << 4));
+          sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                          __builtin_bit_cast(bf16x8, qf[st]), sc[h], 0, 0, 0);
+        }
+      // element i of half h: key 32 h + 16 (i / 8) + 8 f + i % 8
+      if (k0 + kTile > lim_min) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (k0 + 32 * h + 16 * (i >> 3) + 8 * f + (i & 7) >= lim) sc[h][i] = -INFINITY;
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[h][i]);
+      top = pair_max(top) * j.scale_log2;
+      const float mn = top > m + 8.f ? top : m;
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      if (__any(mn != m)) {
+        const float alpha = __builtin_amdgcn_exp2f(m - ref);
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) o[db] *= alpha;
+      }
+      m = mn;
+      u32x4 pf[4];
+      float sum = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(sc[h][i], j.scale_log2, -ref));
+          const float y = __builtin_amdgcn_exp2f(fmaf(sc[h][i + 1], j.scale_log2, -ref));
+          sum += x + y;
+          pf[2 * h + (i >> 3)][(i & 7) >> 1] = pack_f16x2(x, y);
+        }
+      l += sum;
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          const int d = 32 * db + fr;
+          const u32x4 vf = *reinterpret_cast<const u32x4*>(sv + d * 128 + (((2 * st + f) ^ (d & 7)) << 4));
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf), __builtin_bit_cast(half8, pf[st]),
+                                                         o[db], 0, 0, 0);
+        }
+    }
+    l = pair_sum(l);
+    if (w.row0 + 32 * wave + fr >= w.row_end || at.i >= entry.rows) return;
+    // element i of block db: dim 32 db + 8 (i / 4) + 4 f + i % 4
+    if (j.direct) {
+      bf16_t* out = static_cast<bf16_t*>(a.out.p) + at.b * a.out.seq + at.i * a.out.row +
+                    (kvh * j.group + at.g) * a.out.head;
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          store_f(out + 32 * db + 8 * (i >> 2) + 4 * f + (i & 3), lim_row > 0 ? o[db][i] * inv : 0.f);
+    } else {
+      float* rec = record_of(j, w.part, at, kvh, HD);
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(rec + 32 * db + 2 * i + 4 * f) =
+              f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]};
+      if (f == 0) {
+        rec[HD] = m;
+        rec[HD + 1] = l;
+      }
+    }
+  }
+};
+
+template <int HD>
+__global__ __launch_bounds__(kThreads, 2) void wide_kernel(Job j, int prefix_items) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[Wide<HD>::SMEM];
+  const bool in_prefix = int(blockIdx.x) < prefix_items;
+  Share w;
+  if (!share_of(j, in_prefix ? int(blockIdx.x) : int(blockIdx.x) - prefix_items, in_prefix, kWideRows, w)) return;
+  Wide<HD>::run(j, w, blockIdx.y, smem);
+}
+
+// ---------------------------------------------------------------- merge
+
+// out[row] = sum_r o_r 2^(m_r - m) / sum_r l_r 2^(m_r - m) over the ranges that
+// hold positions the row sees, in order; HD / 4 lanes a row
+template <typename T, int HD>
+__global__ __launch_bounds__(kThreads) void join_kernel(Job j) {
+  constexpr int kLanes = HD / 4;
+  const PagedAttn& a = j.a;
+  const int row = blockIdx.x * (kThreads / kLanes) + int(threadIdx.x) / kLanes, c = int(threadIdx.x) % kLanes * 4;
+  if (row >= a.n * a.max_rows * a.heads) return;
+  const int h = row % a.heads, t = row / a.heads, b = t / a.max_rows, i = t % a.max_rows;
+  const Entry e = entry_of(a, b);
+  if (i >= e.rows) return;
+  const int s = shared_of(a), lim = limit_of(a, e, i);
+  const int np = j.prefix.ranges ? (min(lim, s) + j.prefix.range - 1) / j.prefix.range : 0;
+  const int nt = lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
+  const size_t stride = size_t(a.n) * a.max_rows * a.heads * record(HD);
+  const float* rec = a.part + size_t(row) * record(HD);
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < np + nt; ++r) {
+    const float* x = rec + (r < np ? r : j.prefix.ranges + r - np) * stride;
+    const float mr = x[HD], lr = x[HD + 1];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(x + c);
+    const float mn = fmaxf(m, mr), ref = mn == -INFINITY ? 0.f : mn;
+    const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(mr - ref);
+    l = l * w0 + lr * w1;
+    o = o * w0 + v * w1;
+    m = mn;
+  }
+  T* out = static_cast<T*>(a.out.p) + b * a.out.seq + i * a.out.row + h * a.out.head + c;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) store_f(out + x, lim > 0 ? o[x] / l : 0.f);
+}
+
+// ---------------------------------------------------------------- host
+
+constexpr int kSlots = 512;      // workgroups at a time: two on each of 256 CUs
+constexpr int kMaxRanges = 64;
+
+bool is_wide(int dtype, int rows) { return dtype == DLLM_BF16 && rows > kNarrowRows; }
+
+// most key ranges that a part of `wgs` workgroups a range is ever given
+int most_ranges(int64_t wgs) { return int(std::min<int64_t>(kMaxRanges, std::max<int64_t>(1, 2 * kSlots / std::max<int64_t>(wgs, 1)))); }
+
+// rows stacked per key head, in `blocks` separate groups (entries of a tail)
+Part plan_part(int dtype, int rows, int64_t blocks, int kv_heads, int64_t keys, bool wide) {
+  Part p;
+  p.row_tiles = cdiv(rows, wide ? kWideRows : rows > 16 ? kNarrowRows : 16);
+  const int step = wide ? 4 * kTile : 4 * kTile;   // keys of the shortest range
+  const int64_t tiles = (keys + kTile - 1) / kTile;
+  const int most = most_ranges(p.row_tiles * blocks * kv_heads);
+  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>(most, keys / step));
+  p.range = int((tiles + ranges - 1) / ranges * kTile);
+  p.range = std::max(p.range, kTile);
+  p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
+  return p;
 }
 
 }  // namespace
 
-size_t paged_attention_workspace(const dllm_kv_pages&, int, int, int) { return 16; }
+size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads) {
+  const int group = heads / p.n_kv_heads;
+  auto ranges = [&](int rows, int blocks) {
+    const int tile = is_wide(p.dtype, rows) ? kWideRows : rows > 16 ? kNarrowRows : 16;
+    return most_ranges(int64_t(cdiv(rows, tile)) * blocks * p.n_kv_heads);
+  };
+  const size_t parts = ranges(n * max_rows * group, 1) + ranges(max_rows * group, n);
+  return parts * n * max_rows * heads * record(p.head_dim) * sizeof(float);
+}
 
 hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
-  const dim3 grid(cdiv(a.max_rows, kRowWaves), a.heads, a.n), block(kRowWaves * kWave);
-  auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
-    return hipGetLastError();
+  Job j{};
+  j.a = a;
+  j.scale_log2 = a.scale * 1.4426950408889634f;
+  j.group = a.heads / a.p.n_kv_heads;
+  const int dt = a.p.dtype, hd = a.p.head_dim, kvh = a.p.n_kv_heads;
+  const int64_t most = int64_t(a.p.max_blocks) * a.p.page_len;
+  const int64_t shared = std::min<int64_t>(a.shared_len, most) / a.p.page_len * a.p.page_len;
+  const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
+  const bool wide_p = is_wide(dt, rows_p), wide_t = is_wide(dt, rows_t);
+  int prefix_items = 0;
+  if (shared > 0) {
+    j.prefix = plan_part(dt, rows_p, 1, kvh, shared, wide_p);
+    prefix_items = j.prefix.row_tiles * j.prefix.ranges;
+  } else {
+    j.prefix = Part{0, 0, kTile};
+    j.a.shared_len = 0;
+  }
+  j.tail = plan_part(dt, rows_t, a.n, kvh, std::max<int64_t>(1, std::min<int64_t>(a.max_len, most) - shared), wide_t);
+  const int tail_items = a.n * j.tail.row_tiles * j.tail.ranges;
+  j.direct = prefix_items == 0 && j.tail.ranges == 1;
+
+  auto run = [&](auto kernel, int prefix, int tail) {
+    hipLaunchKernelGGL(kernel, dim3(prefix + tail, kvh), dim3(kThreads), 0, s, j, prefix);
   };
-  if (a.p.dtype == DLLM_BF16)
-    return a.p.head_dim == 128 ? launch(row_attn_kernel<bf16_t, 128>) : launch(row_attn_kernel<bf16_t, 64>);
-  return a.p.head_dim == 128 ? launch(row_attn_kernel<float, 128>) : launch(row_attn_kernel<float, 64>);
+  auto narrow = [&](int rows, int prefix, int tail) {
+    if (dt == DLLM_BF16) {
+      if (hd == 128) rows > 16 ? run(narrow_kernel<bf16_t, 128, 2>, prefix, tail) : run(narrow_kernel<bf16_t, 128, 1>, prefix, tail);
+      else rows > 16 ? run(narrow_kernel<bf16_t, 64, 2>, prefix, tail) : run(narrow_kernel<bf16_t, 64, 1>, prefix, tail);
+    } else {
+      if (hd == 128) rows > 16 ? run(narrow_kernel<float, 128, 2>, prefix, tail) : run(narrow_kernel<float, 128, 1>, prefix, tail);
+      else rows > 16 ? run(narrow_kernel<float, 64, 2>, prefix, tail) : run(narrow_kernel<float, 64, 1>, prefix, tail);
+    }
+  };
+  auto wide = [&](int prefix, int tail) {
+    hd == 128 ? run(wide_kernel<128>, prefix, tail) : run(wide_kernel<64>, prefix, tail);
+  };
+  if (prefix_items) wide_p ? wide(prefix_items, 0) : narrow(rows_p, prefix_items, 0);
+  wide_t ? wide(0, tail_items) : narrow(rows_t, 0, tail_items);
+  if (!j.direct) {
+    auto join = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(cdiv(a.n * a.max_rows * a.heads, kThreads / (hd / 4))), dim3(kThreads), 0, s, j);
+    };
+    if (dt == DLLM_BF16) hd == 128 ? join(join_kernel<bf16_t, 128>) : join(join_kernel<bf16_t, 64>);
+    else hd == 128 ? join(join_kernel<float, 128>) : join(join_kernel<float, 64>);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace dllm
