@@ -242,7 +242,8 @@ class KvPages:
         if any(t.device != k.device or not t.is_contiguous() for t in (k, vt, refs, table, len)):
             raise ValueError("the arrays must be contiguous tensors of one device")
         self.k, self.vt, self.refs, self.table, self.len = k, vt, refs, table, len
-        self.page_len, self.head_dim, self.n_kv_heads, self.device = page_len, hd, heads, k.device
+        self.page_len, self.head_dim, self.n_kv_heads, self.dtype = page_len, hd, heads, k.dtype
+        self._index = k.get_device()
         self._c = _abi.KvPagesC(k.data_ptr(), vt.data_ptr(), refs.data_ptr(), table.data_ptr(), len.data_ptr(), L,
                                 n_pages, heads, hd, page_len, table.shape[0], table.shape[1],
                                 DLLM_BF16 if k.dtype == torch.bfloat16 else DLLM_F32)
@@ -261,30 +262,44 @@ class KvPages:
         return pages
 
 
-def _ids(pages: KvPages, t, n: int | None = None):
+_I32 = torch.int32
+
+
+def _ids(pages: KvPages, t, n: int):
     """Address of an int32 list of n entries beside the pages' arrays."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.device != pages.device or not t.is_contiguous() or (n is not None and t.numel() != n):
+    if t.dtype is not _I32 or t.get_device() != pages._index or t.numel() != n or not t.is_contiguous():
         raise ValueError("sequence lists, counts and status are contiguous int32 tensors, one value an entry, beside the pages")
     return t.data_ptr()
 
 
-def _rows(pages: KvPages, t, heads: int, name: str):
+def _rows(pages: KvPages, t, name: str):
     """t [entries, rows, heads, head_dim], any strides over contiguous head_dim, as dllm_rows."""
-    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != pages.head_dim or t.stride(3) != 1:
-        raise ValueError(f"{name} must be [entries, rows, {heads}, {pages.head_dim}] with contiguous rows")
-    if t.dtype != pages.k.dtype or t.device != pages.device:
+    n, rows, heads, hd = t.shape
+    seq, row, head, one = t.stride()
+    if hd != pages.head_dim or one != 1:
+        raise ValueError(f"{name} must be [entries, rows, heads, {pages.head_dim}] with contiguous rows")
+    if t.dtype is not pages.dtype or t.get_device() != pages._index:
         raise ValueError(f"{name} must have the type and device of the pages' keys")
     # a dimension of one has no stride to speak of
-    st = [0 if n == 1 else step for n, step in zip(t.shape, t.stride())]
-    return C.byref(_abi.Rows(t.data_ptr(), st[0], st[1], st[2]))
+    return _abi.Rows(t.data_ptr(), seq if n > 1 else 0, row if rows > 1 else 0, head if heads > 1 else 0)
+
+
+def _scratch(pages: KvPages, ws):
+    """Address and size of a workspace beside the pages."""
+    if ws.get_device() != pages._index or not ws.is_contiguous():
+        raise ValueError("the workspace must be contiguous and beside the pages")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _page_stream(pages: KvPages, stream):
-    if stream is None and pages.device.index != torch.cuda.current_device():
+    if stream is not None:
+        return _stream(stream)
+    dev = torch.cuda.current_device()
+    if dev != pages._index:
         raise ValueError("the pages are on another device than the current one")
-    return _stream(stream)
+    return _raw_stream(dev)
 
 
 def kv_pages_init(pages: KvPages, stream=None):
@@ -294,21 +309,21 @@ def kv_pages_init(pages: KvPages, stream=None):
 def kv_pages_grow(pages: KvPages, seqs, add, status, stream=None):
     """Sequences seqs[i] grow by add[i] positions; status (int32, device) receives a KV_PAGES_ code."""
     n = seqs.numel()
-    _check(lib().kv_pages_grow(pages._ref, _ids(pages, seqs), _ids(pages, add, n), n, _ids(pages, status, 1),
+    _check(lib().kv_pages_grow(pages._ref, _ids(pages, seqs, n), _ids(pages, add, n), n, _ids(pages, status, 1),
                                _page_stream(pages, stream)))
 
 
 def kv_pages_fork(pages: KvPages, src, dst, status, keep=None, stream=None):
     """Empty sequences dst[i] become the first keep[i] positions of src[i] (all of them without keep)."""
     n = src.numel()
-    _check(lib().kv_pages_fork(pages._ref, _ids(pages, src), _ids(pages, dst, n), _ids(pages, keep, n), n,
+    _check(lib().kv_pages_fork(pages._ref, _ids(pages, src, n), _ids(pages, dst, n), _ids(pages, keep, n), n,
                                _ids(pages, status, 1), _page_stream(pages, stream)))
 
 
 def kv_pages_free(pages: KvPages, seqs, status, keep=None, stream=None):
     """Sequences seqs[i] keep their first keep[i] positions (none without keep)."""
     n = seqs.numel()
-    _check(lib().kv_pages_free(pages._ref, _ids(pages, seqs), _ids(pages, keep, n), n, _ids(pages, status, 1),
+    _check(lib().kv_pages_free(pages._ref, _ids(pages, seqs, n), _ids(pages, keep, n), n, _ids(pages, status, 1),
                                _page_stream(pages, stream)))
 
 
@@ -318,18 +333,17 @@ def kv_pages_compact_workspace_bytes(pages: KvPages) -> int:
 
 def kv_pages_compact(pages: KvPages, n_used, ws, stream=None):
     """Pages in use move to ids 0 .. n_used-1 (n_used: int32, device)."""
-    _check(lib().kv_pages_compact(pages._ref, _ids(pages, n_used, 1), _p(ws), ws.numel() * ws.element_size(),
+    _check(lib().kv_pages_compact(pages._ref, _ids(pages, n_used, 1), *_scratch(pages, ws),
                                   _page_stream(pages, stream)))
 
 
 def kv_pages_write(pages: KvPages, layer: int, seqs, k, v, n_rows=None, stream=None):
     """k, v [entries, rows, kv heads, head_dim]: the last n_rows[b] (or all rows) positions of sequence seqs[b]."""
-    n = seqs.numel()
-    if k.shape[0] != n or v.shape[:2] != k.shape[:2]:
-        raise ValueError("k and v need one batch entry per sequence and the same rows")
-    _check(lib().kv_pages_write(pages._ref, layer, _ids(pages, seqs), n, k.shape[1], _ids(pages, n_rows, n),
-                                _rows(pages, k, pages.n_kv_heads, "k"), _rows(pages, v, pages.n_kv_heads, "v"),
-                                _page_stream(pages, stream)))
+    n, rows, heads, _ = k.shape
+    if seqs.numel() != n or v.shape != k.shape or heads != pages.n_kv_heads:
+        raise ValueError("k and v need one batch entry per sequence, the pages' heads and the same shape")
+    _check(lib().kv_pages_write(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n),
+                                _rows(pages, k, "k"), _rows(pages, v, "v"), _page_stream(pages, stream)))
 
 
 def kv_pages_attention_workspace_bytes(pages: KvPages, n: int, max_rows: int, n_heads: int) -> int:
@@ -347,10 +361,10 @@ def kv_pages_attention(pages: KvPages, layer: int, seqs, q, out, ws, n_rows=None
         raise ValueError("q and out need one batch entry per sequence and the same shape")
     if max_len is None:
         max_len = pages.table.shape[1] * pages.page_len
-    _check(lib().kv_pages_attention(pages._ref, layer, _ids(pages, seqs), n, rows, _ids(pages, n_rows, n), heads,
-                                    _rows(pages, q, heads, "q"), _rows(pages, out, heads, "out"), prefix_seq,
-                                    shared_len, max_len, int(causal), hd ** -0.5 if scale is None else scale, _p(ws),
-                                    ws.numel() * ws.element_size(), _page_stream(pages, stream)))
+    _check(lib().kv_pages_attention(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n), heads,
+                                    _rows(pages, q, "q"), _rows(pages, out, "out"), prefix_seq,
+                                    shared_len, max_len, int(causal), hd ** -0.5 if scale is None else scale,
+                                    *_scratch(pages, ws), _page_stream(pages, stream)))
 
 
 # ---------------------------------------------------------------- scheduler

@@ -42,7 +42,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 64;       // keys of a wide tile; ranges are whole tiles
-constexpr int kWideRows = 128;
 constexpr int kNarrowRows = 32;
 // floats per record: HD output values, m, l, padding to 16 bytes
 constexpr int record(int hd) { return hd + 4; }
@@ -87,34 +86,50 @@ __device__ __forceinline__ int limit_of(const PagedAttn& a, const Entry& e, int 
 }
 
 // A workgroup's share: rows row0 .. (stacked as ((entry * max_rows) + row) *
-// group + query head), keys k0 .. k1 - 1 of the table, record index.
+// group + query head) of key head `head`, keys k0 .. k1 - 1 of the table,
+// record index.
 struct Share {
-  int row0, row_end, k0, k1, part;
+  int row0, row_end, head, k0, k1, part;
   const int32_t* table;
 };
 
+// Workgroup x of a part: its item (a key range of one head) and row tile.
+// Workgroups go to the 8 XCDs in turn; the row tiles of an item, which read the
+// same keys, take the same XCD one after the other, so that one L2 fetches them
+// once (16 x 32 rows over 30011 positions, 4 row tiles: a tile's copies came
+// from HBM up to 4 times before).
+struct Item {
+  int item, tile;
+};
+__device__ __forceinline__ Item item_of(int x, int row_tiles) {
+  return Item{x / (8 * row_tiles) * 8 + x % 8, x / 8 % row_tiles};
+}
+int blocks_of(int items, int row_tiles) { return cdiv(items, 8) * 8 * row_tiles; }
+
 // False if the share is empty.
-__device__ __forceinline__ bool share_of(const Job& j, int item, bool in_prefix, int tile_rows, Share& w) {
+__device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, int tile_rows, Share& w) {
   const PagedAttn& a = j.a;
   const int per = a.max_rows * j.group;   // stacked rows of one entry
+  const Part& part = in_prefix ? j.prefix : j.tail;
+  const Item it = item_of(x, part.row_tiles);
+  w.head = it.item % a.p.n_kv_heads;
+  const int t = it.item / a.p.n_kv_heads, r = t % part.ranges, b = t / part.ranges;
+  if (b >= (in_prefix ? 1 : a.n)) return false;   // items are filled up to whole rounds of XCDs
   const int s = shared_of(a);
   if (in_prefix) {
-    const int r = item / j.prefix.row_tiles;
-    w.row0 = item % j.prefix.row_tiles * tile_rows;
+    w.row0 = it.tile * tile_rows;
     w.row_end = a.n * per;
-    w.k0 = r * j.prefix.range;
-    w.k1 = min(w.k0 + j.prefix.range, s);
+    w.k0 = r * part.range;
+    w.k1 = min(w.k0 + part.range, s);
     w.part = r;
     w.table = a.p.table + size_t(a.prefix_seq) * a.p.max_blocks;
     return w.k0 < w.k1;
   }
-  const int b = item / (j.tail.row_tiles * j.tail.ranges), i = item % (j.tail.row_tiles * j.tail.ranges);
-  const int r = i / j.tail.row_tiles;
   const Entry e = entry_of(a, b);
-  w.row0 = b * per + i % j.tail.row_tiles * tile_rows;
+  w.row0 = b * per + it.tile * tile_rows;
   w.row_end = (b + 1) * per;
-  w.k0 = s + r * j.tail.range;
-  w.k1 = r + 1 == j.tail.ranges ? e.held : min(w.k0 + j.tail.range, e.held);
+  w.k0 = s + r * part.range;
+  w.k1 = r + 1 == part.ranges ? e.held : min(w.k0 + part.range, e.held);
   w.part = j.prefix.ranges + r;
   w.table = a.p.table + size_t(max(e.seq, 0)) * a.p.max_blocks;
   // an entry without positions still has its rows set to 0 where nothing is joined
@@ -192,8 +207,9 @@ struct Narrow {
     else return 16 * kb + r;
   }
 
-  __device__ static void run(const Job& j, const Share& w, int kvh, float* smem) {
+  __device__ static void run(const Job& j, const Share& w, float* smem) {
     const PagedAttn& a = j.a;
+    const int kvh = w.head;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int fr = lane & 15, g = lane >> 4;
     const int shift = 31 - __builtin_clz(a.p.page_len), pmask = a.p.page_len - 1;
@@ -407,16 +423,6 @@ struct Narrow {
   }
 };
 
-// grid: prefix items, then tail items; blockIdx.y the key head
-template <typename T, int HD, int NQB>
-__global__ __launch_bounds__(kThreads, 2) void narrow_kernel(Job j, int prefix_items) {
-  __shared__ __attribute__((aligned(16))) float smem[kWaves * Narrow<T, HD, NQB>::STATE * kWave];
-  const bool in_prefix = int(blockIdx.x) < prefix_items;
-  Share w;
-  if (!share_of(j, in_prefix ? int(blockIdx.x) : int(blockIdx.x) - prefix_items, in_prefix, 16 * NQB, w)) return;
-  Narrow<T, HD, NQB>::run(j, w, blockIdx.y, smem);
-}
-
 // ---------------------------------------------------------------- wide
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -444,11 +450,15 @@ struct Wide {
   static constexpr int QS = HD / 16;                // MFMA steps over head_dim
   static constexpr int NDB = HD / 32;
 
-  // chunk slots: rows read together by 8 lanes fall on different banks
-  __device__ __forceinline__ static int kswz(int r) { return (r & 3) | ((r >> 1) & 4); }
+  // chunk c of row r lies in slot c ^ swizzle(r): the 16 rows that 16 lanes
+  // read together fall on different banks (64 of 4 bytes: a 256-byte row, or
+  // two rows of 128)
+  __device__ __forceinline__ static int kswz(int r) { return CK == 16 ? r & 15 : (r >> 1) & 7; }
+  __device__ __forceinline__ static int vswz(int d) { return (d >> 1) & 7; }
 
-  __device__ static void run(const Job& j, const Share& w, int kvh, uint8_t* smem) {
+  __device__ static void run(const Job& j, const Share& w, uint8_t* smem) {
     const PagedAttn& a = j.a;
+    const int kvh = w.head;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int fr = lane & 31, f = lane >> 5;
     const int shift = 31 - __builtin_clz(a.p.page_len), pmask = a.p.page_len - 1;
@@ -477,13 +487,13 @@ struct Wide {
       }
     };
     // this lane's source of each copy: a key row's chunk, a dim row's chunk
-    const int kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vd;
+    const int kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vswz(8 * wave + vd);
     auto issue = [&](int k0, const int (&id)[4], int slot) {
       const uint32_t dst = lds0 + slot * SLOT;
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
-        const int grp = wave * IC + i, r = grp * KROWS + kr;
-        const int sub = grp * KROWS / 16;   // the wave's copies of one i share a 16-key group
+        const int grp = i * kWaves + wave, r = grp * KROWS + kr;
+        const int sub = grp * KROWS / 16;   // a copy's rows share a 16-key group
         const int page = sub == 0 ? id[0] : sub == 1 ? id[1] : sub == 2 ? id[2] : id[3];
         const uint8_t* src = K + page * page_bytes + ((k0 + sub * 16) & pmask) * RB;
         copy16(src + (r & 15) * RB + ((lane % CK) ^ kswz(r)) * 16, dst + grp * 1024);
@@ -492,7 +502,7 @@ struct Wide {
       const uint8_t* src = V + page * page_bytes + size_t(vd) * (a.p.page_len * 2) + ((k0 + 8 * vc) & pmask) * 2;
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
-        const int grp = wave * IC + i;
+        const int grp = i * kWaves + wave;
         copy16(src + size_t(grp) * 8 * (a.p.page_len * 2), dst + KB + grp * 1024);
       }
     };
@@ -518,7 +528,7 @@ struct Wide {
         for (int c = tid; c < HD * 8; c += kThreads) {
           const int d = c >> 3, left = w.k1 - k0 - 8 * (c & 7);
           if (left >= 8) continue;
-          u32x4* p = reinterpret_cast<u32x4*>(sv + d * 128 + (((c & 7) ^ (d & 7)) << 4));
+          u32x4* p = reinterpret_cast<u32x4*>(sv + d * 128 + (((c & 7) ^ vswz(d)) << 4));
           u32x4 x = *p;
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] &= left > 2 * i + 1 ? ~0u : left > 2 * i ? 0xffffu : 0u;
@@ -583,7 +593,7 @@ struct Wide {
 #pragma unroll
         for (int db = 0; db < NDB; ++db) {
           const int d = 32 * db + fr;
-          const u32x4 vf = *reinterpret_cast<const u32x4*>(sv + d * 128 + (((2 * st + f) ^ (d & 7)) << 4));
+          const u32x4 vf = *reinterpret_cast<const u32x4*>(sv + d * 128 + (((2 * st + f) ^ vswz(d)) << 4));
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf), __builtin_bit_cast(half8, pf[st]),
                                                          o[db], 0, 0, 0);
         }
@@ -616,45 +626,99 @@ struct Wide {
   }
 };
 
-template <int HD>
-__global__ __launch_bounds__(kThreads, 2) void wide_kernel(Job j, int prefix_items) {
-  __shared__ __attribute__((aligned(16))) uint8_t smem[Wide<HD>::SMEM];
-  const bool in_prefix = int(blockIdx.x) < prefix_items;
+// ---------------------------------------------------------------- launch
+
+// how a part's rows are taken: 16 or 32 of them narrow, or 128 wide
+enum { ROWS16 = 1, ROWS32 = 2, ROWS128 = 3 };
+constexpr int rows_of(int mode) { return mode == ROWS16 ? 16 : mode == ROWS32 ? 32 : 128; }
+
+template <typename T, int HD, int MODE> struct Taker;
+template <typename T, int HD> struct Taker<T, HD, ROWS16> {
+  static constexpr int SMEM = kWaves * Narrow<T, HD, 1>::STATE * kWave * 4;
+  __device__ static void run(const Job& j, const Share& w, uint8_t* smem) {
+    Narrow<T, HD, 1>::run(j, w, reinterpret_cast<float*>(smem));
+  }
+};
+template <typename T, int HD> struct Taker<T, HD, ROWS32> {
+  static constexpr int SMEM = kWaves * Narrow<T, HD, 2>::STATE * kWave * 4;
+  __device__ static void run(const Job& j, const Share& w, uint8_t* smem) {
+    Narrow<T, HD, 2>::run(j, w, reinterpret_cast<float*>(smem));
+  }
+};
+template <int HD> struct Taker<bf16_t, HD, ROWS128> : Wide<HD> {};
+
+// both parts in one launch: prefix workgroups, then the tails'
+template <typename T, int HD, int PREFIX, int TAIL>
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(Job j, int prefix_blocks) {
+  constexpr int kP = Taker<T, HD, PREFIX>::SMEM, kT = Taker<T, HD, TAIL>::SMEM;
+  __shared__ __attribute__((aligned(16))) uint8_t smem[kP > kT ? kP : kT];
   Share w;
-  if (!share_of(j, in_prefix ? int(blockIdx.x) : int(blockIdx.x) - prefix_items, in_prefix, kWideRows, w)) return;
-  Wide<HD>::run(j, w, blockIdx.y, smem);
+  const int x = blockIdx.x;
+  if (x < prefix_blocks) {
+    if (share_of(j, x, true, rows_of(PREFIX), w)) Taker<T, HD, PREFIX>::run(j, w, smem);
+  } else {
+    if (share_of(j, x - prefix_blocks, false, rows_of(TAIL), w)) Taker<T, HD, TAIL>::run(j, w, smem);
+  }
 }
 
 // ---------------------------------------------------------------- merge
 
 // out[row] = sum_r o_r 2^(m_r - m) / sum_r l_r 2^(m_r - m) over the ranges that
-// hold positions the row sees, in order; HD / 4 lanes a row
+// hold positions the row sees; HD / 4 lanes a row and slice, slice c takes the
+// ranges c, c + slices, .., and the slices are joined in order.
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void join_kernel(Job j) {
+__global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   constexpr int kLanes = HD / 4;
+  __shared__ __attribute__((aligned(16))) float part[kThreads / kLanes][HD + 4];
   const PagedAttn& a = j.a;
-  const int row = blockIdx.x * (kThreads / kLanes) + int(threadIdx.x) / kLanes, c = int(threadIdx.x) % kLanes * 4;
-  if (row >= a.n * a.max_rows * a.heads) return;
-  const int h = row % a.heads, t = row / a.heads, b = t / a.max_rows, i = t % a.max_rows;
+  const int group = int(threadIdx.x) / kLanes, c = int(threadIdx.x) % kLanes * 4, slice = group % slices;
+  const int rows = kThreads / kLanes / slices, row = blockIdx.x * rows + group / slices;
+  const bool in = row < a.n * a.max_rows * a.heads;
+  const int h = row % a.heads, t = row / a.heads, b = in ? t / a.max_rows : 0, i = t % a.max_rows;
   const Entry e = entry_of(a, b);
-  if (i >= e.rows) return;
+  const bool live = in && i < e.rows;
   const int s = shared_of(a), lim = limit_of(a, e, i);
-  const int np = j.prefix.ranges ? (min(lim, s) + j.prefix.range - 1) / j.prefix.range : 0;
-  const int nt = lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
+  const int np = live && j.prefix.ranges ? (min(lim, s) + j.prefix.range - 1) / j.prefix.range : 0;
+  const int nt = live && lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
   const size_t stride = size_t(a.n) * a.max_rows * a.heads * record(HD);
   const float* rec = a.part + size_t(row) * record(HD);
   float m = -INFINITY, l = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int r = 0; r < np + nt; ++r) {
-    const float* x = rec + (r < np ? r : j.prefix.ranges + r - np) * stride;
-    const float mr = x[HD], lr = x[HD + 1];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(x + c);
+  auto add = [&](float mr, float lr, f32x4 v) {
     const float mn = fmaxf(m, mr), ref = mn == -INFINITY ? 0.f : mn;
     const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(mr - ref);
     l = l * w0 + lr * w1;
     o = o * w0 + v * w1;
     m = mn;
+  };
+  // four records in flight
+  for (int r0 = slice; r0 < np + nt; r0 += 4 * slices) {
+    float mr[4], lr[4];
+    f32x4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = min(r0 + u * slices, np + nt - 1);
+      const float* x = rec + (r < np ? r : j.prefix.ranges + r - np) * stride;
+      mr[u] = x[HD];
+      lr[u] = x[HD + 1];
+      v[u] = *reinterpret_cast<const f32x4*>(x + c);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (r0 + u * slices < np + nt) add(mr[u], lr[u], v[u]);
   }
+  if (slices > 1) {
+    *reinterpret_cast<f32x4*>(&part[group][c]) = o;
+    if (c == 0) {
+      part[group][HD] = m;
+      part[group][HD + 1] = l;
+    }
+    __syncthreads();
+    if (slice) return;
+    for (int u = 1; u < slices; ++u)
+      add(part[group + u][HD], part[group + u][HD + 1], *reinterpret_cast<const f32x4*>(&part[group + u][c]));
+  }
+  if (!live) return;
   T* out = static_cast<T*>(a.out.p) + b * a.out.seq + i * a.out.row + h * a.out.head + c;
 #pragma unroll
   for (int x = 0; x < 4; ++x) store_f(out + x, lim > 0 ? o[x] / l : 0.f);
@@ -665,32 +729,66 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j) {
 constexpr int kSlots = 512;      // workgroups at a time: two on each of 256 CUs
 constexpr int kMaxRanges = 64;
 
-bool is_wide(int dtype, int rows) { return dtype == DLLM_BF16 && rows > kNarrowRows; }
+int mode_of(int dtype, int rows) {
+  return dtype == DLLM_BF16 && rows > kNarrowRows ? ROWS128 : rows > 16 ? ROWS32 : ROWS16;
+}
 
 // most key ranges that a part of `wgs` workgroups a range is ever given
-int most_ranges(int64_t wgs) { return int(std::min<int64_t>(kMaxRanges, std::max<int64_t>(1, 2 * kSlots / std::max<int64_t>(wgs, 1)))); }
+int most_ranges(int64_t wgs) {
+  return int(std::min<int64_t>(kMaxRanges, std::max<int64_t>(1, 2 * kSlots / std::max<int64_t>(wgs, 1))));
+}
 
-// rows stacked per key head, in `blocks` separate groups (entries of a tail)
-Part plan_part(int dtype, int rows, int64_t blocks, int kv_heads, int64_t keys, bool wide) {
+// rows stacked per key head, in `groups` separate sets (entries of a tail)
+Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys) {
   Part p;
-  p.row_tiles = cdiv(rows, wide ? kWideRows : rows > 16 ? kNarrowRows : 16);
-  const int step = wide ? 4 * kTile : 4 * kTile;   // keys of the shortest range
+  p.row_tiles = cdiv(rows, rows_of(mode));
   const int64_t tiles = (keys + kTile - 1) / kTile;
-  const int most = most_ranges(p.row_tiles * blocks * kv_heads);
-  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>(most, keys / step));
-  p.range = int((tiles + ranges - 1) / ranges * kTile);
-  p.range = std::max(p.range, kTile);
+  const int most = most_ranges(p.row_tiles * groups * kv_heads);
+  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>(most, tiles / 4));
+  p.range = int(std::max<int64_t>(1, (tiles + ranges - 1) / ranges)) * kTile;
   p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
   return p;
+}
+
+template <typename T, int HD, int PREFIX, int TAIL>
+void launch_parts(const Job& j, hipStream_t s) {
+  const int kvh = j.a.p.n_kv_heads;
+  const int prefix = j.prefix.ranges ? blocks_of(j.prefix.ranges * kvh, j.prefix.row_tiles) : 0;
+  const int tail = blocks_of(j.a.n * j.tail.ranges * kvh, j.tail.row_tiles);
+  hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL>), dim3(prefix + tail), dim3(kThreads), 0, s, j, prefix);
+}
+
+// the batch's rows are at least an entry's: the prefix mode is never the lower one
+template <typename T, int HD>
+void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (tail == ROWS128) return launch_parts<T, HD, ROWS128, ROWS128>(j, s);
+    if (prefix == ROWS128)
+      return tail == ROWS32 ? launch_parts<T, HD, ROWS128, ROWS32>(j, s) : launch_parts<T, HD, ROWS128, ROWS16>(j, s);
+  }
+  if (tail == ROWS32) return launch_parts<T, HD, ROWS32, ROWS32>(j, s);
+  return prefix == ROWS32 ? launch_parts<T, HD, ROWS32, ROWS16>(j, s) : launch_parts<T, HD, ROWS16, ROWS16>(j, s);
+}
+
+template <typename T, int HD>
+void launch(const Job& j, int prefix, int tail, hipStream_t s) {
+  launch_modes<T, HD>(j, prefix, tail, s);
+  if (j.direct) return;
+  // rows of many ranges take several groups of lanes each: the records of a
+  // row come in turn, four at a time
+  constexpr int kGroups = kThreads / (HD / 4);
+  const int ranges = j.prefix.ranges + j.tail.ranges;
+  const int slices = ranges <= 4 ? 1 : ranges <= 8 ? 2 : ranges <= 16 ? 4 : 8;
+  hipLaunchKernelGGL((join_kernel<T, HD>), dim3(cdiv(j.a.n * j.a.max_rows * j.a.heads, kGroups / slices)),
+                     dim3(kThreads), 0, s, j, slices);
 }
 
 }  // namespace
 
 size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads) {
   const int group = heads / p.n_kv_heads;
-  auto ranges = [&](int rows, int blocks) {
-    const int tile = is_wide(p.dtype, rows) ? kWideRows : rows > 16 ? kNarrowRows : 16;
-    return most_ranges(int64_t(cdiv(rows, tile)) * blocks * p.n_kv_heads);
+  auto ranges = [&](int rows, int groups) {
+    return most_ranges(int64_t(cdiv(rows, rows_of(mode_of(p.dtype, rows)))) * groups * p.n_kv_heads);
   };
   const size_t parts = ranges(n * max_rows * group, 1) + ranges(max_rows * group, n);
   return parts * n * max_rows * heads * record(p.head_dim) * sizeof(float);
@@ -701,47 +799,19 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   j.a = a;
   j.scale_log2 = a.scale * 1.4426950408889634f;
   j.group = a.heads / a.p.n_kv_heads;
-  const int dt = a.p.dtype, hd = a.p.head_dim, kvh = a.p.n_kv_heads;
+  const int dt = a.p.dtype, kvh = a.p.n_kv_heads;
   const int64_t most = int64_t(a.p.max_blocks) * a.p.page_len;
   const int64_t shared = std::min<int64_t>(a.shared_len, most) / a.p.page_len * a.p.page_len;
   const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
-  const bool wide_p = is_wide(dt, rows_p), wide_t = is_wide(dt, rows_t);
-  int prefix_items = 0;
-  if (shared > 0) {
-    j.prefix = plan_part(dt, rows_p, 1, kvh, shared, wide_p);
-    prefix_items = j.prefix.row_tiles * j.prefix.ranges;
-  } else {
-    j.prefix = Part{0, 0, kTile};
-    j.a.shared_len = 0;
-  }
-  j.tail = plan_part(dt, rows_t, a.n, kvh, std::max<int64_t>(1, std::min<int64_t>(a.max_len, most) - shared), wide_t);
-  const int tail_items = a.n * j.tail.row_tiles * j.tail.ranges;
-  j.direct = prefix_items == 0 && j.tail.ranges == 1;
-
-  auto run = [&](auto kernel, int prefix, int tail) {
-    hipLaunchKernelGGL(kernel, dim3(prefix + tail, kvh), dim3(kThreads), 0, s, j, prefix);
-  };
-  auto narrow = [&](int rows, int prefix, int tail) {
-    if (dt == DLLM_BF16) {
-      if (hd == 128) rows > 16 ? run(narrow_kernel<bf16_t, 128, 2>, prefix, tail) : run(narrow_kernel<bf16_t, 128, 1>, prefix, tail);
-      else rows > 16 ? run(narrow_kernel<bf16_t, 64, 2>, prefix, tail) : run(narrow_kernel<bf16_t, 64, 1>, prefix, tail);
-    } else {
-      if (hd == 128) rows > 16 ? run(narrow_kernel<float, 128, 2>, prefix, tail) : run(narrow_kernel<float, 128, 1>, prefix, tail);
-      else rows > 16 ? run(narrow_kernel<float, 64, 2>, prefix, tail) : run(narrow_kernel<float, 64, 1>, prefix, tail);
-    }
-  };
-  auto wide = [&](int prefix, int tail) {
-    hd == 128 ? run(wide_kernel<128>, prefix, tail) : run(wide_kernel<64>, prefix, tail);
-  };
-  if (prefix_items) wide_p ? wide(prefix_items, 0) : narrow(rows_p, prefix_items, 0);
-  wide_t ? wide(0, tail_items) : narrow(rows_t, 0, tail_items);
-  if (!j.direct) {
-    auto join = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3(cdiv(a.n * a.max_rows * a.heads, kThreads / (hd / 4))), dim3(kThreads), 0, s, j);
-    };
-    if (dt == DLLM_BF16) hd == 128 ? join(join_kernel<bf16_t, 128>) : join(join_kernel<bf16_t, 64>);
-    else hd == 128 ? join(join_kernel<float, 128>) : join(join_kernel<float, 64>);
-  }
+  const int mode_t = mode_of(dt, rows_t), mode_p = shared > 0 ? mode_of(dt, rows_p) : mode_t;
+  j.prefix = shared > 0 ? plan_part(mode_p, rows_p, 1, kvh, shared) : Part{1, 0, kTile};
+  if (shared == 0) j.a.shared_len = 0;
+  j.tail = plan_part(mode_t, rows_t, a.n, kvh, std::max<int64_t>(1, std::min<int64_t>(a.max_len, most) - shared));
+  j.direct = j.prefix.ranges + j.tail.ranges == 1;
+  if (dt == DLLM_BF16)
+    a.p.head_dim == 128 ? launch<bf16_t, 128>(j, mode_p, mode_t, s) : launch<bf16_t, 64>(j, mode_p, mode_t, s);
+  else
+    a.p.head_dim == 128 ? launch<float, 128>(j, mode_p, mode_t, s) : launch<float, 64>(j, mode_p, mode_t, s);
   return hipGetLastError();
 }
 
