@@ -90,8 +90,11 @@ __device__ __forceinline__ int limit_of(const PagedAttn& a, const Entry& e, int 
 // record index.
 struct Share {
   int row0, row_end, head, k0, k1, part;
-  const int32_t* table;
+  const __attribute__((address_space(4))) int32_t* table;   // read on the scalar unit: uniform, not written here
 };
+__device__ __forceinline__ const __attribute__((address_space(4))) int32_t* table_row(const PagedAttn& a, int seq) {
+  return (const __attribute__((address_space(4))) int32_t*)(a.p.table + size_t(seq) * a.p.max_blocks);
+}
 
 // Workgroup x of a part: its item (a key range of one head) and row tile.
 // Workgroups go to the 8 XCDs in turn; the row tiles of an item, which read the
@@ -122,7 +125,7 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
     w.k0 = r * part.range;
     w.k1 = min(w.k0 + part.range, s);
     w.part = r;
-    w.table = a.p.table + size_t(a.prefix_seq) * a.p.max_blocks;
+    w.table = table_row(a, a.prefix_seq);
     return w.k0 < w.k1;
   }
   const Entry e = entry_of(a, b);
@@ -131,7 +134,7 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
   w.k0 = s + r * part.range;
   w.k1 = r + 1 == part.ranges ? e.held : min(w.k0 + part.range, e.held);
   w.part = j.prefix.ranges + r;
-  w.table = a.p.table + size_t(max(e.seq, 0)) * a.p.max_blocks;
+  w.table = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
   // an entry without positions still has its rows set to 0 where nothing is joined
   return w.row0 < b * per + e.rows * j.group && (w.k0 < w.k1 || j.direct);
 }
@@ -235,20 +238,19 @@ struct Narrow {
     }
     lim_min = wave_min_int(lim_min);
 
-    // page ids of a step's 16-key groups (past the last key: its page again)
+    // table entries of a step's 16-key groups (past the last key: its page
+    // again), brought into the pool where they are used: loads do not wait here
     auto pages_at = [&](int k0, int (&id)[NB]) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int p = w.table[min((k0 + 16 * i) >> shift, last_block)];
-        id[i] = min(max(p, 0), a.p.n_pages - 1);
-      }
+      for (int i = 0; i < NB; ++i) id[i] = w.table[min((k0 + 16 * i) >> shift, last_block)];
     };
+    auto in_pool = [&](int p) { return min(max(p, 0), a.p.n_pages - 1); };
     u32x4 kf[NB][QS], vf[NDB][NV];
     auto load_k = [&](int k0, const int (&id)[NB]) {
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb) {
         const int key = key_of(kb, fr);
-        const int page = kHalf ? (fr < 8 ? id[kb & ~1] : id[kb | 1]) : id[kb];
+        const int page = in_pool(kHalf ? (fr < 8 ? id[kb & ~1] : id[kb | 1]) : id[kb]);
         const T* row = K + page * page_stride + ((k0 + key) & pmask) * HD;
 #pragma unroll
         for (int st = 0; st < QS; ++st) kf[kb][st] = *reinterpret_cast<const u32x4*>(row + (4 * st + g) * E);
@@ -258,7 +260,7 @@ struct Narrow {
 #pragma unroll
       for (int c = 0; c < NV; ++c) {
         const int key = (4 * c + g) * E;   // first of this lane's chunk
-        const int page = kHalf ? (g < 2 ? id[2 * c] : id[2 * c + 1]) : id[c];
+        const int page = in_pool(kHalf ? (g < 2 ? id[2 * c] : id[2 * c + 1]) : id[c]);
         const T* row = V + page * page_stride + size_t(fr) * a.p.page_len + ((k0 + key) & pmask);
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
@@ -481,11 +483,9 @@ struct Wide {
 
     auto pages_at = [&](int k0, int (&id)[4]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p = w.table[min((k0 + 16 * i) >> shift, last_block)];
-        id[i] = min(max(p, 0), a.p.n_pages - 1);
-      }
+      for (int i = 0; i < 4; ++i) id[i] = w.table[min((k0 + 16 * i) >> shift, last_block)];
     };
+    auto in_pool = [&](int p) { return min(max(p, 0), a.p.n_pages - 1); };
     // this lane's source of each copy: a key row's chunk, a dim row's chunk
     const int kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vswz(8 * wave + vd);
     auto issue = [&](int k0, const int (&id)[4], int slot) {
@@ -493,12 +493,14 @@ struct Wide {
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
         const int grp = i * kWaves + wave, r = grp * KROWS + kr;
-        const int sub = grp * KROWS / 16;   // a copy's rows share a 16-key group
-        const int page = sub == 0 ? id[0] : sub == 1 ? id[1] : sub == 2 ? id[2] : id[3];
+        // a copy's rows share a 16-key group
+        const int sub = KROWS == 4 ? i : 2 * i + (wave >> 1);
+        const int even = id[KROWS == 4 ? i : 2 * i], odd = id[KROWS == 4 ? i : 2 * i + 1];
+        const int page = in_pool(wave & 2 ? odd : even);
         const uint8_t* src = K + page * page_bytes + ((k0 + sub * 16) & pmask) * RB;
         copy16(src + (r & 15) * RB + ((lane % CK) ^ kswz(r)) * 16, dst + grp * 1024);
       }
-      const int page = vc < 4 ? (vc < 2 ? id[0] : id[1]) : (vc < 6 ? id[2] : id[3]);
+      const int page = in_pool(vc < 4 ? (vc < 2 ? id[0] : id[1]) : (vc < 6 ? id[2] : id[3]));
       const uint8_t* src = V + page * page_bytes + size_t(vd) * (a.p.page_len * 2) + ((k0 + 8 * vc) & pmask) * 2;
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
@@ -544,15 +546,32 @@ struct Wide {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[h][i] = 0.f;
+      // every K fragment is on its way before the first product waits for one
+      u32x4 kf[2][QS], vf[2][NDB];
 #pragma unroll
       for (int st = 0; st < QS; ++st)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int r = 32 * h + ((fr & 0x13) | ((fr & 4) << 1) | ((fr & 8) >> 1));
-          const u32x4 kf = *reinterpret_cast<const u32x4*>(sk + r * RB + (((2 * st + f) ^ kswz(r)) << 4));
-          sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
-                                                          __builtin_bit_cast(bf16x8, qf[st]), sc[h], 0, 0, 0);
+          kf[h][st] = *reinterpret_cast<const u32x4*>(sk + r * RB + (((2 * st + f) ^ kswz(r)) << 4));
         }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int st = 0; st < QS; ++st)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[h][st]),
+                                                          __builtin_bit_cast(bf16x8, qf[st]), sc[h], 0, 0, 0);
+      auto read_v = [&](int st) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          const int d = 32 * db + fr;
+          vf[st & 1][db] = *reinterpret_cast<const u32x4*>(sv + d * 128 + (((2 * st + f) ^ vswz(d)) << 4));
+        }
+      };
+      read_v(0);
+      read_v(1);
+      __builtin_amdgcn_sched_barrier(0);
       // element i of half h: key 32 h + 16 (i / 8) + 8 f + i % 8
       if (k0 + kTile > lim_min) {
 #pragma unroll
@@ -589,14 +608,13 @@ struct Wide {
         }
       l += sum;
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
+      for (int st = 0; st < 4; ++st) {
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-          const int d = 32 * db + fr;
-          const u32x4 vf = *reinterpret_cast<const u32x4*>(sv + d * 128 + (((2 * st + f) ^ vswz(d)) << 4));
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf), __builtin_bit_cast(half8, pf[st]),
-                                                         o[db], 0, 0, 0);
-        }
+        for (int db = 0; db < NDB; ++db)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf[st & 1][db]),
+                                                         __builtin_bit_cast(half8, pf[st]), o[db], 0, 0, 0);
+        if (st < 2) read_v(st + 2);
+      }
     }
     l = pair_sum(l);
     if (w.row0 + 32 * wave + fr >= w.row_end || at.i >= entry.rows) return;
