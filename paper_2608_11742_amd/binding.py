@@ -243,7 +243,7 @@ class KvPages:
             raise ValueError("the arrays must be contiguous tensors of one device")
         self.k, self.vt, self.refs, self.table, self.len = k, vt, refs, table, len
         self.page_len, self.head_dim, self.n_kv_heads, self.dtype = page_len, hd, heads, k.dtype
-        self._index = k.get_device()
+        self._index, self._scale = k.get_device(), hd ** -0.5
         self._c = _abi.KvPagesC(k.data_ptr(), vt.data_ptr(), refs.data_ptr(), table.data_ptr(), len.data_ptr(), L,
                                 n_pages, heads, hd, page_len, table.shape[0], table.shape[1],
                                 DLLM_BF16 if k.dtype == torch.bfloat16 else DLLM_F32)
@@ -340,8 +340,8 @@ def kv_pages_compact(pages: KvPages, n_used, ws, stream=None):
 def kv_pages_write(pages: KvPages, layer: int, seqs, k, v, n_rows=None, stream=None):
     """k, v [entries, rows, kv heads, head_dim]: the last n_rows[b] (or all rows) positions of sequence seqs[b]."""
     n, rows, heads, _ = k.shape
-    if seqs.numel() != n or v.shape != k.shape or heads != pages.n_kv_heads:
-        raise ValueError("k and v need one batch entry per sequence, the pages' heads and the same shape")
+    if v.shape != k.shape or heads != pages.n_kv_heads:
+        raise ValueError("k and v need the pages' heads and the same shape")
     _check(lib().kv_pages_write(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n),
                                 _rows(pages, k, "k"), _rows(pages, v, "v"), _page_stream(pages, stream)))
 
@@ -356,14 +356,14 @@ def kv_pages_attention(pages: KvPages, layer: int, seqs, q, out, ws, n_rows=None
     """q, out [entries, rows, heads, head_dim]; see kv_pages_attention in dllm_rps.h.
 
     max_len defaults to the tables' length, scale to 1 / sqrt(head_dim)."""
-    n, rows, heads, hd = q.shape
-    if seqs.numel() != n or out.shape != q.shape:
-        raise ValueError("q and out need one batch entry per sequence and the same shape")
+    n, rows, heads, _ = shape = q.shape
+    if out.shape != shape:
+        raise ValueError("q and out need the same shape")
     if max_len is None:
         max_len = pages.table.shape[1] * pages.page_len
     _check(lib().kv_pages_attention(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n), heads,
                                     _rows(pages, q, "q"), _rows(pages, out, "out"), prefix_seq,
-                                    shared_len, max_len, int(causal), hd ** -0.5 if scale is None else scale,
+                                    shared_len, max_len, int(causal), pages._scale if scale is None else scale,
                                     *_scratch(pages, ws), _page_stream(pages, stream)))
 
 

@@ -178,13 +178,6 @@ __device__ __forceinline__ float quad_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// smallest / largest of a value over the wave, as a scalar
-__device__ __forceinline__ int wave_min_int(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o, kWave));
-  return __builtin_amdgcn_readfirstlane(x);
-}
-
 // ---------------------------------------------------------------- narrow
 
 // NQB blocks of 16 rows.  A key step is KS keys in blocks of 16; bf16 keys of
@@ -225,18 +218,14 @@ struct Narrow {
 
     RowAt at[NQB];
     u32x4 qf[NQB][QS];
-    int lim[NQB], lim_min = 1 << 30;
+    int lim[NQB], rows[NQB];
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
       at[qb] = row_at(j, min(w.row0 + 16 * qb + fr, w.row_end - 1));
-      const T* q = static_cast<const T*>(a.q.p) + at[qb].b * a.q.seq + at[qb].i * a.q.row +
-                   (kvh * j.group + at[qb].g) * a.q.head;
-#pragma unroll
-      for (int st = 0; st < QS; ++st) qf[qb][st] = *reinterpret_cast<const u32x4*>(q + (4 * st + g) * E);
-      lim[qb] = min(limit_of(a, entry_of(a, at[qb].b), at[qb].i), w.k1);
-      lim_min = min(lim_min, lim[qb]);
+      const Entry e = entry_of(a, at[qb].b);
+      lim[qb] = min(limit_of(a, e, at[qb].i), w.k1);
+      rows[qb] = e.rows;
     }
-    lim_min = wave_min_int(lim_min);
 
     // table entries of a step's 16-key groups (past the last key: its page
     // again), brought into the pool where they are used: loads do not wait here
@@ -283,8 +272,15 @@ struct Narrow {
     if (k0 < w.k1) {
       pages_at(k0, id);
       load_k(k0, id);
-      load_v(k0, id);
     }
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      const T* q = static_cast<const T*>(a.q.p) + at[qb].b * a.q.seq + at[qb].i * a.q.row +
+                   (kvh * j.group + at[qb].g) * a.q.head;
+#pragma unroll
+      for (int st = 0; st < QS; ++st) qf[qb][st] = *reinterpret_cast<const u32x4*>(q + (4 * st + g) * E);
+    }
+    if (k0 < w.k1) load_v(k0, id);
     for (; k0 < w.k1; k0 += kWaves * KS) {
       const int next = k0 + kWaves * KS;
       const bool more = next < w.k1;
@@ -299,7 +295,10 @@ struct Narrow {
           for (int st = 0; st < QS; ++st) Mfma<T>::run(sc[kb][qb], kf[kb][st], qf[qb][st]);
         }
       if (more) load_k(next, id);
-      if (k0 + KS > lim_min) {
+      bool all = true;
+#pragma unroll
+      for (int qb = 0; qb < NQB; ++qb) all = all && k0 + KS <= lim[qb];
+      if (!__all(all)) {
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
@@ -397,7 +396,7 @@ struct Narrow {
         sum += smem[(v * STATE + STATE - 1) * kWave + lane] * mw[v];
       }
       const int row = w.row0 + 16 * qb + fr;
-      const bool live = row < w.row_end && at[qb].i < entry_of(a, at[qb].b).rows;
+      const bool live = row < w.row_end && at[qb].i < rows[qb];
       const float inv = lim[qb] > 0 ? 1.f / sum : 0.f;
       T* out = static_cast<T*>(a.out.p) + at[qb].b * a.out.seq + at[qb].i * a.out.row +
                (kvh * j.group + at[qb].g) * a.out.head;
@@ -479,7 +478,6 @@ struct Wide {
     for (int st = 0; st < QS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(q + (2 * st + f) * 8);
     const Entry entry = entry_of(a, at.b);
     const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
-    const int lim_min = wave_min_int(lim);
 
     auto pages_at = [&](int k0, int (&id)[4]) {
 #pragma unroll
@@ -573,7 +571,7 @@ struct Wide {
       read_v(1);
       __builtin_amdgcn_sched_barrier(0);
       // element i of half h: key 32 h + 16 (i / 8) + 8 f + i % 8
-      if (k0 + kTile > lim_min) {
+      if (!__all(k0 + kTile <= lim)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -744,25 +742,38 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
 
 // ---------------------------------------------------------------- host
 
-constexpr int kSlots = 512;      // workgroups at a time: two on each of 256 CUs
+constexpr int kCus = 256;
 constexpr int kMaxRanges = 64;
 
-int mode_of(int dtype, int rows) {
-  return dtype == DLLM_BF16 && rows > kNarrowRows ? ROWS128 : rows > 16 ? ROWS32 : ROWS16;
+// How `groups` sets of stacked rows per key head are taken.  fp32 products
+// cost an eighth of the bf16 rate, so there 32 rows, which halve what is
+// read, are only worth it where 16 fill the chip twice.
+int mode_of(int dtype, int rows, int64_t groups, int kv_heads) {
+  if (dtype == DLLM_BF16) return rows > kNarrowRows ? ROWS128 : rows > 16 ? ROWS32 : ROWS16;
+  return rows > 16 && cdiv(rows, 16) * groups * kv_heads > 4 * kCus ? ROWS32 : ROWS16;
 }
 
-// most key ranges that a part of `wgs` workgroups a range is ever given
-int most_ranges(int64_t wgs) {
-  return int(std::min<int64_t>(kMaxRanges, std::max<int64_t>(1, 2 * kSlots / std::max<int64_t>(wgs, 1))));
+// most key ranges that a part of `items` workgroups a range is ever given
+int most_ranges(int64_t items) {
+  return int(std::min<int64_t>(kMaxRanges, std::max<int64_t>(1, 8 * kCus / std::max<int64_t>(items, 1))));
 }
 
-// rows stacked per key head, in `groups` separate sets (entries of a tail)
+// Rows stacked per key head, in `groups` separate sets (entries of a tail).
+// Two workgroups fit a CU.  Narrow parts are bound by memory: as many ranges
+// as fill the chip, and where they are long ones of 24 tiles, so that batches
+// of unlike lengths come out even.  Wide ones take one
+// workgroup a CU, which leaves the other slot to the tails, and two where
+// ranges stay long enough for the second to gain more than its records cost to
+// join.
 Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys) {
   Part p;
   p.row_tiles = cdiv(rows, rows_of(mode));
-  const int64_t tiles = (keys + kTile - 1) / kTile;
-  const int most = most_ranges(p.row_tiles * groups * kv_heads);
-  const int64_t ranges = std::max<int64_t>(1, std::min<int64_t>(most, tiles / 4));
+  const int64_t tiles = (keys + kTile - 1) / kTile, items = p.row_tiles * groups * kv_heads;
+  auto fill = [&](int64_t wgs) { return (wgs + items - 1) / items; };
+  int64_t ranges;
+  if (mode == ROWS128) ranges = tiles >= 24 * fill(kCus) ? fill(2 * kCus) : fill(kCus);
+  else ranges = std::max(fill(2 * kCus), tiles / 24);
+  ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most_ranges(items), tiles / 4}));
   p.range = int(std::max<int64_t>(1, (tiles + ranges - 1) / ranges)) * kTile;
   p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
   return p;
@@ -776,7 +787,7 @@ void launch_parts(const Job& j, hipStream_t s) {
   hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL>), dim3(prefix + tail), dim3(kThreads), 0, s, j, prefix);
 }
 
-// the batch's rows are at least an entry's: the prefix mode is never the lower one
+// of bf16 models the prefix, whose rows are at least an entry's, never takes the lower mode
 template <typename T, int HD>
 void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
@@ -784,6 +795,8 @@ void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
     if (prefix == ROWS128)
       return tail == ROWS32 ? launch_parts<T, HD, ROWS128, ROWS32>(j, s) : launch_parts<T, HD, ROWS128, ROWS16>(j, s);
   }
+  if constexpr (sizeof(T) == 4)
+    if (tail == ROWS32 && prefix == ROWS16) return launch_parts<T, HD, ROWS16, ROWS32>(j, s);
   if (tail == ROWS32) return launch_parts<T, HD, ROWS32, ROWS32>(j, s);
   return prefix == ROWS32 ? launch_parts<T, HD, ROWS32, ROWS16>(j, s) : launch_parts<T, HD, ROWS16, ROWS16>(j, s);
 }
@@ -806,7 +819,7 @@ void launch(const Job& j, int prefix, int tail, hipStream_t s) {
 size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads) {
   const int group = heads / p.n_kv_heads;
   auto ranges = [&](int rows, int groups) {
-    return most_ranges(int64_t(cdiv(rows, rows_of(mode_of(p.dtype, rows)))) * groups * p.n_kv_heads);
+    return most_ranges(int64_t(cdiv(rows, rows_of(mode_of(p.dtype, rows, groups, p.n_kv_heads)))) * groups * p.n_kv_heads);
   };
   const size_t parts = ranges(n * max_rows * group, 1) + ranges(max_rows * group, n);
   return parts * n * max_rows * heads * record(p.head_dim) * sizeof(float);
@@ -821,7 +834,7 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   const int64_t most = int64_t(a.p.max_blocks) * a.p.page_len;
   const int64_t shared = std::min<int64_t>(a.shared_len, most) / a.p.page_len * a.p.page_len;
   const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
-  const int mode_t = mode_of(dt, rows_t), mode_p = shared > 0 ? mode_of(dt, rows_p) : mode_t;
+  const int mode_t = mode_of(dt, rows_t, a.n, kvh), mode_p = shared > 0 ? mode_of(dt, rows_p, 1, kvh) : mode_t;
   j.prefix = shared > 0 ? plan_part(mode_p, rows_p, 1, kvh, shared) : Part{1, 0, kTile};
   if (shared == 0) j.a.shared_len = 0;
   j.tail = plan_part(mode_t, rows_t, a.n, kvh, std::max<int64_t>(1, std::min<int64_t>(a.max_len, most) - shared));

@@ -81,24 +81,35 @@ __device__ __forceinline__ int plan_error(int err, PlanShared& sh) {
 
 __device__ __forceinline__ int blocks_of(int positions, int page_len) { return (positions + page_len - 1) / page_len; }
 
+// this thread's run of page ids, and the free ones among them
+struct Run {
+  int lo, hi, n_free;
+};
+__device__ __forceinline__ Run count_free(const dllm_kv_pages& p) {
+  const int run = (p.n_pages + kPlanThreads - 1) / kPlanThreads;
+  Run r;
+  r.lo = min(int(threadIdx.x) * run, p.n_pages);
+  r.hi = min(r.lo + run, p.n_pages);
+  r.n_free = 0;
+  for (int i = r.lo; i < r.hi; ++i) r.n_free += p.refs[i] <= 0;
+  return r;
+}
+
 // Pages for the plan's entries: entry i (this thread's) needs `need` pages as
 // blocks first .. of sequence seq.  False (and nothing stored) if the pool has
 // fewer free ones.
-__device__ __forceinline__ bool take_pages(const dllm_kv_pages& p, PlanShared& sh, int seq, int first, int need) {
+__device__ __forceinline__ bool take_pages(const dllm_kv_pages& p, PlanShared& sh, const Run& run, int seq, int first,
+                                           int need) {
   const int tid = threadIdx.x;
   int total, have;
   const int off = block_scan(need, sh, total);
   sh.off[tid] = off;
   sh.first[tid] = first;
   sh.seq[tid] = seq;
-  const int run = (p.n_pages + kPlanThreads - 1) / kPlanThreads;
-  const int lo = min(tid * run, p.n_pages), hi = min(lo + run, p.n_pages);
-  int n_free = 0;
-  for (int i = lo; i < hi; ++i) n_free += p.refs[i] <= 0;
-  int rank = block_scan(n_free, sh, have);   // its barriers publish off, first and seq too
+  int rank = block_scan(run.n_free, sh, have);   // its barriers publish off, first and seq too
   if (total > have) return false;
-  if (n_free == 0 || rank >= total) return true;
-  for (int i = lo; i < hi && rank < total; ++i) {
+  if (run.n_free == 0 || rank >= total) return true;
+  for (int i = run.lo; i < run.hi && rank < total; ++i) {
     if (p.refs[i] > 0) continue;
     // the last entry whose needs start at or before this rank (entries that need nothing share their start with the next)
     int a = 0, b = kPlanThreads;
@@ -129,6 +140,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(dllm_kv_pages 
   const int tid = threadIdx.x;
   int err = kNoError, s = -1, held = 0, more = 0;
   const int want_s = tid < n ? seqs[tid] : 0, want_a = tid < n ? add[tid] : 0;
+  const Run run = count_free(p);   // with the lists on their way
   plan_begin(sh);
   if (tid < n) {
     s = check_seq(p, want_s, sh, err);
@@ -140,7 +152,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(dllm_kv_pages 
   if (err == kNoError) {
     const int first = blocks_of(held, p.page_len);
     const int need = tid < n ? blocks_of(held + more, p.page_len) - first : 0;
-    if (!take_pages(p, sh, s, first, need)) err = KV_PAGES_EFULL;
+    if (!take_pages(p, sh, run, s, first, need)) err = KV_PAGES_EFULL;
     else if (tid < n) p.len[s] = held + more;
   }
   if (tid == 0) *status = err == kNoError ? KV_PAGES_OK : err;
@@ -156,6 +168,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(dllm_kv_pages 
   const int tid = threadIdx.x;
   int err = kNoError, d = -1, m = 0;
   const int from = tid < n ? src[tid] : 0, to = tid < n ? dst[tid] : 0, cut = keep && tid < n ? keep[tid] : 0;
+  const Run run = count_free(p);
   plan_begin(sh);
   if (tid < n) {
     d = check_seq(p, to, sh, err);
@@ -169,7 +182,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(dllm_kv_pages 
   err = plan_error(err, sh);   // every length has been read before one is stored
   if (err == kNoError) {
     const int need = tid < n && m % p.page_len ? 1 : 0;
-    if (!take_pages(p, sh, d, m / p.page_len, need)) err = KV_PAGES_EFULL;
+    if (!take_pages(p, sh, run, d, m / p.page_len, need)) err = KV_PAGES_EFULL;
     else if (tid < n) p.len[d] = m;
   }
   if (tid == 0) *status = err == kNoError ? KV_PAGES_OK : err;
