@@ -365,6 +365,25 @@ dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const 
                                const dllm_rows* out, int32_t prefix_seq, int32_t shared_len, int32_t max_len,
                                int32_t causal, float scale, void* ws, size_t ws_bytes, dllm_stream stream);
 
+/* One denoising forward of a batch whose sequences live in pages: requests of
+ * different lengths, or lookahead branches forked off one another.  Row i of
+ * entry b is position len - seq + i of sequence seqs[b] (the last seq
+ * positions it holds, so it is grown by seq first; position ids are clamped to
+ * 0 .. max_pos-1).  In every layer the rows' keys and values are written as by
+ * kv_pages_write and the rows attend, not causally, to all positions of their
+ * sequence as by kv_pages_attention (prefix_seq, shared_len and max_len as
+ * there).  kv_pages_free with keep takes the positions back.
+ *   pages    of the model's type, layers, heads and head_dim.
+ *   seqs     [batch] int32, batch <= KV_MAX_SEQS.
+ *   lm_pos   [n_lm_pos] rows of an entry (0 .. seq-1); row_scale [seq] too.
+ *   Other arguments and the output as dllm_forward. */
+size_t dllm_workspace_bytes_pages(const dllm_model* m, int32_t batch, int32_t seq, int32_t n_lm_pos);
+dllm_status dllm_forward_pages(dllm_model* m, const int32_t* tokens, int32_t batch, int32_t seq,
+                               const dllm_kv_pages* pages, const int32_t* seqs, int32_t prefix_seq,
+                               int32_t shared_len, int32_t max_len, const int32_t* lm_pos, int32_t n_lm_pos,
+                               const float* row_scale, float scale, const dllm_probe* probe, const dllm_stats* out,
+                               void* ws, size_t ws_bytes, dllm_stream stream);
+
 /* Kernel timing for benchmarks.  Between dllm_profile_begin and
  * dllm_profile_end every kernel that dllm_forward launches is bracketed by
  * HIP events on the launch stream (for at most max_launches launches).

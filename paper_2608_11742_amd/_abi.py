@@ -96,6 +96,9 @@ SIGNATURES = {
     "vocab_entropy_topk_workspace_bytes": (sz, [i32, i32]),
     "vocab_entropy_topk": (i32, [vp, vp, i32, i32, i32, i32, vp, f32, i32, C.POINTER(StatsC), vp, sz, vp]),
     "vocab_entropy_topk_noalloc": (i32, [vp, vp, i32, i32, i32, i32, vp, f32, i32, C.POINTER(StatsC), vp]),
+    "dllm_workspace_bytes_pages": (sz, [vp, i32, i32, i32]),
+    "dllm_forward_pages": (i32, [vp, vp, i32, i32, C.POINTER(KvPagesC), vp, i32, i32, i32, vp, i32, vp, f32,
+                                 C.POINTER(Probe), C.POINTER(StatsC), vp, sz, vp]),
     "kv_pages_init": (i32, [C.POINTER(KvPagesC), vp]),
     "kv_pages_grow": (i32, [C.POINTER(KvPagesC), vp, vp, i32, vp, vp]),
     "kv_pages_fork": (i32, [C.POINTER(KvPagesC), vp, vp, vp, i32, vp, vp]),

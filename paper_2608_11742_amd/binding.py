@@ -367,6 +367,24 @@ def kv_pages_attention(pages: KvPages, layer: int, seqs, q, out, ws, n_rows=None
                                     *_scratch(pages, ws), _page_stream(pages, stream)))
 
 
+def dllm_workspace_bytes_pages(handle, batch: int, seq: int, n_lm_pos: int) -> int:
+    return lib().dllm_workspace_bytes_pages(handle, batch, seq, n_lm_pos)
+
+
+def dllm_forward_pages(handle, tokens, pages: KvPages, seqs, lm_pos, out: Stats, ws, prefix_seq: int = 0,
+                       shared_len: int = 0, max_len: int | None = None, row_scale=None, scale: float = 1.0,
+                       probe: Probe | None = None, n_lm_pos: int | None = None, stream=None):
+    """tokens [batch, seq]: the last seq positions of the sequences seqs of `pages`."""
+    batch, seq = tokens.shape
+    n_lm = lm_pos.shape[0] if n_lm_pos is None else n_lm_pos
+    if max_len is None:
+        max_len = pages.table.shape[1] * pages.page_len
+    _check(lib().dllm_forward_pages(handle, _p(tokens), batch, seq, pages._ref, _ids(pages, seqs, batch), prefix_seq,
+                                    shared_len, max_len, _p(lm_pos), n_lm, _p(row_scale), scale,
+                                    None if probe is None else C.byref(probe), C.byref(out.c()), *_scratch(pages, ws),
+                                    _page_stream(pages, stream)))
+
+
 # ---------------------------------------------------------------- scheduler
 
 def rps_select_pivots(base: Stats, m_pos, n_m: int, prm: RpsParams, plan, stream=None):

@@ -102,7 +102,7 @@ dllm_status check_stats(const dllm_stats* s, const char* name) {
 
 // Workspace layout of one forward (256-byte aligned regions).
 struct FwdLayout {
-  size_t x, a, q, k, vt, f, hl, lm, lmsrc, part, attn, total;
+  size_t x, a, q, k, vt, f, hl, lm, lmsrc, part, attn, rope, total;
   int vt_ld;
 };
 
@@ -167,8 +167,10 @@ struct Packing {
 // Regions of a forward with `lm`, `part` and `attn` bytes for the LM head's
 // partials, the split-K parts and the attention's key ranges; the others grow
 // with batch, seq and R, the LM-head rows of the call (batch * n_lm_pos, or
-// (1 + n_branch) * n_lm_pos packed).
-FwdLayout layout_forward(const dllm_model_desc& d, int batch, int seq, int R, size_t lm, size_t part, size_t attn) {
+// (1 + n_branch) * n_lm_pos packed).  paged: rows with positions
+// of their own, which take a row each of the rotary table.
+FwdLayout layout_forward(const dllm_model_desc& d, int batch, int seq, int R, size_t lm, size_t part, size_t attn,
+                         bool paged = false) {
   FwdLayout L;
   const size_t T = elem_bytes(d.dtype);
   const size_t M = size_t(batch) * seq;
@@ -190,6 +192,7 @@ FwdLayout layout_forward(const dllm_model_desc& d, int batch, int seq, int R, si
   L.lmsrc = take(size_t(R) * 8);
   L.part = take(part);
   L.attn = attn ? take(attn) : 0;
+  L.rope = paged ? take(M * d.head_dim / 2 * sizeof(float2)) : 0;
   L.total = off;
   return L;
 }
@@ -200,6 +203,22 @@ FwdLayout plan_forward(const dllm_model_desc& d, int batch, int seq, int R) {
                         attn_partial_bytes(batch, d.n_heads, seq, d.head_dim));
 }
 
+// the heads and types of a model's pages, as far as the attention's workspace goes by them
+dllm_kv_pages pages_shape(const dllm_model_desc& d) {
+  dllm_kv_pages p{};
+  p.n_layers = d.n_layers;
+  p.n_kv_heads = d.n_heads;
+  p.head_dim = d.head_dim;
+  p.dtype = d.dtype;
+  return p;
+}
+
+// what one forward over pages needs
+FwdLayout plan_forward_pages(const dllm_model_desc& d, int batch, int seq, int R) {
+  return layout_forward(d, batch, seq, R, lmhead_workspace(d.dtype, R, d.vocab), plan_gemms(d, batch * seq).bytes,
+                        paged_attention_workspace(pages_shape(d), batch, seq, d.n_heads), true);
+}
+
 // what it and every forward of no more sequences, positions and LM-head rows
 // needs (arguments past kMaxRows are refused by the forward)
 size_t workspace_upto(const dllm_model* m, int64_t batch, int64_t seq, int64_t R) {
@@ -208,6 +227,15 @@ size_t workspace_upto(const dllm_model* m, int64_t batch, int64_t seq, int64_t R
             M = int(std::min<int64_t>(int64_t(b) * s, kMaxRows)), r = int(std::min<int64_t>(R, kMaxRows));
   return layout_forward(d, b, s, r, lm_bytes_upto(m, r), part_bytes_upto(m, M),
                         attn_partial_bytes_upto(M, d.n_heads, d.head_dim)).total;
+}
+
+// the same over pages: every forward of no more entries, rows and LM-head rows
+size_t workspace_pages_upto(const dllm_model* m, int32_t batch, int32_t seq, int64_t R) {
+  const dllm_model_desc& d = m->desc;
+  const int b = std::min(batch, KV_MAX_SEQS), s = std::min(seq, kMaxRows),
+            M = int(std::min<int64_t>(int64_t(b) * s, kMaxRows)), r = int(std::min<int64_t>(R, kMaxRows));
+  return layout_forward(d, b, s, r, lm_bytes_upto(m, r), part_bytes_upto(m, M),
+                        paged_attention_workspace_upto(pages_shape(d), b, s, d.n_heads), true).total;
 }
 
 }  // namespace
@@ -359,6 +387,11 @@ size_t dllm_workspace_bytes(const dllm_model* m, int32_t batch, int32_t seq, int
   return workspace_upto(m, batch, seq, int64_t(batch) * n_lm_pos);
 }
 
+size_t dllm_workspace_bytes_pages(const dllm_model* m, int32_t batch, int32_t seq, int32_t n_lm_pos) {
+  if (!m || batch < 1 || seq < 1 || n_lm_pos < 1) return 0;
+  return workspace_pages_upto(m, batch, seq, int64_t(batch) * n_lm_pos);
+}
+
 size_t dllm_workspace_bytes_packed(const dllm_model* m, int32_t shared_len, int32_t block_len, int32_t n_branch,
                                    int32_t n_lm_pos) {
   if (!m || shared_len < 1 || block_len < 1 || n_branch < 0 || n_lm_pos < 1) return 0;
@@ -367,10 +400,18 @@ size_t dllm_workspace_bytes_packed(const dllm_model* m, int32_t shared_len, int3
 
 namespace {
 
+// a batch over pages (see dllm_forward_pages); pages have been checked
+struct Paging {
+  const dllm_kv_pages* pages;
+  const int32_t* seqs;
+  int prefix_seq, shared_len, max_len;
+};
+
 dllm_status forward_impl(dllm_model* m, const int32_t* tokens, int32_t batch, int32_t seq, int32_t pos_offset,
                          const dllm_kv_cache* kv_prefix, const dllm_kv_cache* kv_out, const int32_t* lm_pos,
                          int32_t n_lm_pos, const float* row_scale, float scale, const dllm_probe* probe,
-                         const dllm_stats* out, void* ws, size_t ws_bytes, dllm_stream stream, const Packing* pk) {
+                         const dllm_stats* out, void* ws, size_t ws_bytes, dllm_stream stream, const Packing* pk,
+                         const Paging* pg = nullptr) {
   if (!m) return fail(DLLM_EINVAL, "dllm_forward: NULL model");
   if (!tokens || !lm_pos || !ws) return fail(DLLM_EINVAL, "dllm_forward: NULL tokens, lm_pos or ws");
   dllm_status st = check_stats(out, "out");
@@ -408,7 +449,7 @@ dllm_status forward_impl(dllm_model* m, const int32_t* tokens, int32_t batch, in
     return fail(DLLM_EINVAL, "probe has a NULL array");
   // LM-head rows: every sequence's n_lm_pos rows; packed: the anchor's, then each branch's
   const int R = (pk ? 1 + pk->n_branch : batch) * n_lm_pos;
-  const FwdLayout L = plan_forward(d, batch, seq, R);
+  const FwdLayout L = pg ? plan_forward_pages(d, batch, seq, R) : plan_forward(d, batch, seq, R);
   if (ws_bytes < L.total) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, L.total);
 
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -421,7 +462,7 @@ dllm_status forward_impl(dllm_model* m, const int32_t* tokens, int32_t batch, in
   void* f = base + L.f;
   void* hl = base + L.hl;
   const int dm = d.d_model, F = d.d_ffn, H = d.n_heads, hd = d.head_dim, dt = d.dtype;
-  const int Mi = int(M);
+  const int Mi = int(M), vt_ld = pg ? int(align_up(M, 8)) : L.vt_ld;
   const GemmSplits gs = plan_gemms(d, Mi);
   float* part = reinterpret_cast<float*>(base + L.part);
   // the residual projections leave their partials to the RMSNorm that follows
@@ -441,6 +482,11 @@ dllm_status forward_impl(dllm_model* m, const int32_t* tokens, int32_t batch, in
     lm_row = rows;
     rs_idx = rows + R;
     lm_n = R;
+  }
+  float2* rope_rows = reinterpret_cast<float2*>(base + L.rope);
+  if (pg) {
+    ProfScope ps(m, s, DLLM_PROF_OTHER);
+    TRY_HIP(pages_rope_rows(*pg->pages, pg->seqs, batch, seq, d.max_pos, m->rope, hd / 2, rope_rows, s), "rope rows");
   }
 
   {
@@ -467,6 +513,11 @@ dllm_status forward_impl(dllm_model* m, const int32_t* tokens, int32_t batch, in
       qo.pack_b0 = pk->b0;
       qo.pack_B = pk->B;
     }
+    if (pg) {   // one sequence of all rows, each at its own row of the gathered table: q, k [H][M][hd], vt [H][hd][M]
+      qo.seq = Mi;
+      qo.vt_ld = vt_ld;
+      qo.rope = rope_rows;
+    }
     {
       ProfScope ps(m, s, DLLM_PROF_GEMM_QKV);
       TRY_HIP(gemm_qkv(dt, a, dm, m->wqkv[l], Mi, dm, qo, s, &sk_qkv), "gemm_qkv");
@@ -477,6 +528,31 @@ dllm_status forward_impl(dllm_model* m, const int32_t* tokens, int32_t batch, in
       TRY_HIP(kv_store(dt, k, vt, H, seq, hd, L.vt_ld, static_cast<uint8_t*>(kv_out->k) + lay,
                        static_cast<uint8_t*>(kv_out->vt) + lay, kv_out->cap, pos_offset, s),
               "kv_store");
+    }
+    if (pg) {
+      // this layer's keys and values into the pages, then over all of them
+      const int64_t entry = int64_t(seq) * hd, head = int64_t(Mi) * hd;
+      {
+        ProfScope ps(m, s, DLLM_PROF_OTHER);
+        TRY_HIP(pages_write_vt(*pg->pages, l, pg->seqs, batch, seq, dllm_rows{k, entry, hd, head}, vt, vt_ld, s),
+                "pages_write");
+      }
+      PagedAttn pa{};
+      pa.p = *pg->pages;
+      pa.layer = l;
+      pa.seqs = pg->seqs;
+      pa.n = batch;
+      pa.max_rows = seq;
+      pa.heads = H;
+      pa.q = dllm_rows{q, entry, hd, head};
+      pa.out = dllm_rows{a, int64_t(seq) * dm, dm, hd};
+      pa.prefix_seq = pg->prefix_seq;
+      pa.shared_len = pg->shared_len;
+      pa.max_len = pg->max_len;
+      pa.scale = 1.0f / sqrtf(float(hd));
+      pa.part = reinterpret_cast<float*>(base + L.attn);
+      ProfScope ps(m, s, DLLM_PROF_ATTENTION);
+      TRY_HIP(paged_attention(pa, s), "attention over pages");
     }
     AttnArgs aa{};
     aa.q = q;
@@ -501,7 +577,7 @@ dllm_status forward_impl(dllm_model* m, const int32_t* tokens, int32_t batch, in
       aa.pack_b0 = pk->b0;
       aa.pack_B = pk->B;
     }
-    {
+    if (!pg) {
       ProfScope ps(m, s, DLLM_PROF_ATTENTION);
       TRY_HIP(attention(dt, aa, s), "attention");
     }
@@ -924,6 +1000,30 @@ dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const 
   a.scale = scale;
   a.part = static_cast<float*>(ws);
   return hip_check(paged_attention(a, static_cast<hipStream_t>(stream)), "kv_pages_attention");
+}
+
+
+dllm_status dllm_forward_pages(dllm_model* m, const int32_t* tokens, int32_t batch, int32_t seq,
+                               const dllm_kv_pages* pages, const int32_t* seqs, int32_t prefix_seq,
+                               int32_t shared_len, int32_t max_len, const int32_t* lm_pos, int32_t n_lm_pos,
+                               const float* row_scale, float scale, const dllm_probe* probe, const dllm_stats* out,
+                               void* ws, size_t ws_bytes, dllm_stream stream) {
+  if (!m) return fail(DLLM_EINVAL, "dllm_forward_pages: NULL model");
+  const dllm_model_desc& d = m->desc;
+  dllm_status st = check_attention(pages, batch, seq, d.n_heads, "dllm_forward_pages");
+  if (st == DLLM_OK) st = check_entries(seqs, batch, "dllm_forward_pages");
+  if (st != DLLM_OK) return st;
+  if (pages->dtype != d.dtype) return fail(DLLM_EDTYPE, "dllm_forward_pages: pages of dtype %d, model %d", pages->dtype, d.dtype);
+  if (pages->n_layers != d.n_layers || pages->n_kv_heads != d.n_heads || pages->head_dim != d.head_dim)
+    return fail(DLLM_ESHAPE, "dllm_forward_pages: pages of %d layers and %d heads of %d", pages->n_layers,
+                pages->n_kv_heads, pages->head_dim);
+  if (shared_len < 0 || max_len < 0)
+    return fail(DLLM_ESHAPE, "dllm_forward_pages: shared_len %d max_len %d", shared_len, max_len);
+  if (shared_len > 0 && (prefix_seq < 0 || prefix_seq >= pages->max_seqs))
+    return fail(DLLM_EINVAL, "dllm_forward_pages: prefix_seq %d outside 0..%d", prefix_seq, pages->max_seqs - 1);
+  const Paging pg{pages, seqs, prefix_seq, shared_len, max_len};
+  return forward_impl(m, tokens, batch, seq, 0, nullptr, nullptr, lm_pos, n_lm_pos, row_scale, scale, probe, out, ws,
+                      ws_bytes, stream, nullptr, &pg);
 }
 
 }  // extern "C"

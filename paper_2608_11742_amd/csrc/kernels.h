@@ -134,8 +134,7 @@ hipError_t rps_commit_step(int32_t* tokens, int seq, int32_t* m_pos, int n_m, co
 hipError_t sched_commit_step(int32_t* tokens, int seq, int32_t* m_pos, int n_m, const StatsOut& st, int rule, int k,
                             int32_t* n_m_out, int32_t* committed, int32_t* n_committed, hipStream_t s);
 
-// paged key/value cache: tables and data (pages.hip).  fork and free take a
-// host-side bound on the table entries of a call, n * max_blocks.
+// paged key/value cache: tables and data (pages.hip)
 hipError_t pages_init(const dllm_kv_pages& p, hipStream_t s);
 hipError_t pages_grow(const dllm_kv_pages& p, const int32_t* seqs, const int32_t* add, int n, int32_t* status,
                       hipStream_t s);
@@ -147,6 +146,13 @@ size_t pages_compact_workspace(int n_pages);
 hipError_t pages_compact(const dllm_kv_pages& p, int32_t* n_used, void* ws, hipStream_t s);
 hipError_t pages_write(const dllm_kv_pages& p, int layer, const int32_t* seqs, int n, int max_rows,
                        const int32_t* n_rows, const dllm_rows& k, const dllm_rows& v, hipStream_t s);
+// the same from a forward's V^T [heads][head_dim][vt_ld], columns n * rows, already in the type of the pages
+hipError_t pages_write_vt(const dllm_kv_pages& p, int layer, const int32_t* seqs, int n, int rows, const dllm_rows& k,
+                          const void* vt, int vt_ld, hipStream_t s);
+// out[b * rows + i][half]: the rotary table's row at the position of row i of
+// entry b, the last `rows` of its sequence (clamped to 0 .. max_pos - 1)
+hipError_t pages_rope_rows(const dllm_kv_pages& p, const int32_t* seqs, int n, int rows, int max_pos,
+                           const float2* rope, int half, float2* out, hipStream_t s);
 
 // attention over the pages of one layer (paged_attention.hip)
 struct PagedAttn {
@@ -162,6 +168,8 @@ struct PagedAttn {
   float* part;             // workspace of paged_attention_workspace bytes
 };
 size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads);
+// enough for every call of no more entries and rows
+size_t paged_attention_workspace_upto(const dllm_kv_pages& p, int n, int max_rows, int heads);
 hipError_t paged_attention(const PagedAttn& a, hipStream_t s);
 
 // register-only bf16 MFMA loop (benchmark calibration); *flop: the launch's MFMA work

@@ -753,9 +753,11 @@ int mode_of(int dtype, int rows, int64_t groups, int kv_heads) {
   return rows > 16 && cdiv(rows, 16) * groups * kv_heads > 4 * kCus ? ROWS32 : ROWS16;
 }
 
-// most key ranges that a part of `items` workgroups a range is ever given
-int most_ranges(int64_t items) {
-  return int(std::min<int64_t>(kMaxRanges, std::max<int64_t>(1, 8 * kCus / std::max<int64_t>(items, 1))));
+// most key ranges that a part of `items` workgroups a range is ever given: a
+// wide part two workgroups a CU, a narrow one eight
+int64_t most_ranges(int mode, int64_t items) {
+  const int64_t wgs = mode == ROWS128 ? 2 * kCus : 8 * kCus;
+  return std::min<int64_t>(kMaxRanges, (wgs + items - 1) / items);
 }
 
 // Rows stacked per key head, in `groups` separate sets (entries of a tail).
@@ -773,7 +775,7 @@ Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys) {
   int64_t ranges;
   if (mode == ROWS128) ranges = tiles >= 24 * fill(kCus) ? fill(2 * kCus) : fill(kCus);
   else ranges = std::max(fill(2 * kCus), tiles / 24);
-  ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most_ranges(items), tiles / 4}));
+  ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most_ranges(mode, items), tiles / 4}));
   p.range = int(std::max<int64_t>(1, (tiles + ranges - 1) / ranges)) * kTile;
   p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
   return p;
@@ -819,10 +821,20 @@ void launch(const Job& j, int prefix, int tail, hipStream_t s) {
 size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads) {
   const int group = heads / p.n_kv_heads;
   auto ranges = [&](int rows, int groups) {
-    return most_ranges(int64_t(cdiv(rows, rows_of(mode_of(p.dtype, rows, groups, p.n_kv_heads)))) * groups * p.n_kv_heads);
+    const int mode = mode_of(p.dtype, rows, groups, p.n_kv_heads);
+    return most_ranges(mode, int64_t(cdiv(rows, rows_of(mode))) * groups * p.n_kv_heads);
   };
   const size_t parts = ranges(n * max_rows * group, 1) + ranges(max_rows * group, n);
   return parts * n * max_rows * heads * record(p.head_dim) * sizeof(float);
+}
+
+size_t paged_attention_workspace_upto(const dllm_kv_pages& p, int n, int max_rows, int heads) {
+  // R rows of all heads in a part of `items` workgroups have at most
+  // kMaxRanges records each, and at most (wgs / items + 1) R <= wgs * tile rows + R
+  // together
+  const int64_t R = int64_t(n) * max_rows * heads;
+  const int64_t each = std::max<int64_t>(2 * kCus * rows_of(ROWS128), 8 * kCus * rows_of(ROWS32));
+  return size_t(2 * std::min(kMaxRanges * R, each + R)) * record(p.head_dim) * sizeof(float);
 }
 
 hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {

@@ -362,8 +362,9 @@ __device__ __forceinline__ int row_count(const int32_t* n_rows, int b, int max_r
 // Tile t of entry b and one head: keys go row by row as they are; values pass
 // through LDS so that each dim's positions are stored together, 8 positions
 // (16 bytes) at a time where the rows fill them.  A tile's page ids are looked
-// up once, by the first lanes.
-template <typename T, typename TV, int HD>
+// up once, by the first lanes.  With kT the values come transposed ([dim][row],
+// v.row elements a dim) in the type of the pages and are only shifted into place.
+template <typename T, typename TV, int HD, bool kT>
 __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(dllm_kv_pages p, int layer,
                                                                     const int32_t* __restrict__ seqs, int n,
                                                                     int max_rows, const int32_t* __restrict__ n_rows,
@@ -371,7 +372,7 @@ __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(dllm_kv_page
   constexpr int E = 16 / int(sizeof(T));          // elements per 16 bytes
   constexpr int CR = HD / E;                      // chunks per row
   constexpr int PITCH = HD + 4 / int(sizeof(T));  // LDS row of one position: an odd number of words
-  __shared__ T sv[kWriteTile * PITCH];
+  __shared__ T sv[kT ? 1 : kWriteTile * PITCH];
   __shared__ int page_of[kWriteTile / 16];
   const int tid = threadIdx.x, b = blockIdx.z, h = blockIdx.y;
   const int s = seqs[b];
@@ -396,19 +397,23 @@ __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(dllm_kv_page
   const size_t head = (size_t(layer) * p.n_pages) * p.n_kv_heads + h;   // + page * n_kv_heads
   const int count = to - from;
   const T* ks = static_cast<const T*>(k.p) + int64_t(b) * k.seq + int64_t(h) * k.head + int64_t(from - first) * k.row;
-  const T* vs = static_cast<const T*>(v.p) + int64_t(b) * v.seq + int64_t(h) * v.head + int64_t(from - first) * v.row;
+  const T* vs = static_cast<const T*>(v.p) + int64_t(b) * v.seq + int64_t(h) * v.head +
+                int64_t(from - first) * (kT ? 1 : v.row);
   for (int c = tid; c < count * CR; c += kWriteThreads) {
     const int r = c / CR, e = c % CR * E, at = from - t0 + r;
     const u32x4 kv = *reinterpret_cast<const u32x4*>(ks + int64_t(r) * k.row + e);
-    const u32x4 vv = *reinterpret_cast<const u32x4*>(vs + int64_t(r) * v.row + e);
+    u32x4 vv;
+    if constexpr (!kT) vv = *reinterpret_cast<const u32x4*>(vs + int64_t(r) * v.row + e);
     const int page = page_of[at >> 4];
     if (page >= 0) {
       T* dst = static_cast<T*>(p.k) + (head + size_t(page) * p.n_kv_heads) * p.page_len * HD;
       *reinterpret_cast<u32x4*>(dst + ((t0 + at) & (p.page_len - 1)) * HD + e) = kv;
     }
-    uint32_t* row = reinterpret_cast<uint32_t*>(sv + at * PITCH + e);
+    if constexpr (!kT) {
+      uint32_t* row = reinterpret_cast<uint32_t*>(sv + at * PITCH + e);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) row[w] = vv[w];
+      for (int w = 0; w < 4; ++w) row[w] = vv[w];
+    }
   }
   __syncthreads();
   // 8 consecutive positions of one dim; 8 lanes side by side hold the tile's 64
@@ -418,23 +423,52 @@ __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(dllm_kv_page
     if (page < 0) continue;
     TV* dst = static_cast<TV*>(p.vt) + ((head + size_t(page) * p.n_kv_heads) * HD + d) * p.page_len +
               ((t0 + at) & (p.page_len - 1));
-    float x[8];
+    const bool full = at >= from - t0 && at + 8 <= to - t0;
+    auto row_of = [&](int i) { return min(max(at + i, from - t0), to - t0 - 1); };
+    if constexpr (kT) {
+      TV x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = load_f(sv + min(max(at + i, from - t0), to - t0 - 1) * PITCH + d);
-    if (at >= from - t0 && at + 8 <= to - t0) {
-      if constexpr (sizeof(TV) == 2) {
-        *reinterpret_cast<u32x4*>(dst) =
-            u32x4{pack_vt2(x[0], x[1]), pack_vt2(x[2], x[3]), pack_vt2(x[4], x[5]), pack_vt2(x[6], x[7])};
+      for (int i = 0; i < 8; ++i) x[i] = vs[int64_t(d) * v.row + row_of(i) - (from - t0)];
+      if (full) {
+        constexpr int W = int(sizeof(TV)) * 8 / 16;
+        u32x4 y[W];
+        __builtin_memcpy(y, x, sizeof x);
+#pragma unroll
+        for (int i = 0; i < W; ++i) reinterpret_cast<u32x4*>(dst)[i] = y[i];
       } else {
-        reinterpret_cast<f32x4*>(dst)[0] = f32x4{x[0], x[1], x[2], x[3]};
-        reinterpret_cast<f32x4*>(dst)[1] = f32x4{x[4], x[5], x[6], x[7]};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (at + i >= from - t0 && at + i < to - t0) dst[i] = x[i];
       }
     } else {
+      float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (at + i >= from - t0 && at + i < to - t0) store_vt(dst + i, x[i]);
+      for (int i = 0; i < 8; ++i) x[i] = load_f(sv + row_of(i) * PITCH + d);
+      if (full) {
+        if constexpr (sizeof(TV) == 2) {
+          *reinterpret_cast<u32x4*>(dst) =
+              u32x4{pack_vt2(x[0], x[1]), pack_vt2(x[2], x[3]), pack_vt2(x[4], x[5]), pack_vt2(x[6], x[7])};
+        } else {
+          reinterpret_cast<f32x4*>(dst)[0] = f32x4{x[0], x[1], x[2], x[3]};
+          reinterpret_cast<f32x4*>(dst)[1] = f32x4{x[4], x[5], x[6], x[7]};
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (at + i >= from - t0 && at + i < to - t0) store_vt(dst + i, x[i]);
+      }
     }
   }
+}
+
+__global__ __launch_bounds__(256) void rope_rows_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs, int n,
+                                                        int rows, int max_pos, const float2* __restrict__ rope,
+                                                        int half, float2* __restrict__ out) {
+  const int t = blockIdx.x * 256 + threadIdx.x, row = t / half, c = t % half;
+  if (row >= n * rows) return;
+  const int s = seqs[row / rows];
+  const int held = s >= 0 && s < p.max_seqs ? p.len[s] : 0;
+  out[t] = rope[size_t(min(max(held - rows + row % rows, 0), max_pos - 1)) * half + c];
 }
 
 size_t page_bytes_of(const dllm_kv_pages& p) {
@@ -493,18 +527,41 @@ hipError_t pages_compact(const dllm_kv_pages& p, int32_t* n_used, void* ws, hipS
   return hipGetLastError();
 }
 
-hipError_t pages_write(const dllm_kv_pages& p, int layer, const int32_t* seqs, int n, int max_rows,
-                       const int32_t* n_rows, const dllm_rows& k, const dllm_rows& v, hipStream_t s) {
+namespace {
+
+template <bool kT>
+hipError_t launch_write(const dllm_kv_pages& p, int layer, const int32_t* seqs, int n, int max_rows,
+                        const int32_t* n_rows, const dllm_rows& k, const dllm_rows& v, hipStream_t s) {
   const dim3 grid((max_rows + kWriteTile - 2) / kWriteTile + 1, p.n_kv_heads, n), block(kWriteThreads);
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, s, p, layer, seqs, n, max_rows, n_rows, k, v);
     return hipGetLastError();
   };
   if (p.dtype == DLLM_BF16)
-    return p.head_dim == 128 ? launch(pages_write_kernel<bf16_t, bf16_t, 128>)
-                             : launch(pages_write_kernel<bf16_t, bf16_t, 64>);
-  return p.head_dim == 128 ? launch(pages_write_kernel<float, float, 128>)
-                           : launch(pages_write_kernel<float, float, 64>);
+    return p.head_dim == 128 ? launch(pages_write_kernel<bf16_t, bf16_t, 128, kT>)
+                             : launch(pages_write_kernel<bf16_t, bf16_t, 64, kT>);
+  return p.head_dim == 128 ? launch(pages_write_kernel<float, float, 128, kT>)
+                           : launch(pages_write_kernel<float, float, 64, kT>);
+}
+
+}  // namespace
+
+hipError_t pages_write(const dllm_kv_pages& p, int layer, const int32_t* seqs, int n, int max_rows,
+                       const int32_t* n_rows, const dllm_rows& k, const dllm_rows& v, hipStream_t s) {
+  return launch_write<false>(p, layer, seqs, n, max_rows, n_rows, k, v, s);
+}
+
+hipError_t pages_write_vt(const dllm_kv_pages& p, int layer, const int32_t* seqs, int n, int rows, const dllm_rows& k,
+                          const void* vt, int vt_ld, hipStream_t s) {
+  const dllm_rows v{const_cast<void*>(vt), rows, vt_ld, int64_t(p.head_dim) * vt_ld};
+  return launch_write<true>(p, layer, seqs, n, rows, nullptr, k, v, s);
+}
+
+hipError_t pages_rope_rows(const dllm_kv_pages& p, const int32_t* seqs, int n, int rows, int max_pos,
+                           const float2* rope, int half, float2* out, hipStream_t s) {
+  const int wgs = int((int64_t(n) * rows * half + 255) / 256);
+  hipLaunchKernelGGL(rope_rows_kernel, dim3(wgs), dim3(256), 0, s, p, seqs, n, rows, max_pos, rope, half, out);
+  return hipGetLastError();
 }
 
 }  // namespace dllm

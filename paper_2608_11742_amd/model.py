@@ -97,3 +97,27 @@ class Model:
                               pos_offset=pos_offset, kv_prefix=kv_prefix, row_scale=row_scale, scale=scale,
                               probe=probe, n_lm_pos=n, stream=stream)
         return out
+
+    def new_kv_pages(self, n_pages: int, page_len: int = 64, max_seqs: int = 64, max_len: int | None = None) -> B.KvPages:
+        """A paged key/value cache for this model, empty: sequences of at most
+        max_len positions (default: every position id the model has)."""
+        s = self.shape
+        max_len = self.desc.max_pos if max_len is None else max_len
+        return B.KvPages.empty(s.n_layers, n_pages, s.n_heads, page_len, s.head_dim, max_seqs,
+                               -(-max_len // page_len), dtype=self.torch_dtype, device=self.device)
+
+    def forward_pages(self, tokens, pages: B.KvPages, seqs, lm_pos, out: B.Stats | None = None,
+                      n_lm_pos: int | None = None, row_scale=None, scale: float = 1.0, prefix_seq: int = 0,
+                      shared_len: int = 0, max_len: int | None = None, probe=None, k: int = 16,
+                      stream=None) -> B.Stats:
+        """Forward of tokens [batch, seq] as the last seq positions of the
+        sequences seqs (int32, device) of `pages`: their keys and values are
+        written to the pages, and every row attends to all of its sequence."""
+        n = lm_pos.shape[0] if n_lm_pos is None else n_lm_pos
+        if out is None:
+            out = B.Stats(tokens.shape[0] * n, k, device=self.device)
+        ws = self._reserve(B.dllm_workspace_bytes_pages(self.handle, tokens.shape[0], tokens.shape[1], n))
+        B.dllm_forward_pages(self.handle, tokens, pages, seqs, lm_pos, out, ws, prefix_seq=prefix_seq,
+                             shared_len=shared_len, max_len=max_len, row_scale=row_scale, scale=scale, probe=probe,
+                             n_lm_pos=n, stream=stream)
+        return out

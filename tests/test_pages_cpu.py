@@ -153,3 +153,13 @@ def test_host_attention_is_a_softmax():
     assert np.all(mass >= np.abs(out))
     out, _, _ = attend(q, [k[:1]], [v[:1]], [3], True, 0.5)
     assert not out[0, :2].any() and np.allclose(out[0, 2], v[0][[0, 0, 1, 1]])
+
+
+@needs_lib
+def test_forward_pages_without_a_model(abi):
+    _abi, lib = abi
+    p = C.byref(pages(_abi))
+    st = _abi.StatsC(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 16)
+    assert lib.dllm_forward_pages(None, FAKE, 1, 4, p, FAKE, 0, 0, 4, FAKE, 1, None, 1.0, None, C.byref(st), FAKE,
+                                  1 << 30, None) == 1
+    assert lib.dllm_workspace_bytes_pages(None, 1, 4, 1) == 0
