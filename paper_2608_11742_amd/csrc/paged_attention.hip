@@ -11,7 +11,10 @@
 //   tail     each entry's own positions after them, for its own rows.
 // and each of the two over workgroups by ranges of keys, where there are few
 // rows.  Every range leaves a record per row, and a merge joins them in order;
-// with one range in all the workgroup writes the output itself.
+// with one range in all the workgroup writes the output itself.  Where the
+// entries are few and short, reading the prefix again for each of them costs
+// less than a join: then every entry's range starts at position 0 and takes its
+// pages from the prefix's table first.
 //
 // Two kernels, by the number of stacked rows:
 //   narrow   up to 32 rows: bound by the keys and values it streams.  Four
@@ -57,6 +60,7 @@ struct Job {
   float scale_log2;   // scale * log2(e)
   int group;          // query heads per key head
   Part prefix, tail;
+  bool stacked;       // the prefix is a part of its own; else each tail starts at position 0
   bool direct;        // one range in all: the output itself
 };
 
@@ -85,16 +89,22 @@ __device__ __forceinline__ int limit_of(const PagedAttn& a, const Entry& e, int 
   return a.causal ? max(0, min(e.held, e.held - e.rows + i + 1)) : e.held;
 }
 
-// A workgroup's share: rows row0 .. (stacked as ((entry * max_rows) + row) *
-// group + query head) of key head `head`, keys k0 .. k1 - 1 of the table,
-// record index.
-struct Share {
-  int row0, row_end, head, k0, k1, part;
-  const __attribute__((address_space(4))) int32_t* table;   // read on the scalar unit: uniform, not written here
-};
-__device__ __forceinline__ const __attribute__((address_space(4))) int32_t* table_row(const PagedAttn& a, int seq) {
-  return (const __attribute__((address_space(4))) int32_t*)(a.p.table + size_t(seq) * a.p.max_blocks);
+// a table's row, read on the scalar unit: uniform, and not written here
+typedef const __attribute__((address_space(4))) int32_t* table_t;
+__device__ __forceinline__ table_t table_row(const PagedAttn& a, int seq) {
+  return (table_t)(a.p.table + size_t(seq) * a.p.max_blocks);
 }
+
+// A workgroup's share: rows row0 .. (stacked as ((entry * max_rows) + row) *
+// group + query head) of key head `head`, keys k0 .. k1 - 1, record index.
+// Pages of positions before `split` are `before`'s, then `after`'s.
+struct Share {
+  int row0, row_end, head, k0, k1, part, split;
+  table_t before, after;
+  __device__ __forceinline__ int page(int pos, int shift, int last_block) const {
+    return (pos < split ? before : after)[min(pos >> shift, last_block)];
+  }
+};
 
 // Workgroup x of a part: its item (a key range of one head) and row tile.
 // Workgroups go to the 8 XCDs in turn; the row tiles of an item, which read the
@@ -125,16 +135,19 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
     w.k0 = r * part.range;
     w.k1 = min(w.k0 + part.range, s);
     w.part = r;
-    w.table = table_row(a, a.prefix_seq);
+    w.split = 0;
+    w.before = w.after = table_row(a, a.prefix_seq);
     return w.k0 < w.k1;
   }
   const Entry e = entry_of(a, b);
   w.row0 = b * per + it.tile * tile_rows;
   w.row_end = (b + 1) * per;
-  w.k0 = s + r * part.range;
+  w.k0 = (j.stacked ? s : 0) + r * part.range;
   w.k1 = r + 1 == part.ranges ? e.held : min(w.k0 + part.range, e.held);
   w.part = j.prefix.ranges + r;
-  w.table = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
+  w.split = j.stacked ? 0 : s;
+  w.before = table_row(a, a.prefix_seq);
+  w.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
   // an entry without positions still has its rows set to 0 where nothing is joined
   return w.row0 < b * per + e.rows * j.group && (w.k0 < w.k1 || j.direct);
 }
@@ -190,8 +203,9 @@ struct Narrow {
   static constexpr int E = 16 / int(sizeof(T));             // elements per chunk
   static constexpr int CK = HD / E;                         // chunks per key row
   // a step's K takes 64 registers at most, its V as many; half of that beside the state of two row blocks
-  static constexpr int KS = (NQB == 1 ? 16 : 8) * 1024 / (HD * int(sizeof(T))) < 64
-                                ? (NQB == 1 ? 16 : 8) * 1024 / (HD * int(sizeof(T))) : 64;
+  // (and with fp32, whose steps the products bound: shorter ones come out more even)
+  static constexpr int kRegs = NQB == 1 && kHalf ? 16 : 8;
+  static constexpr int KS = kRegs * 1024 / (HD * int(sizeof(T))) < 64 ? kRegs * 1024 / (HD * int(sizeof(T))) : 64;
   static constexpr int NB = KS / 16;                        // 16-key blocks of a step
   static constexpr int QS = CK / 4;                         // MFMA steps over head_dim
   static constexpr int NDB = HD / 16;
@@ -231,7 +245,7 @@ struct Narrow {
     // again), brought into the pool where they are used: loads do not wait here
     auto pages_at = [&](int k0, int (&id)[NB]) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i) id[i] = w.table[min((k0 + 16 * i) >> shift, last_block)];
+      for (int i = 0; i < NB; ++i) id[i] = w.page(k0 + 16 * i, shift, last_block);
     };
     auto in_pool = [&](int p) { return min(max(p, 0), a.p.n_pages - 1); };
     u32x4 kf[NB][QS], vf[NDB][NV];
@@ -481,7 +495,7 @@ struct Wide {
 
     auto pages_at = [&](int k0, int (&id)[4]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) id[i] = w.table[min((k0 + 16 * i) >> shift, last_block)];
+      for (int i = 0; i < 4; ++i) id[i] = w.page(k0 + 16 * i, shift, last_block);
     };
     auto in_pool = [&](int p) { return min(max(p, 0), a.p.n_pages - 1); };
     // this lane's source of each copy: a key row's chunk, a dim row's chunk
@@ -693,7 +707,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   const int h = row % a.heads, t = row / a.heads, b = in ? t / a.max_rows : 0, i = t % a.max_rows;
   const Entry e = entry_of(a, b);
   const bool live = in && i < e.rows;
-  const int s = shared_of(a), lim = limit_of(a, e, i);
+  const int s = j.stacked ? shared_of(a) : 0, lim = limit_of(a, e, i);
   const int np = live && j.prefix.ranges ? (min(lim, s) + j.prefix.range - 1) / j.prefix.range : 0;
   const int nt = live && lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
   const size_t stride = size_t(a.n) * a.max_rows * a.heads * record(HD);
@@ -760,13 +774,15 @@ int64_t most_ranges(int mode, int64_t items) {
   return std::min<int64_t>(kMaxRanges, (wgs + items - 1) / items);
 }
 
+constexpr int kStep = kWaves * kTile;   // keys that a narrow workgroup takes at a time, about 1 us
+
 // Rows stacked per key head, in `groups` separate sets (entries of a tail).
 // Two workgroups fit a CU.  Narrow parts are bound by memory: as many ranges
 // as fill the chip, and where they are long ones of 24 tiles, so that batches
-// of unlike lengths come out even.  Wide ones take one
-// workgroup a CU, which leaves the other slot to the tails, and two where
-// ranges stay long enough for the second to gain more than its records cost to
-// join.
+// of unlike lengths come out even; a join costs about as much as 6 steps, so
+// shorter parts are not divided.  Wide ones take one workgroup a CU, which
+// leaves the other slot to the tails, and two where ranges stay long enough for
+// the second to gain more than its records cost to join.
 Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys) {
   Part p;
   p.row_tiles = cdiv(rows, rows_of(mode));
@@ -774,11 +790,22 @@ Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys) {
   auto fill = [&](int64_t wgs) { return (wgs + items - 1) / items; };
   int64_t ranges;
   if (mode == ROWS128) ranges = tiles >= 24 * fill(kCus) ? fill(2 * kCus) : fill(kCus);
-  else ranges = std::max(fill(2 * kCus), tiles / 24);
+  else ranges = keys <= 6 * kStep ? 1 : std::max(fill(2 * kCus), tiles / 24);
   ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most_ranges(mode, items), tiles / 4}));
   p.range = int(std::max<int64_t>(1, (tiles + ranges - 1) / ranges)) * kTile;
   p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
   return p;
+}
+
+// Is the prefix a part of its own?  Not if all entries can walk it by
+// themselves in a few steps (a round of two workgroups a CU) and its keys,
+// read once for every row tile, stay within what the L2s deliver meanwhile.
+bool stacks(const PagedAttn& a, int mode, int rows, int64_t keys) {
+  if (mode == ROWS128) return true;
+  const int64_t items = int64_t(cdiv(rows, rows_of(mode))) * a.n * a.p.n_kv_heads;
+  const int64_t rounds = (items + 2 * kCus - 1) / (2 * kCus), steps = (keys + kStep - 1) / kStep;
+  const int64_t bytes = items * keys * 2 * a.p.head_dim * (a.p.dtype == DLLM_BF16 ? 2 : 4);
+  return rounds * steps > 6 || bytes > (int64_t(48) << 20);
 }
 
 template <typename T, int HD, int PREFIX, int TAIL>
@@ -846,10 +873,13 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   const int64_t most = int64_t(a.p.max_blocks) * a.p.page_len;
   const int64_t shared = std::min<int64_t>(a.shared_len, most) / a.p.page_len * a.p.page_len;
   const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
-  const int mode_t = mode_of(dt, rows_t, a.n, kvh), mode_p = shared > 0 ? mode_of(dt, rows_p, 1, kvh) : mode_t;
-  j.prefix = shared > 0 ? plan_part(mode_p, rows_p, 1, kvh, shared) : Part{1, 0, kTile};
-  if (shared == 0) j.a.shared_len = 0;
-  j.tail = plan_part(mode_t, rows_t, a.n, kvh, std::max<int64_t>(1, std::min<int64_t>(a.max_len, most) - shared));
+  const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
+  const int mode_t = mode_of(dt, rows_t, a.n, kvh);
+  j.stacked = shared > 0 && stacks(a, mode_t, rows_t, std::max(keys, shared));
+  const int mode_p = j.stacked ? mode_of(dt, rows_p, 1, kvh) : mode_t;
+  j.prefix = j.stacked ? plan_part(mode_p, rows_p, 1, kvh, shared) : Part{1, 0, kTile};
+  if (shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
+  j.tail = plan_part(mode_t, rows_t, a.n, kvh, j.stacked ? std::max<int64_t>(1, keys - shared) : keys);
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
   if (dt == DLLM_BF16)
     a.p.head_dim == 128 ? launch<bf16_t, 128>(j, mode_p, mode_t, s) : launch<bf16_t, 64>(j, mode_p, mode_t, s);
