@@ -450,18 +450,18 @@ __device__ __forceinline__ void copy16(const void* src, uint32_t lds) {
                                    16, 0, 0);
 }
 
-// bf16 models.  MFMA row r of a 32-key half is key r with bits 2 and 3
-// exchanged: output registers 8 s .. 8 s + 7 of lane half f are then keys
-// 16 s + 8 f .. + 7, the chunk of V^T that this lane half multiplies in step s.
+// Tiles of 64 bf16 keys in LDS, for 32 x 32 MFMAs.  MFMA row r of a 32-key half
+// is key r with bits 2 and 3 exchanged: output registers 8 s .. 8 s + 7 of lane
+// half f are then keys 16 s + 8 f .. + 7, the chunk of V^T that this lane half
+// multiplies in step s.
 template <int HD>
-struct Wide {
+struct Tile {
   static constexpr int RB = HD * 2;                 // bytes of a key row
   static constexpr int CK = RB / 16;                // chunks of a key row
   static constexpr int KB = kTile * RB;             // K tile; V^T tile: HD rows of 128 bytes
-  static constexpr int SLOT = 2 * KB;
-  static constexpr int SMEM = 2 * SLOT;
+  static constexpr int BYTES = 2 * KB;
   static constexpr int KROWS = kWave / CK;          // key rows of one 1 KB copy
-  static constexpr int IC = KB / 1024 / kWaves;     // copies a wave issues for K, and for V
+  static constexpr int IC = KB / 1024 / kWaves;     // copies each of four waves issues for K, and for V
   static constexpr int QS = HD / 16;                // MFMA steps over head_dim
   static constexpr int NDB = HD / 32;
 
@@ -470,38 +470,37 @@ struct Wide {
   // two rows of 128)
   __device__ __forceinline__ static int kswz(int r) { return CK == 16 ? r & 15 : (r >> 1) & 7; }
   __device__ __forceinline__ static int vswz(int d) { return (d >> 1) & 7; }
+  // key within its 32 of MFMA row r
+  __device__ __forceinline__ static int key_of(int r) { return (r & 0x13) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
-  __device__ static void run(const Job& j, const Share& w, uint8_t* smem) {
-    const PagedAttn& a = j.a;
-    const int kvh = w.head;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int fr = lane & 31, f = lane >> 5;
-    const int shift = 31 - __builtin_clz(a.p.page_len), pmask = a.p.page_len - 1;
-    const size_t head_bytes = size_t(a.p.page_len) * RB, page_bytes = head_bytes * a.p.n_kv_heads;
-    const size_t base = (size_t(a.layer) * a.p.n_pages * a.p.n_kv_heads + kvh) * head_bytes;
-    const uint8_t* K = static_cast<const uint8_t*>(a.p.k) + base;
-    const uint8_t* V = static_cast<const uint8_t*>(a.p.vt) + base;
-    const int last_block = max(w.k1 - 1, 0) >> shift;
-    const uint32_t lds0 = lds_address(smem);
+  // one wave's part (`wave` of four) of copying a tile
+  struct Copier {
+    const uint8_t* K;
+    const uint8_t* V;
+    size_t page_bytes;
+    int wave, lane, page_len, n_pages, shift, last_block;
 
-    const RowAt at = row_at(j, min(w.row0 + 32 * wave + fr, w.row_end - 1));
-    u32x4 qf[QS];
-    const bf16_t* q = static_cast<const bf16_t*>(a.q.p) + at.b * a.q.seq + at.i * a.q.row +
-                      (kvh * j.group + at.g) * a.q.head;
-#pragma unroll
-    for (int st = 0; st < QS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(q + (2 * st + f) * 8);
-    const Entry entry = entry_of(a, at.b);
-    const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
-
-    auto pages_at = [&](int k0, int (&id)[4]) {
+    __device__ __forceinline__ Copier(const PagedAttn& a, int head, int wave_, int end) : wave(wave_) {
+      lane = threadIdx.x & 63;
+      page_len = a.p.page_len;
+      n_pages = a.p.n_pages;
+      shift = 31 - __builtin_clz(page_len);
+      last_block = max(end - 1, 0) >> shift;
+      const size_t head_bytes = size_t(page_len) * RB;
+      page_bytes = head_bytes * a.p.n_kv_heads;
+      const size_t base = (size_t(a.layer) * n_pages * a.p.n_kv_heads + head) * head_bytes;
+      K = static_cast<const uint8_t*>(a.p.k) + base;
+      V = static_cast<const uint8_t*>(a.p.vt) + base;
+    }
+    __device__ __forceinline__ int in_pool(int p) const { return min(max(p, 0), n_pages - 1); }
+    // table entries of the tile's 16-key groups (past the last key: its page
+    // again), brought into the pool where they are used: loads do not wait here
+    __device__ __forceinline__ void pages_at(const Share& w, int k0, int (&id)[4]) const {
 #pragma unroll
       for (int i = 0; i < 4; ++i) id[i] = w.page(k0 + 16 * i, shift, last_block);
-    };
-    auto in_pool = [&](int p) { return min(max(p, 0), a.p.n_pages - 1); };
-    // this lane's source of each copy: a key row's chunk, a dim row's chunk
-    const int kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vswz(8 * wave + vd);
-    auto issue = [&](int k0, const int (&id)[4], int slot) {
-      const uint32_t dst = lds0 + slot * SLOT;
+    }
+    __device__ __forceinline__ void issue(int k0, const int (&id)[4], uint32_t dst) const {
+      const int pmask = page_len - 1, kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vswz(8 * wave + vd);
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
         const int grp = i * kWaves + wave, r = grp * KROWS + kr;
@@ -513,148 +512,371 @@ struct Wide {
         copy16(src + (r & 15) * RB + ((lane % CK) ^ kswz(r)) * 16, dst + grp * 1024);
       }
       const int page = in_pool(vc < 4 ? (vc < 2 ? id[0] : id[1]) : (vc < 6 ? id[2] : id[3]));
-      const uint8_t* src = V + page * page_bytes + size_t(vd) * (a.p.page_len * 2) + ((k0 + 8 * vc) & pmask) * 2;
+      const uint8_t* src = V + page * page_bytes + size_t(vd) * (page_len * 2) + ((k0 + 8 * vc) & pmask) * 2;
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
         const int grp = i * kWaves + wave;
-        copy16(src + size_t(grp) * 8 * (a.p.page_len * 2), dst + KB + grp * 1024);
+        copy16(src + size_t(grp) * 8 * (page_len * 2), dst + KB + grp * 1024);
       }
-    };
+    }
+  };
 
-    f32x16 o[NDB];
+  // values of keys from `left` on (whatever they are) set to 0; t: thread of 256
+  __device__ __forceinline__ static void zero_values(uint8_t* sv, int t, int left) {
+    for (int c = t; c < HD * 8; c += kThreads) {
+      const int d = c >> 3, n = left - 8 * (c & 7);
+      if (n >= 8) continue;
+      u32x4* p = reinterpret_cast<u32x4*>(sv + d * 128 + (((c & 7) ^ vswz(d)) << 4));
+      u32x4 x = *p;
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+      for (int i = 0; i < 4; ++i) x[i] &= n > 2 * i + 1 ? ~0u : n > 2 * i ? 0xffffu : 0u;
+      *p = x;
+    }
+  }
+  __device__ __forceinline__ static u32x4 key_chunk(const uint8_t* sk, int h, int st, int lane) {
+    const int r = 32 * h + key_of(lane & 31);
+    return *reinterpret_cast<const u32x4*>(sk + r * RB + (((2 * st + (lane >> 5)) ^ kswz(r)) << 4));
+  }
+  __device__ __forceinline__ static u32x4 value_chunk(const uint8_t* sv, int st, int db, int lane) {
+    const int d = 32 * db + (lane & 31);
+    return *reinterpret_cast<const u32x4*>(sv + d * 128 + (((2 * st + (lane >> 5)) ^ vswz(d)) << 4));
+  }
+};
+
+// one wave's 32 rows: state of their softmax and a block of H x 32 keys into it
+template <int HD>
+struct Rows32 {
+  using L = Tile<HD>;
+  u32x4 qf[L::QS];
+  f32x16 o[L::NDB];
+  float m = -INFINITY, l = 0.f;   // reference (log2 units), this lane's part of the sum
+
+  __device__ __forceinline__ void begin() {
+#pragma unroll
+    for (int db = 0; db < L::NDB; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
+  }
+  __device__ __forceinline__ void load_q(const bf16_t* q) {
+    const int f = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int st = 0; st < L::QS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(q + (2 * st + f) * 8);
+  }
+  template <int H>
+  __device__ __forceinline__ void scores(const u32x4 (&kf)[H][L::QS], f32x16 (&sc)[H]) const {
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[h][i] = 0.f;
+#pragma unroll
+    for (int st = 0; st < L::QS; ++st)
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[h][st]),
+                                                        __builtin_bit_cast(bf16x8, qf[st]), sc[h], 0, 0, 0);
+  }
+  // scores of keys k0 .. into probabilities (binary16 pairs); keys from lim on are not seen
+  template <int H>
+  __device__ __forceinline__ void softmax(f32x16 (&sc)[H], int k0, int lim, float scale_log2, u32x4 (&pf)[2 * H]) {
+    const int f = (threadIdx.x >> 5) & 1;
+    // element i of half h: key 32 h + 16 (i / 8) + 8 f + i % 8
+    if (!__all(k0 + 32 * H <= lim)) {
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (k0 + 32 * h + 16 * (i >> 3) + 8 * f + (i & 7) >= lim) sc[h][i] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[h][i]);
+    top = pair_max(top) * scale_log2;
+    const float mn = top > m + 8.f ? top : m;
+    const float ref = mn == -INFINITY ? 0.f : mn;
+    if (__any(mn != m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < L::NDB; ++db) o[db] *= alpha;
+    }
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(sc[h][i], scale_log2, -ref));
+        const float y = __builtin_amdgcn_exp2f(fmaf(sc[h][i + 1], scale_log2, -ref));
+        sum += x + y;
+        pf[2 * h + (i >> 3)][(i & 7) >> 1] = pack_f16x2(x, y);
+      }
+    l += sum;
+  }
+  __device__ __forceinline__ void add(int db, u32x4 vf, u32x4 pf) {
+    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf), __builtin_bit_cast(half8, pf), o[db],
+                                                   0, 0, 0);
+  }
+};
+
+// 128 rows, 32 a wave, over one range of keys
+template <int HD>
+struct Wide {
+  using L = Tile<HD>;
+  static constexpr int SMEM = 2 * L::BYTES;
+
+  __device__ static void run(const Job& j, const Share& w, uint8_t* smem) {
+    const PagedAttn& a = j.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int fr = lane & 31, f = lane >> 5;
+    const uint32_t lds0 = lds_address(smem);
+    const typename L::Copier copier(a, w.head, wave, w.k1);
+
+    const RowAt at = row_at(j, min(w.row0 + 32 * wave + fr, w.row_end - 1));
+    Rows32<HD> rows;
+    rows.load_q(static_cast<const bf16_t*>(a.q.p) + at.b * a.q.seq + at.i * a.q.row +
+                (w.head * j.group + at.g) * a.q.head);
+    rows.begin();
+    const Entry entry = entry_of(a, at.b);
+    const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
 
     int id[4];
-    pages_at(w.k0, id);
-    if (w.k0 < w.k1) issue(w.k0, id, 0);
-    pages_at(w.k0 + kTile, id);
+    copier.pages_at(w, w.k0, id);
+    if (w.k0 < w.k1) copier.issue(w.k0, id, lds0);
+    copier.pages_at(w, w.k0 + kTile, id);
     int slot = 0;
     for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
       wait_vmcnt<0>();
       __syncthreads();   // tile k0 has landed; the other slot has been read
-      const uint8_t* sk = smem + slot * SLOT;
-      uint8_t* sv = smem + slot * SLOT + KB;
-      if (k0 + kTile > w.k1) {   // values past the last key: whatever they are, times 0
-        for (int c = tid; c < HD * 8; c += kThreads) {
-          const int d = c >> 3, left = w.k1 - k0 - 8 * (c & 7);
-          if (left >= 8) continue;
-          u32x4* p = reinterpret_cast<u32x4*>(sv + d * 128 + (((c & 7) ^ vswz(d)) << 4));
-          u32x4 x = *p;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] &= left > 2 * i + 1 ? ~0u : left > 2 * i ? 0xffffu : 0u;
-          *p = x;
-        }
+      const uint8_t* sk = smem + slot * L::BYTES;
+      uint8_t* sv = smem + slot * L::BYTES + L::KB;
+      if (k0 + kTile > w.k1) {
+        L::zero_values(sv, tid, w.k1 - k0);
         __syncthreads();
       } else if (k0 + kTile < w.k1) {
-        issue(k0 + kTile, id, slot ^ 1);
-        pages_at(k0 + 2 * kTile, id);
+        copier.issue(k0 + kTile, id, lds0 + (slot ^ 1) * L::BYTES);
+        copier.pages_at(w, k0 + 2 * kTile, id);
       }
+      // every K fragment is on its way before the first product waits for one,
+      // half of the V fragments before the softmax
+      u32x4 kf[2][L::QS], vf[2][L::NDB], pf[4];
       f32x16 sc[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int st = 0; st < L::QS; ++st)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[h][i] = 0.f;
-      // every K fragment is on its way before the first product waits for one
-      u32x4 kf[2][QS], vf[2][NDB];
-#pragma unroll
-      for (int st = 0; st < QS; ++st)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = 32 * h + ((fr & 0x13) | ((fr & 4) << 1) | ((fr & 8) >> 1));
-          kf[h][st] = *reinterpret_cast<const u32x4*>(sk + r * RB + (((2 * st + f) ^ kswz(r)) << 4));
-        }
+        for (int h = 0; h < 2; ++h) kf[h][st] = L::key_chunk(sk, h, st, lane);
       __builtin_amdgcn_sched_barrier(0);
+      rows.scores(kf, sc);
 #pragma unroll
-      for (int st = 0; st < QS; ++st)
+      for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[h][st]),
-                                                          __builtin_bit_cast(bf16x8, qf[st]), sc[h], 0, 0, 0);
-      auto read_v = [&](int st) {
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) {
-          const int d = 32 * db + fr;
-          vf[st & 1][db] = *reinterpret_cast<const u32x4*>(sv + d * 128 + (((2 * st + f) ^ vswz(d)) << 4));
-        }
-      };
-      read_v(0);
-      read_v(1);
+        for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, st, db, lane);
       __builtin_amdgcn_sched_barrier(0);
-      // element i of half h: key 32 h + 16 (i / 8) + 8 f + i % 8
-      if (!__all(k0 + kTile <= lim)) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (k0 + 32 * h + 16 * (i >> 3) + 8 * f + (i & 7) >= lim) sc[h][i] = -INFINITY;
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[h][i]);
-      top = pair_max(top) * j.scale_log2;
-      const float mn = top > m + 8.f ? top : m;
-      const float ref = mn == -INFINITY ? 0.f : mn;
-      if (__any(mn != m)) {
-        const float alpha = __builtin_amdgcn_exp2f(m - ref);
-        l *= alpha;
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) o[db] *= alpha;
-      }
-      m = mn;
-      u32x4 pf[4];
-      float sum = 0.f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(sc[h][i], j.scale_log2, -ref));
-          const float y = __builtin_amdgcn_exp2f(fmaf(sc[h][i + 1], j.scale_log2, -ref));
-          sum += x + y;
-          pf[2 * h + (i >> 3)][(i & 7) >> 1] = pack_f16x2(x, y);
-        }
-      l += sum;
+      rows.softmax(sc, k0, lim, j.scale_log2, pf);
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
 #pragma unroll
-        for (int db = 0; db < NDB; ++db)
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf[st & 1][db]),
-                                                         __builtin_bit_cast(half8, pf[st]), o[db], 0, 0, 0);
-        if (st < 2) read_v(st + 2);
+        for (int db = 0; db < L::NDB; ++db) rows.add(db, vf[st & 1][db], pf[st]);
+        if (st < 2) {
+#pragma unroll
+          for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, st + 2, db, lane);
+        }
       }
     }
-    l = pair_sum(l);
+    const float l = pair_sum(rows.l);
     if (w.row0 + 32 * wave + fr >= w.row_end || at.i >= entry.rows) return;
     // element i of block db: dim 32 db + 8 (i / 4) + 4 f + i % 4
     if (j.direct) {
       bf16_t* out = static_cast<bf16_t*>(a.out.p) + at.b * a.out.seq + at.i * a.out.row +
-                    (kvh * j.group + at.g) * a.out.head;
+                    (w.head * j.group + at.g) * a.out.head;
       const float inv = 1.f / l;
 #pragma unroll
-      for (int db = 0; db < NDB; ++db)
+      for (int db = 0; db < L::NDB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          store_f(out + 32 * db + 8 * (i >> 2) + 4 * f + (i & 3), lim_row > 0 ? o[db][i] * inv : 0.f);
+          store_f(out + 32 * db + 8 * (i >> 2) + 4 * f + (i & 3), lim_row > 0 ? rows.o[db][i] * inv : 0.f);
     } else {
-      float* rec = record_of(j, w.part, at, kvh, HD);
+      float* rec = record_of(j, w.part, at, w.head, HD);
 #pragma unroll
-      for (int db = 0; db < NDB; ++db)
+      for (int db = 0; db < L::NDB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
           *reinterpret_cast<f32x4*>(rec + 32 * db + 2 * i + 4 * f) =
-              f32x4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]};
+              f32x4{rows.o[db][i], rows.o[db][i + 1], rows.o[db][i + 2], rows.o[db][i + 3]};
       if (f == 0) {
-        rec[HD] = m;
+        rec[HD] = rows.m;
         rec[HD + 1] = l;
       }
     }
   }
 };
+
+// ---------------------------------------------------------------- pairs
+
+// Two blocks of 32 rows, each of one entry, over the shared prefix and then
+// each over its own tail, in one workgroup of 8 waves that writes the output:
+// wave w takes block w % 2 and every fourth 32 keys.  A pair of 64-key tiles of
+// the prefix is in LDS at a time; waves 0 .. 3 copy and use the first, 4 .. 7 the
+// second.  A tail's keys are few and used by one block alone: their fragments
+// come straight from memory.  The four states of a block are joined through LDS.
+template <int HD>
+struct Pairs {
+  using L = Tile<HD>;
+  static constexpr int kWays = 4;
+  static constexpr int kPairThreads = 2 * kWays * kWave;
+  static constexpr int kKeys = kWays * 32;             // keys of a step
+  static constexpr int RING = 4 * L::BYTES;            // two slots of two tiles
+  static constexpr int STATE = 32 + 2;                 // floats a lane hands over at a time
+  static constexpr int JOIN = 2 * kWays * STATE * kWave * 4;
+  static constexpr int SMEM = RING > JOIN ? RING : JOIN;
+
+  __device__ static void run(const Job& j, int x, uint8_t* smem) {
+    const PagedAttn& a = j.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int fr = lane & 31, f = lane >> 5, block = wave & 1, way = wave >> 1, tile = wave >> 2;
+    const int per = a.max_rows * j.group, per_blocks = (per + 31) / 32, pairs = (a.n * per_blocks + 1) / 2;
+    const Item it = item_of(x, pairs);
+    if (it.item >= a.p.n_kv_heads) return;
+    const int head = it.item;
+    const int rb = min(2 * it.tile + block, a.n * per_blocks - 1);   // an odd last block is taken twice
+    const bool own = 2 * it.tile + block < a.n * per_blocks;
+    const int b = rb / per_blocks, r0 = rb % per_blocks * 32;
+
+    const int s = shared_of(a);
+    const Entry e = entry_of(a, b);
+    Share prefix{}, tail{};
+    prefix.before = prefix.after = table_row(a, a.prefix_seq);
+    tail.before = tail.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
+    const typename L::Copier copier(a, head, wave & 3, s), own_keys(a, head, 0, e.held);
+    const int first = kTile * tile;   // of this wave's tile in a step
+    const uint32_t lds0 = lds_address(smem) + tile * L::BYTES;
+    int id[4];
+    copier.pages_at(prefix, first, id);
+    if (s > 0) copier.issue(first, id, lds0);
+    copier.pages_at(prefix, first + kKeys, id);
+
+    const int row = min(r0 + fr, per - 1), i = row / j.group, g = row % j.group;
+    Rows32<HD> rows;
+    rows.load_q(static_cast<const bf16_t*>(a.q.p) + b * a.q.seq + i * a.q.row + (head * j.group + g) * a.q.head);
+    rows.begin();
+    const int limit = limit_of(a, e, i), lim = min(limit, s);
+
+    int slot = 0;
+    for (int k0 = 0; k0 < s; k0 += kKeys, slot ^= 1) {
+      wait_vmcnt<0>();
+      __syncthreads();
+      uint8_t* sk = smem + slot * (2 * L::BYTES) + tile * L::BYTES;
+      uint8_t* sv = sk + L::KB;
+      if (k0 + kKeys > s) {
+        L::zero_values(sv, tid & (kThreads - 1), s - k0 - first);
+        __syncthreads();
+      } else if (k0 + kKeys < s) {
+        copier.issue(k0 + kKeys + first, id, lds0 + (slot ^ 1) * (2 * L::BYTES));
+        copier.pages_at(prefix, k0 + 2 * kKeys + first, id);
+      }
+      const int h = way & 1, keys = k0 + 32 * way;
+      u32x4 kf[1][L::QS], vf[2][L::NDB], pf[2];
+      f32x16 sc[1];
+#pragma unroll
+      for (int st = 0; st < L::QS; ++st) kf[0][st] = L::key_chunk(sk, h, st, lane);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, 2 * h + st, db, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      rows.scores(kf, sc);
+      rows.softmax(sc, keys, lim, j.scale_log2, pf);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < L::NDB; ++db) rows.add(db, vf[st][db], pf[st]);
+    }
+
+    // this block's own keys
+    const int pmask = a.p.page_len - 1;
+    for (int k0 = s + 32 * way; k0 < e.held; k0 += kKeys) {
+      const int p0 = own_keys.in_pool(tail.page(k0, own_keys.shift, own_keys.last_block));
+      const int p1 = own_keys.in_pool(tail.page(k0 + 16, own_keys.shift, own_keys.last_block));
+      const int kr = L::key_of(fr);
+      const uint8_t* ks = own_keys.K + (kr < 16 ? p0 : p1) * own_keys.page_bytes + ((k0 + kr) & pmask) * L::RB;
+      u32x4 kf[1][L::QS], vf[2][L::NDB], pf[2];
+      f32x16 sc[1];
+#pragma unroll
+      for (int st = 0; st < L::QS; ++st) kf[0][st] = *reinterpret_cast<const u32x4*>(ks + (2 * st + f) * 16);
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const uint8_t* vs = own_keys.V + (st ? p1 : p0) * own_keys.page_bytes + ((k0 + 16 * st + 8 * f) & pmask) * 2;
+        const int left = e.held - (k0 + 16 * st + 8 * f);
+#pragma unroll
+        for (int db = 0; db < L::NDB; ++db)
+          vf[st][db] = *reinterpret_cast<const u32x4*>(vs + size_t(32 * db + fr) * (a.p.page_len * 2));
+        if (k0 + 32 > e.held) {   // values past the last key: whatever they are, times 0
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t keep = left > 2 * c + 1 ? ~0u : left > 2 * c ? 0xffffu : 0u;
+#pragma unroll
+            for (int db = 0; db < L::NDB; ++db) vf[st][db][c] &= keep;
+          }
+        }
+      }
+      rows.scores(kf, sc);
+      rows.softmax(sc, k0, limit, j.scale_log2, pf);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < L::NDB; ++db) rows.add(db, vf[st][db], pf[st]);
+    }
+
+    // join the ways, two dim blocks at a time: way v sums 8 of a lane's 32 elements
+    const float lsum = pair_sum(rows.l);
+    float* xs = reinterpret_cast<float*>(smem) + block * (kWays * STATE * kWave) + lane;
+    bf16_t* out = static_cast<bf16_t*>(a.out.p) + b * a.out.seq + i * a.out.row + (head * j.group + g) * a.out.head;
+    const bool live = own && r0 + fr < per && i < e.rows;
+#pragma unroll
+    for (int d2 = 0; d2 < L::NDB; d2 += 2) {
+      __syncthreads();   // the ring, or the last two blocks, have been read
+#pragma unroll
+      for (int c = 0; c < 32; ++c) xs[(way * STATE + c) * kWave] = rows.o[d2 + (c >> 4)][c & 15];
+      xs[(way * STATE + 32) * kWave] = rows.m;
+      xs[(way * STATE + 33) * kWave] = lsum;
+      __syncthreads();
+      float wt[kWays], top = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int v = 0; v < kWays; ++v) {
+        wt[v] = xs[(v * STATE + 32) * kWave];
+        top = fmaxf(top, wt[v]);
+      }
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int v = 0; v < kWays; ++v) {
+        wt[v] = __builtin_amdgcn_exp2f(wt[v] - ref);
+        l += xs[(v * STATE + 33) * kWave] * wt[v];
+      }
+      const float inv = 1.f / l;
+#pragma unroll
+      for (int c = 0; c < 8; c += 4) {
+        const int c0 = 8 * way + c;   // element c0 % 16 of block d2 + c0 / 16
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < kWays; ++v)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) y[u] += xs[(v * STATE + c0 + u) * kWave] * wt[v];
+        if (live) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            store_f(out + 32 * (d2 + (c0 >> 4)) + 2 * (c0 & 15) + 4 * f + u, limit > 0 ? y[u] * inv : 0.f);
+        }
+      }
+    }
+  }
+};
+
+template <int HD>
+__global__ __launch_bounds__(Pairs<HD>::kPairThreads, 2) void pairs_kernel(Job j) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[Pairs<HD>::SMEM];
+  Pairs<HD>::run(j, blockIdx.x, smem);
+}
 
 // ---------------------------------------------------------------- launch
 
@@ -864,6 +1086,22 @@ size_t paged_attention_workspace_upto(const dllm_kv_pages& p, int n, int max_row
   return size_t(2 * std::min(kMaxRanges * R, each + R)) * record(p.head_dim) * sizeof(float);
 }
 
+namespace {
+
+// Blocks of 32 rows in pairs (see Pairs)?  For bf16 batches over a shared
+// prefix whose entries fill whole blocks, or nearly, and whose pairs fill most
+// of the chip by themselves.  A prefix tile is copied for 64 rows there and for
+// 128 wide ones, which wins where the prefix is long (16 x 32 rows, 32 heads:
+// 22 us against 32 over 1024 positions, 32 against 40 over 2048, 385 against
+// 320 over 30000).
+bool pairs_up(const PagedAttn& a, int rows, int kv_heads, int64_t shared) {
+  if (a.p.dtype != DLLM_BF16 || rows < 24 || shared > 4096) return false;
+  const int blocks = cdiv(rows, 32);
+  return blocks * 32 * 3 <= rows * 4 && int64_t(a.n) * blocks * kv_heads >= 3 * kCus / 2;
+}
+
+}  // namespace
+
 hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   Job j{};
   j.a = a;
@@ -876,6 +1114,13 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
   const int mode_t = mode_of(dt, rows_t, a.n, kvh);
   j.stacked = shared > 0 && stacks(a, mode_t, rows_t, std::max(keys, shared));
+  if (j.stacked && pairs_up(a, rows_t, kvh, shared)) {
+    j.direct = true;
+    const int grid = blocks_of(kvh, cdiv(a.n * cdiv(rows_t, 32), 2));
+    if (a.p.head_dim == 128) hipLaunchKernelGGL(pairs_kernel<128>, dim3(grid), dim3(Pairs<128>::kPairThreads), 0, s, j);
+    else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
+    return hipGetLastError();
+  }
   const int mode_p = j.stacked ? mode_of(dt, rows_p, 1, kvh) : mode_t;
   j.prefix = j.stacked ? plan_part(mode_p, rows_p, 1, kvh, shared) : Part{1, 0, kTile};
   if (shared == 0) j.a.shared_len = j.a.prefix_seq = 0;

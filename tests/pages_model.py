@@ -100,17 +100,18 @@ def attend(q, keys, values, counts, causal, scale):
     n, rows, heads, hd = q.shape
     out, mass, size = np.zeros(q.shape), np.zeros(q.shape), np.zeros((n, rows, heads, 1))
     for b in range(n):
-        m = keys[b].shape[0]
-        for i in range(counts[b]):
-            lim = max(0, min(m, m - counts[b] + i + 1)) if causal else m
-            if lim == 0:
-                continue
-            for h in range(heads):
-                kv = h // (heads // keys[b].shape[1])
-                k, v = keys[b][:lim, kv], values[b][:lim, kv]
-                z = k @ q[b, i, h] * scale
-                w = np.exp(z - z.max())
-                w /= w.sum()
-                out[b, i, h], mass[b, i, h] = w @ v, w @ np.abs(v)
-                size[b, i, h] = (np.abs(k) @ np.abs(q[b, i, h])).max() * scale
+        m, c = keys[b].shape[0], counts[b]
+        lim = np.array([max(0, min(m, m - c + i + 1)) if causal else m for i in range(c)], dtype=int)
+        if m == 0 or c == 0:
+            continue
+        seen = np.arange(m)[None] < lim[:, None]
+        for h in range(heads):
+            kv = h // (heads // keys[b].shape[1])
+            k, v = keys[b][:, kv], values[b][:, kv]
+            z = np.where(seen, q[b, :c, h] @ k.T * scale, -np.inf)
+            top = np.where(lim[:, None] > 0, z.max(1, keepdims=True), 0.0)
+            w = np.exp(z - top)
+            w /= np.maximum(w.sum(1, keepdims=True), 1e-300)
+            out[b, :c, h], mass[b, :c, h] = w @ v, w @ np.abs(v)
+            size[b, :c, h, 0] = np.where(seen, np.abs(q[b, :c, h]) @ np.abs(k).T, 0).max(1) * scale
     return out, mass, size

@@ -356,6 +356,23 @@ def test_attention_over_a_shared_prefix(dtype, hd, page, heads, kv, rows, prefix
                     causal, shared_len=prefix, **kw)
 
 
+@pytest.mark.parametrize("hd,page,n,rows,prefix,lens,counts", [
+    (64, 64, 12, 32, 192, [224], None),                               # whole steps, equal branches
+    (128, 16, 13, 25, 173, [198, 160, 0, 339], None),                 # an odd count of blocks, one ends inside the prefix
+    (64, 128, 7, 61, 256, [317, 280, 600], [61, 0, 17]),              # two blocks an entry, nothing behind the prefix's pages in some
+    (128, 32, 12, 24, 31, [55, 31, 90], [24, 5, 23]),                 # no whole page is shared
+])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_of_many_branches(hd, page, n, rows, prefix, lens, counts, causal):
+    """Enough blocks of rows to fill the chip: 32 heads, entries of about whole blocks."""
+    lens = [lens[i % len(lens)] for i in range(n)]
+    kp = shared_batch(torch.bfloat16, hd, page, 32, prefix, lens)
+    poison(kp)
+    q = queries(n, rows, 32, hd, torch.bfloat16)
+    check_attention(kp, 1, list(range(1, n + 1)), q, None if counts is None else [counts[i % len(counts)] for i in range(n)],
+                    causal, prefix_seq=0, shared_len=prefix, max_len=max(lens))
+
+
 def test_attention_extremes():
     """Scores far apart, infinities among the values, keys that are not numbers in one sequence alone."""
     kp = hold(new_pages(seqs=4, pages=60, blocks=20), [300, 200, 290, 17])
