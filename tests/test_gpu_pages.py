@@ -373,6 +373,21 @@ def test_attention_of_many_branches(hd, page, n, rows, prefix, lens, counts, cau
                     causal, prefix_seq=0, shared_len=prefix, max_len=max(lens))
 
 
+@pytest.mark.parametrize("hd,page,heads,kv,n,rows,prefix,lens,causal", [
+    (64, 64, 32, 32, 3, 50, 16400, [16450, 16433, 16600], False),     # stacked rows end inside a row tile
+    (128, 128, 64, 8, 5, 26, 16500, [16526, 16700, 16550, 16390, 0], True),   # grouped heads, one entry inside the prefix, one empty
+    (64, 256, 16, 4, 1, 300, 0, [65800], True),                       # one sequence, nothing shared
+])
+def test_attention_of_heavy_batches(hd, page, heads, kv, n, rows, prefix, lens, causal):
+    """Many rows over many keys: 256 rows a workgroup, ranges of the keys joined."""
+    kp = shared_batch(torch.bfloat16, hd, page, kv, prefix, lens) if prefix else hold(
+        new_pages(pages=lens[0] // page + 3, heads=kv, page=page, hd=hd, seqs=1, blocks=-(-lens[0] // page)), lens)
+    poison(kp)
+    q = queries(n, rows, heads, hd, torch.bfloat16)
+    check_attention(kp, 0, list(range(1, n + 1)) if prefix else [0], q, [rows, 3, rows - 1, rows, 1][:n], causal, prefix_seq=0,
+                    shared_len=prefix, max_len=max(lens))
+
+
 def test_attention_extremes():
     """Scores far apart, infinities among the values, keys that are not numbers in one sequence alone."""
     kp = hold(new_pages(seqs=4, pages=60, blocks=20), [300, 200, 290, 17])
