@@ -1030,10 +1030,14 @@ constexpr int kStep = kWaves * kTile;   // keys that a narrow workgroup takes at
 // of unlike lengths come out even; a join costs about as much as 6 steps, so
 // shorter parts are not divided.  Wide ones take one workgroup a CU, which
 // leaves the other slot to the tails, and two where ranges stay long enough for
-// the second to gain more than its records cost to join.  256 rows take the
+// the second to gain more than its records cost to join; beside tails that
+// take `beside_us` by themselves, only as many as end by then (14 us and 1.2 us
+// a tile: 64 single tokens over 8000 shared positions and up to 1500 of their
+// own, 16 ranges 60 us, 8 ranges 49).  256 rows take the
 // count with the least time: rounds of a workgroup a CU, 8 us and 1.2 us a
 // tile each, and the records at 4 TB/s.
-Part plan_part(int dtype, int hd, int mode, int rows, int64_t groups, int kv_heads, int64_t keys) {
+Part plan_part(int dtype, int hd, int mode, int rows, int64_t groups, int kv_heads, int64_t keys,
+               double beside_us = 0.0) {
   Part p;
   p.row_tiles = cdiv(rows, rows_of(mode));
   const int64_t tiles = (keys + kTile - 1) / kTile, items = p.row_tiles * groups * kv_heads;
@@ -1051,8 +1055,10 @@ Part plan_part(int dtype, int hd, int mode, int rows, int64_t groups, int kv_hea
         ranges = r;
       }
     }
-  } else if (mode == ROWS128) ranges = tiles >= 24 * fill(kCus) ? fill(2 * kCus) : fill(kCus);
-  else ranges = keys <= 6 * kStep ? 1 : std::max(fill(2 * kCus), tiles / 24);
+  } else if (mode == ROWS128) {
+    ranges = tiles >= 24 * fill(kCus) ? fill(2 * kCus) : fill(kCus);
+    if (beside_us > 16.0) ranges = std::min(ranges, int64_t(1.2 * double(tiles) / (beside_us - 14.0)) + 1);
+  } else ranges = keys <= 6 * kStep ? 1 : std::max(fill(2 * kCus), tiles / 24);
   ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most, tiles / 4}));
   p.range = int(std::max<int64_t>(1, (tiles + ranges - 1) / ranges)) * kTile;
   p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
@@ -1167,7 +1173,10 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   if (mode_t == ROWS256) mode_p = ROWS256;
   if (mode_p == ROWS256 && mode_t == ROWS128) rows_t > 128 ? mode_t = ROWS256 : mode_p = ROWS128;
   const int hd = a.p.head_dim;
-  j.prefix = j.stacked ? plan_part(dt, hd, mode_p, rows_p, 1, kvh, shared) : Part{1, 0, kTile};
+  // streaming the tails at 5 TB/s, if on average they are half as long as the longest
+  const double tail_us = double(a.n) * cdiv(rows_t, rows_of(mode_t)) * kvh * double(std::max<int64_t>(0, keys - shared)) *
+                         hd * (dt == DLLM_BF16 ? 2 : 4) / 5e6;
+  j.prefix = j.stacked ? plan_part(dt, hd, mode_p, rows_p, 1, kvh, shared, tail_us) : Part{1, 0, kTile};
   if (shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
   j.tail = plan_part(dt, hd, mode_t, rows_t, a.n, kvh, j.stacked ? std::max<int64_t>(1, keys - shared) : keys);
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
