@@ -294,12 +294,10 @@ def _scratch(pages: KvPages, ws):
 
 
 def _page_stream(pages: KvPages, stream):
-    if stream is not None:
-        return _stream(stream)
     dev = torch.cuda.current_device()
-    if dev != pages._index:
-        raise ValueError("the pages are on another device than the current one")
-    return _raw_stream(dev)
+    if dev != pages._index or (isinstance(stream, torch.cuda.Stream) and stream.device_index != dev):
+        raise ValueError("the pages are on another device than the current one or the stream")
+    return _raw_stream(dev) if stream is None else _stream(stream)
 
 
 def kv_pages_init(pages: KvPages, stream=None):

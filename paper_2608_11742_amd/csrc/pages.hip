@@ -3,14 +3,14 @@
 //
 // A call that changes tables is planned by one workgroup of 1024 threads: it
 // checks the sequences (thread i: entry i), sums the pages they need, and
-// walks the reference counts with one contiguous run of page ids per thread,
-// so that one scan over the threads' free counts gives every free page its
-// rank in id order; the page of rank r goes to the entry whose range of needs
-// holds r.  The check comes before any store: a call that fails changes
-// nothing.  What moves pages or many table entries is done by a second,
-// chip-wide launch that reads the plan.  At 10 000 pages (280 GB of the
-// 8B-class shape's) a plan reads 40 KB and is bound by the latency of its
-// scans, the second launch by memory.
+// counts the free pages with one contiguous run of page ids per wave, 64 at a
+// time by ballot, so that a free page's rank in id order is the counts before
+// its wave's run plus the bits before it; the page of rank r goes to the entry
+// whose range of needs holds r.  The check comes before any store: a call that
+// fails changes nothing.  What moves pages or many table entries is done by a
+// second, chip-wide launch that reads the plan.  A plan is bound by the latency
+// of three dependent loads and two scans (4 us up to 8192 pages, 280 GB of the
+// 8B-class shape's; 8 us at 32768, 150 at 2^20), the second launch by memory.
 #include <algorithm>
 
 #include "common.h"
@@ -81,47 +81,106 @@ __device__ __forceinline__ int plan_error(int err, PlanShared& sh) {
 
 __device__ __forceinline__ int blocks_of(int positions, int page_len) { return (positions + page_len - 1) / page_len; }
 
-// this thread's run of page ids, and the free ones among them
+// positions a sequence holds, inside its table
+__device__ __forceinline__ int held_of(const dllm_kv_pages& p, int s) {
+  return min(max(p.len[s], 0), p.max_blocks * p.page_len);
+}
+
+// this wave's run of page ids
 struct Run {
-  int lo, hi, n_free;
+  int lo, hi;
 };
-__device__ __forceinline__ Run count_free(const dllm_kv_pages& p) {
-  const int run = (p.n_pages + kPlanThreads - 1) / kPlanThreads;
-  Run r;
-  r.lo = min(int(threadIdx.x) * run, p.n_pages);
-  r.hi = min(r.lo + run, p.n_pages);
-  r.n_free = 0;
-  for (int i = r.lo; i < r.hi; ++i) r.n_free += p.refs[i] <= 0;
-  return r;
+__device__ __forceinline__ Run run_of(const dllm_kv_pages& p) {
+  const int ids = (p.n_pages + kPlanThreads - 1) / kPlanThreads * kWave;
+  const int lo = min(__builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6) * ids, p.n_pages);
+  return Run{lo, min(lo + ids, p.n_pages)};
+}
+// f(first id, bits of the used ones) for every 64 ids of a run, the counts of
+// 512 on their way together; ids past the run are neither used nor free.  f
+// returns whether to go on.
+template <class F>
+__device__ __forceinline__ void for_ids(const dllm_kv_pages& p, Run r, F&& f) {
+  constexpr int kBatch = 8;
+  const int lane = threadIdx.x & 63;
+  for (int i0 = r.lo; i0 < r.hi; i0 += kBatch * kWave) {
+    int refs[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) refs[u] = p.refs[min(i0 + u * kWave + lane, p.n_pages - 1)];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int i = i0 + u * kWave;
+      if (i >= r.hi || !f(i, __ballot(refs[u] > 0))) return;
+    }
+  }
+}
+// bits of the ids i .. i + 63 that lie in lo .. hi - 1
+__device__ __forceinline__ uint64_t inside(int i, int lo, int hi) {
+  const int a = min(max(lo - i, 0), 64), b = min(max(hi - i, 0), 64);
+  const uint64_t below_b = b == 64 ? ~uint64_t(0) : (uint64_t(1) << b) - 1;
+  return a == 64 ? 0 : below_b & ~((uint64_t(1) << a) - 1);
+}
+// bits below this lane's
+__device__ __forceinline__ int bits_before(uint64_t m) {
+  return __popcll(m & ((uint64_t(1) << (threadIdx.x & 63)) - 1));
+}
+__device__ __forceinline__ int count_free(const dllm_kv_pages& p, Run r) {
+  int n = 0;
+  for_ids(p, r, [&](int i, uint64_t used) {
+    n += __popcll(inside(i, r.lo, r.hi) & ~used);
+    return true;
+  });
+  return n;
+}
+
+// sum of the waves' counts, and of those before this wave
+__device__ __forceinline__ int wave_scan(int n, PlanShared& sh, int& total) {
+  const int wave = threadIdx.x >> 6;
+  __syncthreads();   // earlier sums have been read
+  if ((threadIdx.x & 63) == 0) sh.wave_sum[wave] = n;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const int t = sh.wave_sum[w];
+    before += w < wave ? t : 0;
+    total += t;
+  }
+  return __builtin_amdgcn_readfirstlane(before);
 }
 
 // Pages for the plan's entries: entry i (this thread's) needs `need` pages as
-// blocks first .. of sequence seq.  False (and nothing stored) if the pool has
-// fewer free ones.
-__device__ __forceinline__ bool take_pages(const dllm_kv_pages& p, PlanShared& sh, const Run& run, int seq, int first,
-                                           int need) {
+// blocks first .. of sequence seq; n_free: the free pages of this wave's run.
+// False (and nothing stored) if the pool has fewer free ones.
+__device__ __forceinline__ bool take_pages(const dllm_kv_pages& p, PlanShared& sh, Run run, int n_free, int seq,
+                                           int first, int need) {
   const int tid = threadIdx.x;
   int total, have;
   const int off = block_scan(need, sh, total);
   sh.off[tid] = off;
   sh.first[tid] = first;
   sh.seq[tid] = seq;
-  int rank = block_scan(run.n_free, sh, have);   // its barriers publish off, first and seq too
+  int rank0 = wave_scan(n_free, sh, have);   // its barriers publish off, first and seq too
   if (total > have) return false;
-  if (run.n_free == 0 || rank >= total) return true;
-  for (int i = run.lo; i < run.hi && rank < total; ++i) {
-    if (p.refs[i] > 0) continue;
-    // the last entry whose needs start at or before this rank (entries that need nothing share their start with the next)
-    int a = 0, b = kPlanThreads;
-    while (b - a > 1) {
-      const int m = (a + b) >> 1;
-      if (sh.off[m] <= rank) a = m;
-      else b = m;
+  if (n_free == 0 || rank0 >= total) return true;
+  for_ids(p, run, [&](int i0, uint64_t used) {
+    const uint64_t free = inside(i0, run.lo, run.hi) & ~used;
+    const int rank = rank0 + bits_before(free);
+    rank0 += __popcll(free);
+    if ((free >> (tid & 63) & 1) && rank < total) {
+      // the last entry whose needs start at or before this rank (entries that need nothing share their start with the next)
+      int a = 0, b = kPlanThreads;
+      while (b - a > 1) {
+        const int m = (a + b) >> 1;
+        if (sh.off[m] <= rank) a = m;
+        else b = m;
+      }
+      const int page = i0 + (tid & 63);
+      p.table[size_t(sh.seq[a]) * p.max_blocks + sh.first[a] + rank - sh.off[a]] = page;
+      p.refs[page] = 1;
     }
-    p.table[size_t(sh.seq[a]) * p.max_blocks + sh.first[a] + rank - sh.off[a]] = i;
-    p.refs[i] = 1;
-    ++rank;
-  }
+    return rank0 < total;
+  });
   return true;
 }
 
@@ -140,19 +199,20 @@ __global__ __launch_bounds__(kPlanThreads) void pages_grow_kernel(dllm_kv_pages 
   const int tid = threadIdx.x;
   int err = kNoError, s = -1, held = 0, more = 0;
   const int want_s = tid < n ? seqs[tid] : 0, want_a = tid < n ? add[tid] : 0;
-  const Run run = count_free(p);   // with the lists on their way
+  const Run run = run_of(p);
+  const int n_free = count_free(p, run);   // with the lists on their way
   plan_begin(sh);
   if (tid < n) {
     s = check_seq(p, want_s, sh, err);
     more = want_a;
-    if (s >= 0) held = p.len[s];
+    if (s >= 0) held = held_of(p, s);
     if (err == kNoError && (more < 0 || int64_t(held) + more > int64_t(p.max_blocks) * p.page_len)) err = KV_PAGES_ELEN;
   }
   err = plan_error(err, sh);
   if (err == kNoError) {
     const int first = blocks_of(held, p.page_len);
     const int need = tid < n ? blocks_of(held + more, p.page_len) - first : 0;
-    if (!take_pages(p, sh, run, s, first, need)) err = KV_PAGES_EFULL;
+    if (!take_pages(p, sh, run, n_free, s, first, need)) err = KV_PAGES_EFULL;
     else if (tid < n) p.len[s] = held + more;
   }
   if (tid == 0) *status = err == kNoError ? KV_PAGES_OK : err;
@@ -168,13 +228,14 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(dllm_kv_pages 
   const int tid = threadIdx.x;
   int err = kNoError, d = -1, m = 0;
   const int from = tid < n ? src[tid] : 0, to = tid < n ? dst[tid] : 0, cut = keep && tid < n ? keep[tid] : 0;
-  const Run run = count_free(p);
+  const Run run = run_of(p);
+  const int n_free = count_free(p, run);
   plan_begin(sh);
   if (tid < n) {
     d = check_seq(p, to, sh, err);
     if (from < 0 || from >= p.max_seqs || (d >= 0 && p.len[d] != 0)) err = KV_PAGES_ESEQ;
     if (err == kNoError) {
-      const int held = p.len[from];
+      const int held = held_of(p, from);
       m = keep ? cut : held;
       if (m < 0 || m > held) err = KV_PAGES_ELEN;
     }
@@ -182,7 +243,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(dllm_kv_pages 
   err = plan_error(err, sh);   // every length has been read before one is stored
   if (err == kNoError) {
     const int need = tid < n && m % p.page_len ? 1 : 0;
-    if (!take_pages(p, sh, run, d, m / p.page_len, need)) err = KV_PAGES_EFULL;
+    if (!take_pages(p, sh, run, n_free, d, m / p.page_len, need)) err = KV_PAGES_EFULL;
     else if (tid < n) p.len[d] = m;
   }
   if (tid == 0) *status = err == kNoError ? KV_PAGES_OK : err;
@@ -260,7 +321,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_free_kernel(dllm_kv_pages 
     s = check_seq(p, want, sh, err);
     m = keep ? cut : 0;
     if (err == kNoError) {
-      const int held = p.len[s];
+      const int held = held_of(p, s);
       if (m < 0 || m > held) {
         err = KV_PAGES_ELEN;
       } else if (m < held && m % p.page_len) {
@@ -305,23 +366,37 @@ __host__ __device__ CompactPlan compact_plan(void* ws, int n_pages) {
 
 __global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(dllm_kv_pages p, int32_t* n_used, CompactPlan c) {
   __shared__ PlanShared sh;
-  const int tid = threadIdx.x;
-  const int run = (p.n_pages + kPlanThreads - 1) / kPlanThreads;
-  const int lo = min(tid * run, p.n_pages), hi = min(lo + run, p.n_pages);
-  int used = 0, total, holes, moved;
-  for (int i = lo; i < hi; ++i) used += p.refs[i] > 0;
-  block_scan(used, sh, total);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const Run run = run_of(p);
+  int total, holes, moved;
+  int h = count_free(p, run), m = run.hi - run.lo - h;
+  wave_scan(m, sh, total);
   // below `total` free ids are filled, from there on used ones move
-  const int mid = min(max(total, lo), hi);
-  int n_hole = 0, n_move = 0;
-  for (int i = lo; i < mid; ++i) n_hole += p.refs[i] <= 0;
-  for (int i = mid; i < hi; ++i) n_move += p.refs[i] > 0;
-  int h = block_scan(n_hole, sh, holes), m = block_scan(n_move, sh, moved);
-  for (int i = lo; i < mid; ++i)
-    if (p.refs[i] <= 0) c.to[h++] = i;
-  for (int i = mid; i < hi; ++i)
-    if (p.refs[i] > 0) c.from[m++] = i;
-  __syncthreads();   // as many holes below as used pages past them: moved == holes
+  const int mid = min(max(total, run.lo), run.hi);
+  h = m = 0;
+  for_ids(p, run, [&](int i, uint64_t used) {
+    h += __popcll(inside(i, run.lo, mid) & ~used);
+    m += __popcll(inside(i, mid, run.hi) & used);
+    return true;
+  });
+  h = wave_scan(h, sh, holes);
+  m = wave_scan(m, sh, moved);   // as many holes below as used pages past them
+  if (moved == 0) {   // nothing to list
+    if (tid == 0) {
+      *n_used = total;
+      *c.moved = 0;
+    }
+    return;
+  }
+  for_ids(p, run, [&](int i, uint64_t used) {
+    const uint64_t hole = inside(i, run.lo, mid) & ~used, move = inside(i, mid, run.hi) & used;
+    if (hole >> lane & 1) c.to[h + bits_before(hole)] = i + lane;
+    if (move >> lane & 1) c.from[m + bits_before(move)] = i + lane;
+    h += __popcll(hole);
+    m += __popcll(move);
+    return true;
+  });
+  __syncthreads();
   for (int r = tid; r < moved; r += kPlanThreads) {
     const int a = c.from[r], b = c.to[r];
     c.new_id[a] = b;
