@@ -592,32 +592,43 @@ struct Rows32 {
         for (int i = 0; i < 16; ++i)
           if (k0 + 32 * h + 16 * (i >> 3) + 8 * f + (i & 7) >= lim) sc[h][i] = -INFINITY;
     }
-    float top = -INFINITY;
+    // With the reference as it is, unless a weight would pass what binary16 holds
+    // (or there is none yet): no lane's 16 H weights sum up to more than 2^13.
+    // Their maximum is only looked for where it has to move.
+    float sum = weights(sc, scale_log2, m, pf);
+    if (!__all(sum <= 8192.f)) {
+      float top = -INFINITY;
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[h][i]);
-    top = pair_max(top) * scale_log2;
-    const float mn = top > m + 8.f ? top : m;
-    const float ref = mn == -INFINITY ? 0.f : mn;
-    if (__any(mn != m)) {
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[h][i]);
+      top = pair_max(top) * scale_log2;
+      const float mn = top > m + 8.f ? top : m;
+      const float ref = mn == -INFINITY ? 0.f : mn;   // no key seen yet: weights 2^-inf
       const float alpha = __builtin_amdgcn_exp2f(m - ref);
       l *= alpha;
 #pragma unroll
       for (int db = 0; db < L::NDB; ++db) o[db] *= alpha;
+      m = mn;
+      sum = weights(sc, scale_log2, ref, pf);
     }
-    m = mn;
+    l += sum;
+  }
+  // 2^(score - ref) in binary16, and their sum as rounded
+  template <int H>
+  __device__ __forceinline__ static float weights(const f32x16 (&sc)[H], float scale_log2, float ref, u32x4 (&pf)[2 * H]) {
+    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
     float sum = 0.f;
 #pragma unroll
     for (int h = 0; h < H; ++h)
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(sc[h][i], scale_log2, -ref));
-        const float y = __builtin_amdgcn_exp2f(fmaf(sc[h][i + 1], scale_log2, -ref));
-        sum += x + y;
-        pf[2 * h + (i >> 3)][(i & 7) >> 1] = pack_f16x2(x, y);
+        const uint32_t xy = pack_f16x2(__builtin_amdgcn_exp2f(fmaf(sc[h][i], scale_log2, -ref)),
+                                       __builtin_amdgcn_exp2f(fmaf(sc[h][i + 1], scale_log2, -ref)));
+        sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, xy), half2v{1, 1}, sum, false);
+        pf[2 * h + (i >> 3)][(i & 7) >> 1] = xy;
       }
-    l += sum;
+    return sum;
   }
   __device__ __forceinline__ void add(int db, u32x4 vf, u32x4 pf) {
     o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vf), __builtin_bit_cast(half8, pf), o[db],
