@@ -243,7 +243,7 @@ class KvPages:
             raise ValueError("the arrays must be contiguous tensors of one device")
         self.k, self.vt, self.refs, self.table, self.len = k, vt, refs, table, len
         self.page_len, self.head_dim, self.n_kv_heads, self.dtype = page_len, hd, heads, k.dtype
-        self._index, self._scale = k.get_device(), hd ** -0.5
+        self.device, self._index, self._scale = k.device, k.get_device(), hd ** -0.5
         self._c = _abi.KvPagesC(k.data_ptr(), vt.data_ptr(), refs.data_ptr(), table.data_ptr(), len.data_ptr(), L,
                                 n_pages, heads, hd, page_len, table.shape[0], table.shape[1],
                                 DLLM_BF16 if k.dtype == torch.bfloat16 else DLLM_F32)
@@ -262,7 +262,9 @@ class KvPages:
         return pages
 
 
-_I32 = torch.int32
+_I32, _Rows = torch.int32, _abi.Rows
+# of a process that has tensors on a device: without the check for a first use
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _ids(pages: KvPages, t, n: int):
@@ -274,16 +276,13 @@ def _ids(pages: KvPages, t, n: int):
     return t.data_ptr()
 
 
-def _rows(pages: KvPages, t, name: str):
-    """t [entries, rows, heads, head_dim], any strides over contiguous head_dim, as dllm_rows."""
-    n, rows, heads, hd = t.shape
+def _rows(pages: KvPages, t, n: int, rows: int, heads: int, name: str):
+    """t [n, rows, heads, head_dim], any strides over contiguous head_dim, as dllm_rows."""
     seq, row, head, one = t.stride()
-    if hd != pages.head_dim or one != 1:
-        raise ValueError(f"{name} must be [entries, rows, heads, {pages.head_dim}] with contiguous rows")
-    if t.dtype is not pages.dtype or t.get_device() != pages._index:
-        raise ValueError(f"{name} must have the type and device of the pages' keys")
+    if one != 1 or t.dtype is not pages.dtype or t.get_device() != pages._index:
+        raise ValueError(f"{name} must have contiguous rows, and the type and device of the pages' keys")
     # a dimension of one has no stride to speak of
-    return _abi.Rows(t.data_ptr(), seq if n > 1 else 0, row if rows > 1 else 0, head if heads > 1 else 0)
+    return _Rows(t.data_ptr(), seq if n > 1 else 0, row if rows > 1 else 0, head if heads > 1 else 0)
 
 
 def _scratch(pages: KvPages, ws):
@@ -294,10 +293,14 @@ def _scratch(pages: KvPages, ws):
 
 
 def _page_stream(pages: KvPages, stream):
-    dev = torch.cuda.current_device()
-    if dev != pages._index or (isinstance(stream, torch.cuda.Stream) and stream.device_index != dev):
-        raise ValueError("the pages are on another device than the current one or the stream")
-    return _raw_stream(dev) if stream is None else _stream(stream)
+    dev = _current_device()
+    if dev != pages._index:
+        raise ValueError("the pages are on another device than the current one")
+    if stream is None:
+        return _raw_stream(dev)
+    if isinstance(stream, torch.cuda.Stream) and stream.device_index != dev:
+        raise ValueError("the stream is of another device than the pages")
+    return _stream(stream)
 
 
 def kv_pages_init(pages: KvPages, stream=None):
@@ -337,11 +340,12 @@ def kv_pages_compact(pages: KvPages, n_used, ws, stream=None):
 
 def kv_pages_write(pages: KvPages, layer: int, seqs, k, v, n_rows=None, stream=None):
     """k, v [entries, rows, kv heads, head_dim]: the last n_rows[b] (or all rows) positions of sequence seqs[b]."""
-    n, rows, heads, _ = k.shape
-    if v.shape != k.shape or heads != pages.n_kv_heads:
-        raise ValueError("k and v need the pages' heads and the same shape")
+    n, rows, heads, hd = shape = k.shape
+    if v.shape != shape or heads != pages.n_kv_heads or hd != pages.head_dim:
+        raise ValueError("k and v need the pages' heads and head_dim and the same shape")
     _check(lib().kv_pages_write(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n),
-                                _rows(pages, k, "k"), _rows(pages, v, "v"), _page_stream(pages, stream)))
+                                _rows(pages, k, n, rows, heads, "k"), _rows(pages, v, n, rows, heads, "v"),
+                                _page_stream(pages, stream)))
 
 
 def kv_pages_attention_workspace_bytes(pages: KvPages, n: int, max_rows: int, n_heads: int) -> int:
@@ -354,13 +358,14 @@ def kv_pages_attention(pages: KvPages, layer: int, seqs, q, out, ws, n_rows=None
     """q, out [entries, rows, heads, head_dim]; see kv_pages_attention in dllm_rps.h.
 
     max_len defaults to the tables' length, scale to 1 / sqrt(head_dim)."""
-    n, rows, heads, _ = shape = q.shape
-    if out.shape != shape:
-        raise ValueError("q and out need the same shape")
+    n, rows, heads, hd = shape = q.shape
+    if out.shape != shape or hd != pages.head_dim:
+        raise ValueError("q and out need the pages' head_dim and the same shape")
     if max_len is None:
         max_len = pages.table.shape[1] * pages.page_len
     _check(lib().kv_pages_attention(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n), heads,
-                                    _rows(pages, q, "q"), _rows(pages, out, "out"), prefix_seq,
+                                    _rows(pages, q, n, rows, heads, "q"),
+                                    _rows(pages, out, n, rows, heads, "out"), prefix_seq,
                                     shared_len, max_len, int(causal), pages._scale if scale is None else scale,
                                     *_scratch(pages, ws), _page_stream(pages, stream)))
 
