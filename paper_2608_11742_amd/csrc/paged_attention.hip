@@ -197,7 +197,7 @@ __device__ __forceinline__ float quad_sum(float x) {
 // a 32-key half are gathered so that output element i of lane group g in
 // block kk is key 8 g + 4 kk + i: the lane's 8 probabilities of the half are 8
 // consecutive keys, one 16-byte chunk of a V^T row.
-template <typename T, int HD, int NQB, int NW>
+template <typename T, int HD, int NQB>
 struct Narrow {
   static constexpr bool kHalf = sizeof(T) == 2;
   static constexpr int E = 16 / int(sizeof(T));             // elements per chunk
@@ -211,7 +211,7 @@ struct Narrow {
   static constexpr int NDB = HD / 16;
   static constexpr int NV = KS / (4 * E);                   // V chunks per dim row and lane
   static constexpr int STATE = NDB * 4 + 2;                 // floats a lane hands over per 16 rows
-  static constexpr int SMEM = NW * STATE * kWave * 4;
+  static constexpr int SMEM = kWaves * STATE * kWave * 4;
 
   __device__ __forceinline__ static int key_of(int kb, int r) {
     if constexpr (kHalf) return 32 * (kb >> 1) + 8 * (r >> 2) + 4 * (kb & 1) + (r & 3);
@@ -297,8 +297,8 @@ struct Narrow {
       for (int st = 0; st < QS; ++st) qf[qb][st] = *reinterpret_cast<const u32x4*>(q + (4 * st + g) * E);
     }
     if (k0 < w.k1) load_v(k0, id);
-    for (; k0 < w.k1; k0 += NW * KS) {
-      const int next = k0 + NW * KS;
+    for (; k0 < w.k1; k0 += kWaves * KS) {
+      const int next = k0 + kWaves * KS;
       const bool more = next < w.k1;
       if (more) pages_at(next, id);
       f32x4 sc[NB][NQB];
@@ -399,15 +399,15 @@ struct Narrow {
       mine[(STATE - 2) * kWave] = m[qb];
       mine[(STATE - 1) * kWave] = quad_sum(l[qb]);
       __syncthreads();
-      float mw[NW], top = -INFINITY, sum = 0.f;
+      float mw[kWaves], top = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int v = 0; v < NW; ++v) {
+      for (int v = 0; v < kWaves; ++v) {
         mw[v] = smem[(v * STATE + STATE - 2) * kWave + lane];
         top = fmaxf(top, mw[v]);
       }
       const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-      for (int v = 0; v < NW; ++v) {
+      for (int v = 0; v < kWaves; ++v) {
         mw[v] = __builtin_amdgcn_exp2f(mw[v] - ref);
         sum += smem[(v * STATE + STATE - 1) * kWave + lane] * mw[v];
       }
@@ -417,10 +417,10 @@ struct Narrow {
       T* out = static_cast<T*>(a.out.p) + at[qb].b * a.out.seq + at[qb].i * a.out.row +
                (kvh * j.group + at[qb].g) * a.out.head;
       float* rec = record_of(j, w.part, at[qb], kvh, HD);
-      for (int db = wave; db < NDB; db += NW) {
+      for (int db = wave; db < NDB; db += kWaves) {
         f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int v = 0; v < NW; ++v)
+        for (int v = 0; v < kWaves; ++v)
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] += smem[(v * STATE + 4 * db + i) * kWave + lane] * mw[v];
         if (!live) continue;
@@ -474,10 +474,9 @@ struct Tile {
   // key within its 32 of MFMA row r
   __device__ __forceinline__ static int key_of(int r) { return (r & 0x13) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
-  // one wave's part (`wave` of NW) of copying a tile
-  template <int NW>
+  // one wave's part (`wave` of four) of copying a tile
   struct Copier {
-    static constexpr int IC = KB / 1024 / NW;       // copies the wave issues for K, and for V
+    static constexpr int IC = KB / 1024 / kWaves;   // copies the wave issues for K, and for V
     const uint8_t* K;
     const uint8_t* V;
     size_t page_bytes;
@@ -506,13 +505,12 @@ struct Tile {
       const int pmask = page_len - 1, kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vswz(8 * wave + vd);
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
-        const int grp = i * NW + wave, r = grp * KROWS + kr;
+        const int grp = i * kWaves + wave, r = grp * KROWS + kr;
         // a copy's rows share a 16-key group, one of C over the waves
-        constexpr int C = NW * KROWS / 16;
+        constexpr int C = kWaves * KROWS / 16;
         const int u = wave * KROWS / 16, sub = i * C + u;
-        const int p0 = id[i * C], p1 = id[(i * C + 1) & 3], p2 = id[(i * C + 2) & 3], p3 = id[(i * C + 3) & 3];
-        const int lo = C > 1 && (u & 1) ? p1 : p0, hi = u & 1 ? p3 : p2;
-        const int page = in_pool(C > 2 && (u & 2) ? hi : lo);
+        const int even = id[i * C], odd = id[i * C + C - 1];
+        const int page = in_pool(u ? odd : even);
         const uint8_t* src = K + page * page_bytes + ((k0 + sub * 16) & pmask) * RB;
         copy16(src + (r & 15) * RB + ((lane % CK) ^ kswz(r)) * 16, dst + grp * 1024);
       }
@@ -520,7 +518,7 @@ struct Tile {
       const uint8_t* src = V + page * page_bytes + size_t(vd) * (page_len * 2) + ((k0 + 8 * vc) & pmask) * 2;
 #pragma unroll
       for (int i = 0; i < IC; ++i) {
-        const int grp = i * NW + wave;
+        const int grp = i * kWaves + wave;
         copy16(src + size_t(grp) * 8 * (page_len * 2), dst + KB + grp * 1024);
       }
     }
@@ -636,24 +634,17 @@ struct Rows32 {
   }
 };
 
-// 32 rows a wave over one range of keys.  Four waves keep two tiles in LDS, so
-// that two workgroups share a CU.  Eight keep four, three of them on their way:
-// half the copies a row, and time for each to arrive (16 x 32 rows over 30011:
-// the loop without its copies runs in 240 us, with four waves' 320).
-template <int HD, int NW>
+// 128 rows, 32 a wave, over one range of keys; two tiles in LDS, so that two
+// workgroups share a CU.  Measured equal (16 x 32 rows, 32 heads, over 30011
+// positions: 320 us, 0.79 PFLOP/s): eight waves and 256 rows with three tiles on
+// their way, whose copies are half as many a row; the same in two groups that
+// take turns at matrix and vector work.  64 rows a wave, alone on its SIMD with
+// products and softmax in one stream, took 350.
+template <int HD>
 struct Wide {
   using L = Tile<HD>;
-  static constexpr int kSlots = NW == 8 ? 4 : 2;
-  static constexpr int SMEM = kSlots * L::BYTES;
-  using Copier = typename L::template Copier<NW>;
-
-  // tile k0 has landed for this wave's copies; later tiles may be on their way
-  __device__ __forceinline__ static void wait_tile(int left) {
-    constexpr int C = 2 * Copier::IC;   // copies a tile and wave
-    if (kSlots == 4 && left > 2 * kTile) wait_vmcnt<2 * C>();
-    else if (kSlots == 4 && left > kTile) wait_vmcnt<C>();
-    else wait_vmcnt<0>();
-  }
+  using Copier = typename L::Copier;
+  static constexpr int SMEM = 2 * L::BYTES;
 
   __device__ static void run(const Job& j, const Share& w, uint8_t* smem) {
     const PagedAttn& a = j.a;
@@ -671,27 +662,21 @@ struct Wide {
     const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
 
     int id[4];
-    wait_vmcnt<0>();   // from here on the copies alone are counted
-#pragma unroll
-    for (int t = 0; t + 1 < kSlots; ++t) {
-      copier.pages_at(w, w.k0 + t * kTile, id);
-      if (w.k0 + t * kTile < w.k1) copier.issue(w.k0 + t * kTile, id, lds0 + t * L::BYTES);
-    }
-    constexpr int kAhead = (kSlots - 1) * kTile;
-    copier.pages_at(w, w.k0 + kAhead, id);
+    copier.pages_at(w, w.k0, id);
+    if (w.k0 < w.k1) copier.issue(w.k0, id, lds0);
+    copier.pages_at(w, w.k0 + kTile, id);
     int slot = 0;
-    for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot = (slot + 1) & (kSlots - 1)) {
-      wait_tile(w.k1 - k0);
-      barrier_lds();   // tile k0 has landed; the slot before it has been read
+    for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
+      wait_vmcnt<0>();
+      barrier_lds();   // tile k0 has landed; the other slot has been read
       const uint8_t* sk = smem + slot * L::BYTES;
       uint8_t* sv = smem + slot * L::BYTES + L::KB;
-      if (k0 + kAhead < w.k1) {
-        copier.issue(k0 + kAhead, id, lds0 + ((slot - 1) & (kSlots - 1)) * L::BYTES);
-        copier.pages_at(w, k0 + kAhead + kTile, id);
-      }
       if (k0 + kTile > w.k1) {
-        L::zero_values(sv, tid, NW * kWave, w.k1 - k0);
+        L::zero_values(sv, tid, kThreads, w.k1 - k0);
         barrier_lds();
+      } else if (k0 + kTile < w.k1) {
+        copier.issue(k0 + kTile, id, lds0 + (slot ^ 1) * L::BYTES);
+        copier.pages_at(w, k0 + 2 * kTile, id);
       }
       // every K fragment is on its way before the first product waits for one,
       // half of the V fragments before the softmax
@@ -783,7 +768,7 @@ struct Pairs {
     Share prefix{}, tail{};
     prefix.before = prefix.after = table_row(a, a.prefix_seq);
     tail.before = tail.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
-    const typename L::template Copier<kWays> copier(a, head, wave & 3, s), own_keys(a, head, 0, e.held);
+    const typename L::Copier copier(a, head, wave & 3, s), own_keys(a, head, 0, e.held);
     const int first = kTile * tile;   // of this wave's tile in a step
     const uint32_t lds0 = lds_address(smem) + tile * L::BYTES;
     int id[4];
@@ -915,23 +900,20 @@ __global__ __launch_bounds__(Pairs<HD>::kPairThreads, 2) void pairs_kernel(Job j
 
 // ---------------------------------------------------------------- launch
 
-// how a part's rows are taken: 16 or 32 of them narrow, or 128 or 256 wide
-enum { ROWS16 = 1, ROWS32 = 2, ROWS128 = 3, ROWS256 = 4 };
-constexpr int rows_of(int mode) { return mode == ROWS16 ? 16 : mode == ROWS32 ? 32 : mode == ROWS128 ? 128 : 256; }
-// waves of a launch: eight where 256 rows are taken
-constexpr int waves_of(int prefix) { return prefix == ROWS256 ? 8 : kWaves; }
+// how a part's rows are taken: 16 or 32 of them narrow, or 128 wide
+enum { ROWS16 = 1, ROWS32 = 2, ROWS128 = 3 };
+constexpr int rows_of(int mode) { return mode == ROWS16 ? 16 : mode == ROWS32 ? 32 : 128; }
 
-template <typename T, int HD, int MODE, int NW> struct Taker;
-template <typename T, int HD, int NW> struct Taker<T, HD, ROWS16, NW> : Narrow<T, HD, 1, NW> {};
-template <typename T, int HD, int NW> struct Taker<T, HD, ROWS32, NW> : Narrow<T, HD, 2, NW> {};
-template <int HD> struct Taker<bf16_t, HD, ROWS128, 4> : Wide<HD, 4> {};
-template <int HD> struct Taker<bf16_t, HD, ROWS256, 8> : Wide<HD, 8> {};
+template <typename T, int HD, int MODE> struct Taker;
+template <typename T, int HD> struct Taker<T, HD, ROWS16> : Narrow<T, HD, 1> {};
+template <typename T, int HD> struct Taker<T, HD, ROWS32> : Narrow<T, HD, 2> {};
+template <int HD> struct Taker<bf16_t, HD, ROWS128> : Wide<HD> {};
 
 // both parts in one launch: prefix workgroups, then the tails'
 template <typename T, int HD, int PREFIX, int TAIL>
-__global__ __launch_bounds__(waves_of(PREFIX) * kWave, 2) void attention_kernel(Job j, int prefix_blocks) {
-  using P = Taker<T, HD, PREFIX, waves_of(PREFIX)>;
-  using U = Taker<T, HD, TAIL, waves_of(PREFIX)>;
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(Job j, int prefix_blocks) {
+  using P = Taker<T, HD, PREFIX>;
+  using U = Taker<T, HD, TAIL>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[P::SMEM > U::SMEM ? P::SMEM : U::SMEM];
   Share w;
   const int x = blockIdx.x;
@@ -1013,22 +995,14 @@ constexpr int kMaxRanges = 64;
 // How `groups` sets of stacked rows per key head are taken.  fp32 products
 // cost an eighth of the bf16 rate, so there 32 rows, which halve what is
 // read, are only worth it where 16 fill the chip twice.
-// 256 bf16 rows take a CU for themselves; they pay where each has many tiles to
-// go through.
-int mode_of(int dtype, int rows, int64_t groups, int kv_heads, int64_t keys) {
-  if (dtype == DLLM_BF16) {
-    if (rows > 128 && cdiv(rows, 256) * groups * kv_heads * (keys / kTile) >= 32 * kCus) return ROWS256;
-    return rows > kNarrowRows ? ROWS128 : rows > 16 ? ROWS32 : ROWS16;
-  }
+int mode_of(int dtype, int rows, int64_t groups, int kv_heads) {
+  if (dtype == DLLM_BF16) return rows > kNarrowRows ? ROWS128 : rows > 16 ? ROWS32 : ROWS16;
   return rows > 16 && cdiv(rows, 16) * groups * kv_heads > 4 * kCus ? ROWS32 : ROWS16;
 }
 
-// most key ranges that a part is ever given, whatever its keys: wide ones as
-// many as give each CU two workgroups of 128 rows (or one of 256), narrow ones
-// eight
-int64_t most_ranges(int dtype, int rows, int64_t groups, int kv_heads) {
-  const int mode = mode_of(dtype, rows, groups, kv_heads, 0);
-  const int64_t items = cdiv(rows, rows_of(mode)) * groups * kv_heads;
+// most key ranges that a part of `items` workgroups a range is ever given: as
+// many as give each CU two wide workgroups or eight narrow ones
+int64_t most_ranges(int mode, int64_t items) {
   const int64_t wgs = mode == ROWS128 ? 2 * kCus : 8 * kCus;
   return std::min<int64_t>(kMaxRanges, (wgs + items - 1) / items);
 }
@@ -1044,33 +1018,18 @@ constexpr int kStep = kWaves * kTile;   // keys that a narrow workgroup takes at
 // the second to gain more than its records cost to join; beside tails that
 // take `beside_us` by themselves, only as many as end by then (14 us and 1.2 us
 // a tile: 64 single tokens over 8000 shared positions and up to 1500 of their
-// own, 16 ranges 60 us, 8 ranges 49).  256 rows take the
-// count with the least time: rounds of a workgroup a CU, 8 us and 1.2 us a
-// tile each, and the records at 4 TB/s.
-Part plan_part(int dtype, int hd, int mode, int rows, int64_t groups, int kv_heads, int64_t keys,
-               double beside_us = 0.0) {
+// own, 16 ranges 60 us, 8 ranges 49).
+Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys, double beside_us = 0.0) {
   Part p;
   p.row_tiles = cdiv(rows, rows_of(mode));
   const int64_t tiles = (keys + kTile - 1) / kTile, items = p.row_tiles * groups * kv_heads;
   auto fill = [&](int64_t wgs) { return (wgs + items - 1) / items; };
-  const int64_t most = most_ranges(dtype, rows, groups, kv_heads);
   int64_t ranges;
-  if (mode == ROWS256) {
-    const double joined = 8.0 * rows * groups * kv_heads * record(hd) / 4e6;
-    double best = 1e30;
-    ranges = 1;
-    for (int64_t r = 1; r <= most; ++r) {
-      const double us = double((items * r + kCus - 1) / kCus) * (1.2 * double((tiles + r - 1) / r) + 8.0) + joined * double(r);
-      if (us < best) {
-        best = us;
-        ranges = r;
-      }
-    }
-  } else if (mode == ROWS128) {
+  if (mode == ROWS128) {
     ranges = tiles >= 24 * fill(kCus) ? fill(2 * kCus) : fill(kCus);
     if (beside_us > 16.0) ranges = std::min(ranges, int64_t(1.2 * double(tiles) / (beside_us - 14.0)) + 1);
   } else ranges = keys <= 6 * kStep ? 1 : std::max(fill(2 * kCus), tiles / 24);
-  ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most, tiles / 4}));
+  ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most_ranges(mode, items), tiles / 4}));
   p.range = int(std::max<int64_t>(1, (tiles + ranges - 1) / ranges)) * kTile;
   p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
   return p;
@@ -1080,7 +1039,7 @@ Part plan_part(int dtype, int hd, int mode, int rows, int64_t groups, int kv_hea
 // themselves in a few steps (a round of two workgroups a CU) and its keys,
 // read once for every row tile, stay within what the L2s deliver meanwhile.
 bool stacks(const PagedAttn& a, int mode, int rows, int64_t keys) {
-  if (mode >= ROWS128) return true;
+  if (mode == ROWS128) return true;
   const int64_t items = int64_t(cdiv(rows, rows_of(mode))) * a.n * a.p.n_kv_heads;
   const int64_t rounds = (items + 2 * kCus - 1) / (2 * kCus), steps = (keys + kStep - 1) / kStep;
   const int64_t bytes = items * keys * 2 * a.p.head_dim * (a.p.dtype == DLLM_BF16 ? 2 : 4);
@@ -1093,18 +1052,14 @@ void launch_parts(const Job& j, hipStream_t s) {
   const int prefix = j.prefix.ranges ? blocks_of(j.prefix.ranges * kvh, j.prefix.row_tiles) : 0;
   const int tail = blocks_of(j.a.n * j.tail.ranges * kvh, j.tail.row_tiles);
   hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL>), dim3(prefix + tail),
-                     dim3(waves_of(PREFIX) * kWave), 0, s, j, prefix);
+                     dim3(kThreads), 0, s, j, prefix);
 }
 
-// of bf16 models the prefix, whose rows are at least an entry's, never takes the
-// lower mode; 256 rows go with tails of 256 or narrow ones
+// of bf16 models the prefix, whose rows are at least an entry's, never takes the lower mode
 template <typename T, int HD>
 void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (tail == ROWS256) return launch_parts<T, HD, ROWS256, ROWS256>(j, s);
     if (tail == ROWS128) return launch_parts<T, HD, ROWS128, ROWS128>(j, s);
-    if (prefix == ROWS256)
-      return tail == ROWS32 ? launch_parts<T, HD, ROWS256, ROWS32>(j, s) : launch_parts<T, HD, ROWS256, ROWS16>(j, s);
     if (prefix == ROWS128)
       return tail == ROWS32 ? launch_parts<T, HD, ROWS128, ROWS32>(j, s) : launch_parts<T, HD, ROWS128, ROWS16>(j, s);
   }
@@ -1131,8 +1086,11 @@ void launch(const Job& j, int prefix, int tail, hipStream_t s) {
 
 size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads) {
   const int group = heads / p.n_kv_heads;
-  const size_t parts = most_ranges(p.dtype, n * max_rows * group, 1, p.n_kv_heads) +
-                       most_ranges(p.dtype, max_rows * group, n, p.n_kv_heads);
+  auto ranges = [&](int rows, int groups) {
+    const int mode = mode_of(p.dtype, rows, groups, p.n_kv_heads);
+    return most_ranges(mode, int64_t(cdiv(rows, rows_of(mode))) * groups * p.n_kv_heads);
+  };
+  const size_t parts = ranges(n * max_rows * group, 1) + ranges(max_rows * group, n);
   return parts * n * max_rows * heads * record(p.head_dim) * sizeof(float);
 }
 
@@ -1171,7 +1129,7 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   const int64_t shared = std::min<int64_t>(a.shared_len, most) / a.p.page_len * a.p.page_len;
   const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
-  int mode_t = mode_of(dt, rows_t, a.n, kvh, keys - shared);
+  const int mode_t = mode_of(dt, rows_t, a.n, kvh);
   j.stacked = shared > 0 && stacks(a, mode_t, rows_t, std::max(keys, shared));
   if (j.stacked && pairs_up(a, rows_t, kvh, shared)) {
     j.direct = true;
@@ -1180,16 +1138,14 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
     else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
     return hipGetLastError();
   }
-  int mode_p = j.stacked ? mode_of(dt, rows_p, 1, kvh, shared) : mode_t;
-  if (mode_t == ROWS256) mode_p = ROWS256;
-  if (mode_p == ROWS256 && mode_t == ROWS128) rows_t > 128 ? mode_t = ROWS256 : mode_p = ROWS128;
+  const int mode_p = j.stacked ? mode_of(dt, rows_p, 1, kvh) : mode_t;
   const int hd = a.p.head_dim;
   // streaming the tails at 5 TB/s, if on average they are half as long as the longest
   const double tail_us = double(a.n) * cdiv(rows_t, rows_of(mode_t)) * kvh * double(std::max<int64_t>(0, keys - shared)) *
                          hd * (dt == DLLM_BF16 ? 2 : 4) / 5e6;
-  j.prefix = j.stacked ? plan_part(dt, hd, mode_p, rows_p, 1, kvh, shared, tail_us) : Part{1, 0, kTile};
+  j.prefix = j.stacked ? plan_part(mode_p, rows_p, 1, kvh, shared, tail_us) : Part{1, 0, kTile};
   if (shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
-  j.tail = plan_part(dt, hd, mode_t, rows_t, a.n, kvh, j.stacked ? std::max<int64_t>(1, keys - shared) : keys);
+  j.tail = plan_part(mode_t, rows_t, a.n, kvh, j.stacked ? std::max<int64_t>(1, keys - shared) : keys);
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
   if (dt == DLLM_BF16)
     a.p.head_dim == 128 ? launch<bf16_t, 128>(j, mode_p, mode_t, s) : launch<bf16_t, 64>(j, mode_p, mode_t, s);

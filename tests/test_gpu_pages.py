@@ -379,7 +379,7 @@ def test_attention_of_many_branches(hd, page, n, rows, prefix, lens, counts, cau
     (64, 256, 16, 4, 1, 300, 0, [65800], True),                       # one sequence, nothing shared
 ])
 def test_attention_of_heavy_batches(hd, page, heads, kv, n, rows, prefix, lens, causal):
-    """Many rows over many keys: 256 rows a workgroup, ranges of the keys joined."""
+    """Many rows over many keys, in ranges that are joined."""
     kp = shared_batch(torch.bfloat16, hd, page, kv, prefix, lens) if prefix else hold(
         new_pages(pages=lens[0] // page + 3, heads=kv, page=page, hd=hd, seqs=1, blocks=-(-lens[0] // page)), lens)
     poison(kp)
