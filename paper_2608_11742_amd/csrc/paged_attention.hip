@@ -994,10 +994,14 @@ constexpr int kMaxRanges = 64;
 
 // How `groups` sets of stacked rows per key head are taken.  fp32 products
 // cost an eighth of the bf16 rate, so there 32 rows, which halve what is
-// read, are only worth it where 16 fill the chip twice.
+// read, are only worth it where 16 fill the chip twice over (1000 positions, 16
+// key heads of 64, 16 / 32 rows a workgroup: 16 x 32 rows 32 us / 34, 16 x 64
+// 57 / 49).  bf16 takes the wide kernel from 33 rows on (narrow / wide: 8 x 40
+// rows over 1000 positions 39 us / 34, 16 x 48 over 2000 143 / 113, but 4 x 64
+// over 300 12 / 14).
 int mode_of(int dtype, int rows, int64_t groups, int kv_heads) {
   if (dtype == DLLM_BF16) return rows > kNarrowRows ? ROWS128 : rows > 16 ? ROWS32 : ROWS16;
-  return rows > 16 && cdiv(rows, 16) * groups * kv_heads > 4 * kCus ? ROWS32 : ROWS16;
+  return rows > 16 && cdiv(rows, 16) * groups * kv_heads >= 4 * kCus ? ROWS32 : ROWS16;
 }
 
 // most key ranges that a part of `items` workgroups a range is ever given: as
@@ -1012,13 +1016,16 @@ constexpr int kStep = kWaves * kTile;   // keys that a narrow workgroup takes at
 // Rows stacked per key head, in `groups` separate sets (entries of a tail).
 // Two workgroups fit a CU.  Narrow parts are bound by memory: as many ranges
 // as fill the chip, and where they are long ones of 24 tiles, so that batches
-// of unlike lengths come out even; a join costs about as much as 6 steps, so
-// shorter parts are not divided.  Wide ones take one workgroup a CU, which
-// leaves the other slot to the tails, and two where ranges stay long enough for
-// the second to gain more than its records cost to join; beside tails that
-// take `beside_us` by themselves, only as many as end by then (14 us and 1.2 us
-// a tile: 64 single tokens over 8000 shared positions and up to 1500 of their
-// own, 16 ranges 60 us, 8 ranges 49).
+// of unlike lengths come out even.  Joining them costs 3 us, so parts of up to
+// two steps are not divided, nor parts of up to six that have a workgroup for
+// every CU (single tokens of 8 key heads: 8 over 500 positions whole 11.7 us,
+// over 520 divided 12.2, over 1000 whole 19.2, divided 13.2; 32 over 1000 23.5
+// and 26.7, over 1500 33.3 and 36.0).
+// Wide ones take one workgroup a CU, which leaves the other slot to the tails,
+// and two where ranges stay long enough for the second to gain more than its
+// records cost to join; beside tails that take `beside_us` by themselves, only
+// as many as end by then (14 us and 1.2 us a tile: 64 single tokens over 8000
+// shared positions and up to 1500 of their own, 16 ranges 60 us, 8 ranges 49).
 Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys, double beside_us = 0.0) {
   Part p;
   p.row_tiles = cdiv(rows, rows_of(mode));
@@ -1028,22 +1035,24 @@ Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys, d
   if (mode == ROWS128) {
     ranges = tiles >= 24 * fill(kCus) ? fill(2 * kCus) : fill(kCus);
     if (beside_us > 16.0) ranges = std::min(ranges, int64_t(1.2 * double(tiles) / (beside_us - 14.0)) + 1);
-  } else ranges = keys <= 6 * kStep ? 1 : std::max(fill(2 * kCus), tiles / 24);
+  } else ranges = keys <= (items >= kCus ? 6 : 2) * kStep ? 1 : std::max(fill(2 * kCus), tiles / 24);
   ranges = std::max<int64_t>(1, std::min<int64_t>({ranges, most_ranges(mode, items), tiles / 4}));
   p.range = int(std::max<int64_t>(1, (tiles + ranges - 1) / ranges)) * kTile;
   p.ranges = int(std::max<int64_t>(1, (keys + p.range - 1) / p.range));
   return p;
 }
 
-// Is the prefix a part of its own?  Not if all entries can walk it by
-// themselves in a few steps (a round of two workgroups a CU) and its keys,
-// read once for every row tile, stay within what the L2s deliver meanwhile.
+// Is the prefix a part of its own?  Narrow entries walk it by themselves,
+// which spares the second part and the join of its records, as long as that
+// costs each of two workgroups a CU no more than a step, or two steps where
+// they end there (own / part, us; single tokens of 8 key heads: 8 over 1000
+// positions 13.1 / 14.4, over 2000 17.9 / 14.7; 32 over 250 10.3 / 13.6, over
+// 1000 24 / 17; fp32, 16 key heads, 7 x 19 rows: over 203 10.0 / 13.3, over 500
+// 18.5 / 16.6).
 bool stacks(const PagedAttn& a, int mode, int rows, int64_t keys) {
   if (mode == ROWS128) return true;
-  const int64_t items = int64_t(cdiv(rows, rows_of(mode))) * a.n * a.p.n_kv_heads;
-  const int64_t rounds = (items + 2 * kCus - 1) / (2 * kCus), steps = (keys + kStep - 1) / kStep;
-  const int64_t bytes = items * keys * 2 * a.p.head_dim * (a.p.dtype == DLLM_BF16 ? 2 : 4);
-  return rounds * steps > 6 || bytes > (int64_t(48) << 20);
+  const int64_t items = int64_t(cdiv(rows, rows_of(mode))) * a.n * a.p.n_kv_heads, steps = (keys + kStep - 1) / kStep;
+  return items * steps > (steps > 2 ? 2 : 4) * kCus;
 }
 
 template <typename T, int HD, int PREFIX, int TAIL>
@@ -1108,11 +1117,11 @@ namespace {
 // Blocks of 32 rows in pairs (see Pairs)?  For bf16 batches over a shared
 // prefix whose entries fill whole blocks, or nearly, and whose pairs fill most
 // of the chip by themselves.  A prefix tile is copied for 64 rows there and for
-// 128 wide ones, which wins where the prefix is long (16 x 32 rows, 32 heads:
-// 22 us against 32 over 1024 positions, 32 against 40 over 2048, 385 against
-// 320 over 30000).
+// 128 wide ones, which wins where the prefix is long (16 x 32 rows, 32 heads,
+// pairs / wide, us: over 1024 positions 22 / 32, 2048 32 / 40, 4500 69 / 79,
+// 6500 85 / 88, 8000 96 / 96, 30000 385 / 313).
 bool pairs_up(const PagedAttn& a, int rows, int kv_heads, int64_t shared) {
-  if (a.p.dtype != DLLM_BF16 || rows < 24 || shared > 4096) return false;
+  if (a.p.dtype != DLLM_BF16 || rows < 24 || shared > 8000) return false;
   const int blocks = cdiv(rows, 32);
   return blocks * 32 * 3 <= rows * 4 && int64_t(a.n) * blocks * kv_heads >= 3 * kCus / 2;
 }
