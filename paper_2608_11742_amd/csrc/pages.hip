@@ -156,7 +156,8 @@ __device__ __forceinline__ bool take_pages(const dllm_kv_pages& p, PlanShared& s
                                            int first, int need) {
   const int tid = threadIdx.x;
   int total, have;
-  const int off = block_scan(need, sh, total);
+  // needs past the pool fail below as they are; up to there 1024 of them sum up to less than 2^31
+  const int off = block_scan(min(need, p.n_pages + 1), sh, total);
   sh.off[tid] = off;
   sh.first[tid] = first;
   sh.seq[tid] = seq;

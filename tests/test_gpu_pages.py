@@ -153,6 +153,22 @@ def test_full_and_empty_pool():
     both.compact()
 
 
+def test_needs_past_31_bits():
+    """Tables of the largest length: 32 sequences that ask for 2^26 pages each, 2^31 together."""
+    kp = P.KvPages.empty(1, 4, 1, 16, 64, 32, 1 << 26, device=DEV)
+    status, seqs = ints([99]), ints(list(range(32)))
+    for n in (32, 31, 1):
+        P.kv_pages_grow(kp, seqs[:n], ints([1 << 30] * n), status)
+        assert status.item() == EFULL
+        assert kp.len.tolist() == [0] * 32 and kp.refs.tolist() == [0] * 4
+    P.kv_pages_grow(kp, seqs, ints([17] + [0] * 30 + [20]), status)
+    assert status.item() == OK
+    assert kp.len.tolist() == [17] + [0] * 30 + [20] and kp.refs.tolist() == [1] * 4
+    assert kp.table[:, :3].tolist() == [[0, 1, -1]] + [[-1] * 3] * 30 + [[2, 3, -1]]
+    P.kv_pages_free(kp, seqs, status)
+    assert status.item() == OK and kp.refs.tolist() == [0] * 4 and bool((kp.table[31] == -1).all())
+
+
 # ---------------------------------------------------------------- rows
 
 def hold(kp, lens, seed=0):
