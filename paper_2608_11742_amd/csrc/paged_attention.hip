@@ -27,11 +27,14 @@
 //            copied one tile ahead, on 32 x 32 MFMAs.
 // Scores are computed transposed (S^T = K Q^T): a lane then holds one row's
 // scores, and with the key order below its probabilities are, as they lie in
-// its registers, the operand of o^T += V^T P^T.  The exponent reference moves
-// only when a score passes it by 8 (log2 units), so o is rescaled rarely.
-// Probabilities of bf16 models are rounded to binary16 (below 2^8, 11
-// significant bits) for the product with binary16 values; the sums l take them
-// unrounded.
+// its registers, the operand of o^T += V^T P^T.  The exponent reference is set
+// to 8 (log2 units) under a row's largest score and stands until a weight may
+// pass 2^15, so o is rescaled rarely.  Weights of bf16 models are rounded to
+// binary16 for the product with binary16 values: 11 significant bits down to
+// 2^-22 of the row's largest, and off by 2^-33 of it at most below, so that a
+// million keys that weigh 2^-25 each are not lost beside one that weighs 1.  The
+// sums l and products o are held in 32 bits; wide and pairs sum the weights as
+// rounded, narrow before.
 #include <algorithm>
 
 #include "common.h"
@@ -46,6 +49,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 64;       // keys of a wide tile; ranges are whole tiles
 constexpr int kNarrowRows = 32;
+constexpr float kFirst = 8.f, kMost = 15.f;   // log2 of a row's largest weight when its reference moves, and ever
 // floats per record: HD output values, m, l, padding to 16 bytes
 constexpr int record(int hd) { return hd + 4; }
 
@@ -333,7 +337,7 @@ struct Narrow {
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[kb][qb][i]);
         top = quad_max(top) * j.scale_log2;
-        const float mn = top > m[qb] + 8.f ? top : m[qb];
+        const float mn = top > m[qb] + kMost ? top - kFirst : m[qb];
         const float ref = mn == -INFINITY ? 0.f : mn;   // a row that has seen no key yet: exponents 2^-inf
         alpha[qb] = __builtin_amdgcn_exp2f(m[qb] - ref);
         moved = moved || mn != m[qb];
@@ -591,17 +595,18 @@ struct Rows32 {
           if (k0 + 32 * h + 16 * (i >> 3) + 8 * f + (i & 7) >= lim) sc[h][i] = -INFINITY;
     }
     // With the reference as it is, unless a weight would pass what binary16 holds
-    // (or there is none yet): no lane's 16 H weights sum up to more than 2^13.
-    // Their maximum is only looked for where it has to move.
+    // (or there is none yet): no lane's 16 H weights sum up to more than 2^kMost.
+    // Their maximum is only looked for where it may have to move: not if none
+    // of them passes 2^kMost / 32.
     float sum = weights(sc, scale_log2, m, pf);
-    if (!__all(sum <= 8192.f)) {
+    if (!__all(sum <= float(1 << int(kMost)))) {
       float top = -INFINITY;
 #pragma unroll
       for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[h][i]);
       top = pair_max(top) * scale_log2;
-      const float mn = top > m + 8.f ? top : m;
+      const float mn = top > m + (kMost - 5.f) ? top - kFirst : m;
       const float ref = mn == -INFINITY ? 0.f : mn;   // no key seen yet: weights 2^-inf
       const float alpha = __builtin_amdgcn_exp2f(m - ref);
       l *= alpha;

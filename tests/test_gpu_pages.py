@@ -419,6 +419,37 @@ def test_attention_extremes():
     assert torch.equal(out[[0, 2, 3]], clean[[0, 2, 3]]) and out[1].isnan().all()
 
 
+@pytest.mark.parametrize("n,rows,keys,shared", [
+    (1024, 1, 1500, 0),          # rows of single tokens
+    (1, 65536, 20000, 0),        # many rows
+    (400, 32, 8000, 8000),       # branches over a prefix
+    (2, 16, 60000, 60000),       # ranges joined
+])
+def test_attention_weights_far_below_the_largest(n, rows, keys, shared):
+    """Key 0 outweighs every other one by 2^25, its value is 0 and theirs 1: the
+    output is what the others weigh together, a bf16 rounding (2^-8) and their
+    weights' rounding (2^-17 of binary16 with 2^8 the largest: half a step of
+    2^-24 is 2^-8 of it) away."""
+    page, hd = 64, 64
+    whole = -(-keys // page)
+    kp = P.KvPages.empty(1, whole, 1, page, hd, 1024, whole, device=DEV)
+    kp.k.zero_()
+    kp.vt.fill_(1)
+    kp.k[0, 0, 0, 0, 0] = 4.34375
+    kp.vt[0, 0, 0, :, 0] = 0
+    kp.table[:] = torch.arange(whole, dtype=torch.int32, device=DEV)
+    kp.len.fill_(keys)
+    kp.refs.fill_(1024)
+    q = torch.zeros(n, rows, 1, hd, dtype=torch.bfloat16, device=DEV)
+    q[..., 0] = 4
+    out = torch.empty_like(q)
+    ws = torch.empty(P.kv_pages_attention_workspace_bytes(kp, n, rows, 1), dtype=torch.uint8, device=DEV)
+    P.kv_pages_attention(kp, 0, ints(list(range(n))), q, out, ws, shared_len=shared, max_len=keys, scale=1.0)
+    want = (keys - 1) / (np.exp(4 * 4.34375) + keys - 1)
+    diff = (out.double() / want - 1).abs().max().item()
+    assert diff <= 2.0 ** -8 + 2.0 ** -7.9 + 2.0 ** -10
+
+
 def test_attention_strides_and_heads_first():
     kp = hold(new_pages(seqs=3, pages=60, blocks=20, heads=4), [300, 64, 290])
     g = torch.Generator(device=DEV).manual_seed(3)
