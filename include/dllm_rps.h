@@ -266,6 +266,8 @@ dllm_status vocab_entropy_topk_noalloc(const void* hidden, const void* w_lm, int
  * n_pages <= KV_MAX_PAGES, max_seqs <= KV_MAX_SEQS, n_kv_heads <= 1024,
  * max_blocks * page_len <= KV_MAX_POSITIONS.
  *
+ * Workspaces are 16-byte aligned.
+ *
  * Sequence lists are device arrays.  The calls that change tables check them
  * on the device: `status` (device int32) receives KV_PAGES_OK, or the lowest
  * code that applies and nothing is changed. */
@@ -358,7 +360,8 @@ dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int3
  *                sees positions 0 .. len - n_rows[b] + i.
  * A row that sees no position is 0, and so are the rows of a sequence outside
  * 0 .. max_seqs-1.  Table entries outside the pool are clamped.  Positions past
- * a row's last are never used, whatever they hold. */
+ * a sequence's last are never used, whatever they hold; with causal, a row
+ * gives those after its own the weight 0, so their values are to be finite. */
 size_t kv_pages_attention_workspace_bytes(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads);
 dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
                                int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,

@@ -921,7 +921,8 @@ dllm_status kv_pages_compact(const dllm_kv_pages* pages, int32_t* n_used, void* 
                              dllm_stream stream) {
   dllm_status st = check_pages(pages, "kv_pages_compact");
   if (st != DLLM_OK) return st;
-  if (!n_used || !ws) return fail(DLLM_EINVAL, "kv_pages_compact: NULL n_used or ws");
+  if (!n_used) return fail(DLLM_EINVAL, "kv_pages_compact: NULL n_used");
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "kv_pages_compact: ws NULL or not 16-byte aligned");
   const size_t need = pages_compact_workspace(pages->n_pages);
   if (ws_bytes < need) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, need);
   return hip_check(pages_compact(*pages, n_used, ws, static_cast<hipStream_t>(stream)), "kv_pages_compact");
@@ -1021,6 +1022,7 @@ dllm_status dllm_forward_pages(dllm_model* m, const int32_t* tokens, int32_t bat
     return fail(DLLM_ESHAPE, "dllm_forward_pages: shared_len %d max_len %d", shared_len, max_len);
   if (shared_len > 0 && (prefix_seq < 0 || prefix_seq >= pages->max_seqs))
     return fail(DLLM_EINVAL, "dllm_forward_pages: prefix_seq %d outside 0..%d", prefix_seq, pages->max_seqs - 1);
+  if (reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "dllm_forward_pages: ws not 16-byte aligned");
   const Paging pg{pages, seqs, prefix_seq, shared_len, max_len};
   return forward_impl(m, tokens, batch, seq, 0, nullptr, nullptr, lm_pos, n_lm_pos, row_scale, scale, probe, out, ws,
                       ws_bytes, stream, nullptr, &pg);

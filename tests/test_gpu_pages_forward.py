@@ -176,3 +176,13 @@ def test_refusals(P, tiny, small_bf16):
     with pytest.raises(P.binding.DllmError):
         P.dllm_forward_pages(model.handle, t, kp, seqs, lm, P.Stats(1, 16, device=DEV),
                              torch.empty(1024, dtype=torch.uint8, device=DEV))
+
+
+def test_workspace_alignment(P, tiny):
+    shape, _, model = tiny
+    kp = model.new_kv_pages(10, page_len=16, max_seqs=2, max_len=64)
+    t, seqs, lm = torch.zeros(1, 4, dtype=torch.int32, device=DEV), ints([0]), ints([0])
+    ws = torch.empty(P.dllm_workspace_bytes_pages(model.handle, 1, 4, 1) + 16, dtype=torch.uint8, device=DEV)
+    for by in (1, 4, 8):
+        with pytest.raises(P.binding.DllmError):
+            P.dllm_forward_pages(model.handle, t, kp, seqs, lm, P.Stats(1, 16, device=DEV), ws[by:])

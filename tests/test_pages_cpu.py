@@ -74,6 +74,14 @@ def test_call_arguments(abi):
 
 
 @needs_lib
+def test_workspace_alignment(abi):
+    _abi, lib = abi
+    p = C.byref(pages(_abi))
+    for ws in (None, FAKE + 1, FAKE + 4, FAKE + 8):
+        assert lib.kv_pages_compact(p, FAKE, ws, 1 << 30, None) == 1
+
+
+@needs_lib
 def test_row_arguments(abi):
     _abi, lib = abi
     p = C.byref(pages(_abi))
