@@ -16,15 +16,25 @@
 // less than a join: then every entry's range starts at position 0 and takes its
 // pages from the prefix's table first.
 //
-// Two kernels, by the number of stacked rows:
+// Three kernels, by the number of stacked rows (MI355X; floors by the rates of
+// a large copy, 4.9 TB/s, and a large bf16 product, 1190 TFLOP/s):
 //   narrow   up to 32 rows: bound by the keys and values it streams.  The
 //            waves share the rows and take the key steps in turn; a step's
 //            fragments come straight from memory into registers, K of the
 //            next step while the softmax runs, V after it (no LDS, no
-//            barrier), and the waves' states are joined through LDS at the end.
-//   wide     128 rows, 32 a wave: bound by MFMAs and the softmax's vector
-//            instructions.  Tiles of 64 keys go through a two-slot LDS ring,
-//            copied one tile ahead, on 32 x 32 MFMAs.
+//            barrier), and the waves' states are joined through LDS at the
+//            end.  Single tokens of 4 sequences up to 120000 long, 8 key heads
+//            of 128: 217 us, 5.7 TB/s.
+//   wide     128 rows, 32 a wave (bf16).  Tiles of 64 keys go through a
+//            two-slot LDS ring, copied one tile ahead, on 32 x 32 MFMAs.  16 x
+//            32 rows of 32 heads over 30011 positions: 318 us, 0.80 PFLOP/s,
+//            floor 213.  Matrix units are busy 43% of it and vector ALUs 37%:
+//            products and softmax alone take 177 us, fragment reads from LDS
+//            add 50, the copies 85 and the join of the ranges 15.
+//   pairs    two entries' 32 rows each (bf16): prefix and own tails in one
+//            launch that writes the output.  16 x 32 rows over 1024: 21 us, of
+//            which 7 are spent before and after the keys, 1.4 on every 128
+//            positions and 2.5 on the tail; floor 7.4.
 // Scores are computed transposed (S^T = K Q^T): a lane then holds one row's
 // scores, and with the key order below its probabilities are, as they lie in
 // its registers, the operand of o^T += V^T P^T.  The exponent reference is set
