@@ -186,3 +186,50 @@ def test_workspace_alignment(P, tiny):
     for by in (1, 4, 8):
         with pytest.raises(P.binding.DllmError):
             P.dllm_forward_pages(model.handle, t, kp, seqs, lm, P.Stats(1, 16, device=DEV), ws[by:])
+
+
+def test_forward_captured_and_replayed(P, tiny):
+    """Grow, forward and roll back in one graph, one entry of the batch padding;
+    every replay bit for bit the eager pass over the same tokens, and as the
+    entries by themselves."""
+    shape, _, model = tiny
+    kp = model.new_kv_pages(30, page_len=16, max_seqs=4, max_len=128)
+    st = ints([0])
+    P.kv_pages_grow(kp, ints([0]), ints([40]), st)
+    model.forward_pages(torch.from_numpy(toks("s", 40, shape))[None].to(DEV), kp, ints([0]), ints([0]))
+    P.kv_pages_fork(kp, ints([0, 0]), ints([1, 2]), st)
+    seqs, padded, add, keep, lm = ints([1, 2]), ints([1, -1, 2]), ints([24, 24]), ints([40, 40]), ints([5, 23])
+    block = torch.zeros(3, 24, dtype=torch.int32, device=DEV)
+    out = P.Stats(6, 16, device=DEV)
+    ws = torch.empty(P.dllm_workspace_bytes_pages(model.handle, 3, 24, 2), dtype=torch.uint8, device=DEV)
+
+    def step():
+        P.kv_pages_grow(kp, seqs, add, st)
+        P.dllm_forward_pages(model.handle, block, kp, padded, lm, out, ws, prefix_seq=0, shared_len=40, max_len=64)
+        P.kv_pages_free(kp, seqs, st, keep=keep)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for replay in range(3):
+        block.copy_(torch.from_numpy(np.stack([toks(f"{x}{replay}", 24, shape) for x in "tuv"])))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {k: v.copy() for k, v in out.numpy().items()}
+        assert st.item() == 0 and kp.len.tolist() == [40, 40, 40, 0]
+        step()
+        torch.cuda.synchronize()
+        eager = out.numpy()
+        assert all(np.array_equal(eager[k], got[k]) for k in got)
+        assert np.isfinite(got["H"]).all()
+        for entry, s in ((0, 1), (2, 2)):
+            P.kv_pages_grow(kp, ints([s]), ints([24]), st)
+            alone = model.forward_pages(block[entry:entry + 1].contiguous(), kp, ints([s]), lm).numpy()
+            P.kv_pages_free(kp, ints([s]), st, keep=ints([40]))
+            assert np.allclose(alone["H"], got["H"][2 * entry:2 * entry + 2], rtol=1e-4, atol=1e-4)
+            assert np.array_equal(alone["argmax"], got["argmax"][2 * entry:2 * entry + 2])
