@@ -1134,11 +1134,14 @@ namespace {
 // of the chip by themselves.  A prefix tile is copied for 64 rows there and for
 // 128 wide ones, which wins where the prefix is long (16 x 32 rows, 32 heads,
 // pairs / wide, us: over 1024 positions 22 / 32, 2048 32 / 40, 4500 69 / 79,
-// 6500 85 / 88, 8000 96 / 96, 30000 385 / 313).
+// 6500 85 / 88, 8000 96 / 96, 30000 385 / 313), sooner where the pairs take
+// more than a round of the chip (64 x 32: 1024 75 / 88, 2048 116 / 120, 4096
+// 205 / 194; 32 x 32, heads of 64: 1024 26 / 35, 4096 70 / 66).
 bool pairs_up(const PagedAttn& a, int rows, int kv_heads, int64_t shared) {
-  if (a.p.dtype != DLLM_BF16 || rows < 24 || shared > 8000) return false;
   const int blocks = cdiv(rows, 32);
-  return blocks * 32 * 3 <= rows * 4 && int64_t(a.n) * blocks * kv_heads >= 3 * kCus / 2;
+  const int64_t all = int64_t(a.n) * blocks * kv_heads;
+  return a.p.dtype == DLLM_BF16 && rows >= 24 && blocks * 32 * 3 <= rows * 4 && all >= 3 * kCus / 2 &&
+         shared <= (all <= 2 * kCus ? 8000 : 4000);
 }
 
 }  // namespace
