@@ -1136,12 +1136,15 @@ namespace {
 // pairs / wide, us: over 1024 positions 22 / 32, 2048 32 / 40, 4500 69 / 79,
 // 6500 85 / 88, 8000 96 / 96, 30000 385 / 313), sooner where the pairs take
 // more than a round of the chip (64 x 32: 1024 75 / 88, 2048 116 / 120, 4096
-// 205 / 194; 32 x 32, heads of 64: 1024 26 / 35, 4096 70 / 66).
+// 205 / 194; 32 x 32, heads of 64: 1024 26 / 35, 4096 70 / 66).  Shorter than a
+// step of theirs, entries by themselves win (16 x 32, pairs / entries: over 64
+// 11.0 / 10.4, 128 10.5 / 12.7, 256 12.1 / 16.2, 448 15.6 / 21.3; 64 x 32: 64 41 /
+// 32, 128 40 / 41, 256 46 / 52).
 bool pairs_up(const PagedAttn& a, int rows, int kv_heads, int64_t shared) {
   const int blocks = cdiv(rows, 32);
   const int64_t all = int64_t(a.n) * blocks * kv_heads;
   return a.p.dtype == DLLM_BF16 && rows >= 24 && blocks * 32 * 3 <= rows * 4 && all >= 3 * kCus / 2 &&
-         shared <= (all <= 2 * kCus ? 8000 : 4000);
+         shared >= Pairs<64>::kKeys && shared <= (all <= 2 * kCus ? 8000 : 4000);
 }
 
 }  // namespace
@@ -1157,14 +1160,14 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
   const int mode_t = mode_of(dt, rows_t, a.n, kvh);
-  j.stacked = shared > 0 && stacks(a, mode_t, rows_t, std::max(keys, shared));
-  if (j.stacked && pairs_up(a, rows_t, kvh, shared)) {
+  if (pairs_up(a, rows_t, kvh, shared)) {
     j.direct = true;
     const int grid = blocks_of(kvh, cdiv(a.n * cdiv(rows_t, 32), 2));
     if (a.p.head_dim == 128) hipLaunchKernelGGL(pairs_kernel<128>, dim3(grid), dim3(Pairs<128>::kPairThreads), 0, s, j);
     else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
     return hipGetLastError();
   }
+  j.stacked = shared > 0 && stacks(a, mode_t, rows_t, std::max(keys, shared));
   const int mode_p = j.stacked ? mode_of(dt, rows_p, 1, kvh) : mode_t;
   const int hd = a.p.head_dim;
   // streaming the tails at 5 TB/s, if on average they are half as long as the longest
