@@ -12,9 +12,9 @@
 // and each of the two over workgroups by ranges of keys, where there are few
 // rows.  Every range leaves a record per row, and a merge joins them in order;
 // with one range in all the workgroup writes the output itself.  Where the
-// entries are few and short, reading the prefix again for each of them costs
-// less than a join: then every entry's range starts at position 0 and takes its
-// pages from the prefix's table first.
+// entries are few, short or fill their workgroups, reading the prefix again for
+// each of them costs less than a join: then every entry's range starts at
+// position 0 and takes its pages from the prefix's table first.
 //
 // Three kernels, by the number of stacked rows (MI355X; floors by the rates of
 // a large copy, 4.9 TB/s, and a large bf16 product, 1190 TFLOP/s):
@@ -1057,19 +1057,6 @@ Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys, d
   return p;
 }
 
-// Is the prefix a part of its own?  Narrow entries walk it by themselves,
-// which spares the second part and the join of its records, as long as that
-// costs each of two workgroups a CU no more than a step, or two steps where
-// they end there (own / part, us; single tokens of 8 key heads: 8 over 1000
-// positions 13.1 / 14.4, over 2000 17.9 / 14.7; 32 over 250 10.3 / 13.6, over
-// 1000 24 / 17; fp32, 16 key heads, 7 x 19 rows: over 203 10.0 / 13.3, over 500
-// 18.5 / 16.6).
-bool stacks(const PagedAttn& a, int mode, int rows, int64_t keys) {
-  if (mode == ROWS128) return true;
-  const int64_t items = int64_t(cdiv(rows, rows_of(mode))) * a.n * a.p.n_kv_heads, steps = (keys + kStep - 1) / kStep;
-  return items * steps > (steps > 2 ? 2 : 4) * kCus;
-}
-
 template <typename T, int HD, int PREFIX, int TAIL>
 void launch_parts(const Job& j, hipStream_t s) {
   const int kvh = j.a.p.n_kv_heads;
@@ -1129,22 +1116,48 @@ size_t paged_attention_workspace_upto(const dllm_kv_pages& p, int n, int max_row
 
 namespace {
 
-// Blocks of 32 rows in pairs (see Pairs)?  For bf16 batches over a shared
-// prefix whose entries fill whole blocks, or nearly, and whose pairs fill most
-// of the chip by themselves.  A prefix tile is copied for 64 rows there and for
-// 128 wide ones, which wins where the prefix is long (16 x 32 rows, 32 heads,
-// pairs / wide, us: over 1024 positions 22 / 32, 2048 32 / 40, 4500 69 / 79,
-// 6500 85 / 88, 8000 96 / 96, 30000 385 / 313), sooner where the pairs take
-// more than a round of the chip (64 x 32: 1024 75 / 88, 2048 116 / 120, 4096
-// 205 / 194; 32 x 32, heads of 64: 1024 26 / 35, 4096 70 / 66).  Shorter than a
-// step of theirs, entries by themselves win (16 x 32, pairs / entries: over 64
-// 11.0 / 10.4, 128 10.5 / 12.7, 256 12.1 / 16.2, 448 15.6 / 21.3; 64 x 32: 64 41 /
-// 32, 128 40 / 41, 256 46 / 52).
-bool pairs_up(const PagedAttn& a, int rows, int kv_heads, int64_t shared) {
-  const int blocks = cdiv(rows, 32);
-  const int64_t all = int64_t(a.n) * blocks * kv_heads;
-  return a.p.dtype == DLLM_BF16 && rows >= 24 && blocks * 32 * 3 <= rows * 4 && all >= 3 * kCus / 2 &&
-         shared >= Pairs<64>::kKeys && shared <= (all <= 2 * kCus ? 8000 : 4000);
+// Three ways to take a batch over a shared prefix: every entry by itself, from
+// position 0 on; the prefix and the tails as parts, joined; pairs.  The one of the
+// least estimated time is taken (measured, us, heads of 128, entries / parts /
+// pairs: 32 heads, 16 x 32 rows over 64 positions 10.4 / 21.8 / 10.8, over 256
+// 16.4 / 22.8 / 12.1, over 1024 38 / 31 / 21, over 8000 - / 96 / 96, over 30000
+// 1013 / 321 / 380; 16 x 128 over 1024 53 / 83 / 83; 16 x 40 over 128 15 / 28 /
+// 20, over 4096 147 / 86 / 102; 64 x 32 over 64 32 / 60 / 41, over 4096 461 / 186
+// / 203; 8 key heads, 32 single tokens over 500 13.7 / 19.0, over 1000 20.9 /
+// 16.8; fp32, 16 heads of 64, 7 x 19 over 203 10.0 / 13.4, 7 x 4 over 1000 18.5 /
+// 12.6).  Of 118 batches of this kind all but a few were within 10% of the best
+// of the three.
+//
+// Estimated times, in us on a whole MI355X:
+//   work   of a part where the chip is full of it: keys and values of narrow
+//          workgroups at 8.5 TB/s (they come from the caches for the most
+//          part), and 4.5 for every round of two workgroups a CU after the
+//          first; 2.4 for a wide tile of two workgroups on every CU
+//   wait   along one workgroup: 2.7 a narrow step, 1.6 a wide tile
+struct Cost {
+  double work, wait;
+};
+Cost cost_of(const PagedAttn& a, int mode, const Part& p, int groups, double keys) {
+  const double items = double(p.row_tiles) * groups * a.p.n_kv_heads, range = std::min(double(p.range), keys);
+  const int row = a.p.head_dim * (a.p.dtype == DLLM_BF16 ? 2 : 4);
+  if (mode == ROWS128) {
+    const double u = row / 256.0 / kTile;
+    return {2.4 * u * keys * items / (2 * kCus), 1.6 * u * range};
+  }
+  const int step = kWaves * std::min(64, (mode == ROWS16 && a.p.dtype == DLLM_BF16 ? 16 : 8) * 1024 / row);
+  return {items * keys * 2 * row / 8.5e6 + 4.5 * std::max(0.0, items / (2 * kCus) - 1), 2.7 * range / step};
+}
+// a launch, two parts in it, and the join of a row's records, written and read at 5 TB/s
+double parts_us(const PagedAttn& a, int mode, Cost x, Cost y, int records) {
+  const double rows = double(a.n) * a.max_rows * a.heads;
+  return (mode == ROWS32 ? 7.0 : 6.0) + std::max({x.work + y.work, x.wait, y.wait}) +
+         (records > 1 ? 3.0 + rows * records * 2 * record(a.p.head_dim) * sizeof(float) / 5e6 : 0.0);
+}
+// blocks of 32 rows in pairs (see Pairs), a pair on a CU: steps of 128 keys of
+// the prefix, then of the tail
+double pairs_us(const PagedAttn& a, int rows, int64_t shared, double tail) {
+  const double u = a.p.head_dim / 128.0, all = double(a.n) * cdiv(rows, 32) * a.p.n_kv_heads;
+  return std::ceil(all / (2 * kCus)) * (4.8 + u * (3.4 + (1.45 * shared + 3.5 * tail) / Pairs<128>::kKeys));
 }
 
 }  // namespace
@@ -1160,22 +1173,39 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
   const int mode_t = mode_of(dt, rows_t, a.n, kvh);
-  if (pairs_up(a, rows_t, kvh, shared)) {
-    j.direct = true;
-    const int grid = blocks_of(kvh, cdiv(a.n * cdiv(rows_t, 32), 2));
-    if (a.p.head_dim == 128) hipLaunchKernelGGL(pairs_kernel<128>, dim3(grid), dim3(Pairs<128>::kPairThreads), 0, s, j);
-    else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
-    return hipGetLastError();
-  }
-  j.stacked = shared > 0 && stacks(a, mode_t, rows_t, std::max(keys, shared));
-  const int mode_p = j.stacked ? mode_of(dt, rows_p, 1, kvh) : mode_t;
   const int hd = a.p.head_dim;
-  // streaming the tails at 5 TB/s, if on average they are half as long as the longest
-  const double tail_us = double(a.n) * cdiv(rows_t, rows_of(mode_t)) * kvh * double(std::max<int64_t>(0, keys - shared)) *
-                         hd * (dt == DLLM_BF16 ? 2 : 4) / 5e6;
-  j.prefix = j.stacked ? plan_part(mode_p, rows_p, 1, kvh, shared, tail_us) : Part{1, 0, kTile};
+  // lengths of the tails: the longest, and half of it on average
+  const int64_t longest = std::max<int64_t>(1, keys - shared);
+  const double mean = std::max<int64_t>(0, keys - shared) / 2.0;
+  j.prefix = Part{1, 0, kTile};
+  j.tail = plan_part(mode_t, rows_t, a.n, kvh, std::max(keys, shared));
+  int mode_p = mode_t;
+  if (shared > 0) {
+    const Cost none{0, 0};
+    const double own = parts_us(a, mode_t, cost_of(a, mode_t, j.tail, a.n, shared + mean), none, j.tail.ranges);
+    const int mode = mode_of(dt, rows_p, 1, kvh);
+    const Part tail = plan_part(mode_t, rows_t, a.n, kvh, longest);
+    // what the tails take by themselves, at 5 TB/s
+    const double tail_us = double(a.n) * tail.row_tiles * kvh * mean * 2 * hd * (dt == DLLM_BF16 ? 2 : 4) / 5e6;
+    const Part prefix = plan_part(mode, rows_p, 1, kvh, shared, tail_us);
+    const double parts = parts_us(a, mode_t, cost_of(a, mode, prefix, 1, double(shared)),
+                                  cost_of(a, mode_t, tail, a.n, mean), prefix.ranges + tail.ranges);
+    // (of fewer rows than half a block most of a pair would be empty)
+    if (dt == DLLM_BF16 && rows_t >= 16 && pairs_us(a, rows_t, shared, mean) < std::min(own, parts)) {
+      j.direct = true;
+      const int grid = blocks_of(kvh, cdiv(a.n * cdiv(rows_t, 32), 2));
+      if (hd == 128) hipLaunchKernelGGL(pairs_kernel<128>, dim3(grid), dim3(Pairs<128>::kPairThreads), 0, s, j);
+      else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
+      return hipGetLastError();
+    }
+    j.stacked = parts < own;
+    if (j.stacked) {
+      j.prefix = prefix;
+      j.tail = tail;
+      mode_p = mode;
+    }
+  }
   if (shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
-  j.tail = plan_part(mode_t, rows_t, a.n, kvh, j.stacked ? std::max<int64_t>(1, keys - shared) : keys);
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
   if (dt == DLLM_BF16)
     a.p.head_dim == 128 ? launch<bf16_t, 128>(j, mode_p, mode_t, s) : launch<bf16_t, 64>(j, mode_p, mode_t, s);

@@ -389,6 +389,28 @@ def test_attention_of_many_branches(hd, page, n, rows, prefix, lens, counts, cau
                     causal, prefix_seq=0, shared_len=prefix, max_len=max(lens))
 
 
+@pytest.mark.parametrize("hd,page,heads,kv,n,rows,prefix,lens", [
+    (128, 16, 2, 2, 5, 130, 173, [303, 180, 90, 0, 500]),             # entries by themselves fill workgroups
+    (64, 32, 4, 4, 3, 70, 1000, [1070, 1100, 900]),                   # and are divided
+    (128, 16, 8, 8, 20, 33, 117, [150, 117, 160]),
+    (64, 64, 4, 4, 4, 128, 700, [828, 1500, 60]),
+    (128, 64, 8, 2, 6, 40, 130, [170, 300, 131]),                     # grouped heads
+    (64, 128, 32, 32, 7, 60, 640, [700, 655, 641, 100]),              # two blocks an entry, in pairs
+    (128, 32, 32, 32, 9, 17, 517, [534, 520, 0, 612]),                # blocks half empty
+    (64, 16, 32, 4, 9, 5, 530, [535, 530, 700]),                      # rows of grouped heads in a block
+])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_of_entries_and_parts(hd, page, heads, kv, n, rows, prefix, lens, causal):
+    """Batches about where one way to take them over a prefix gives place to another."""
+    lens = [lens[i % len(lens)] for i in range(n)]
+    kp = shared_batch(torch.bfloat16, hd, page, kv, prefix, lens)
+    poison(kp)
+    q = queries(n, rows, heads, hd, torch.bfloat16)
+    counts = [max(0, rows - 7 * (i % 4)) for i in range(n)]
+    for most in (max(lens), 1, 20000):
+        check_attention(kp, 1, list(range(1, n + 1)), q, counts, causal, prefix_seq=0, shared_len=prefix, max_len=most)
+
+
 @pytest.mark.parametrize("hd,page,heads,kv,n,rows,prefix,lens,causal", [
     (64, 64, 32, 32, 3, 50, 16400, [16450, 16433, 16600], False),     # stacked rows end inside a row tile
     (128, 128, 64, 8, 5, 26, 16500, [16526, 16700, 16550, 16390, 0], True),   # grouped heads, one entry inside the prefix, one empty
