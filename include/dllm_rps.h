@@ -368,6 +368,24 @@ dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const 
                                const dllm_rows* out, int32_t prefix_seq, int32_t shared_len, int32_t max_len,
                                int32_t causal, float scale, void* ws, size_t ws_bytes, dllm_stream stream);
 
+/* How kv_pages_attention divides a call of these sizes.  A host function:
+ * nothing is launched, and the arrays of `pages` are not read.
+ *   KV_WAY_ENTRIES   every entry by itself, over the prefix and its own pages
+ *   KV_WAY_PARTS     the prefix for the rows of all entries, the tails for
+ *                    each one's own, the two joined
+ *   KV_WAY_PAIRS     two blocks of 32 rows in a workgroup, prefix and tails
+ * `rows` of a part are those of a workgroup, 16, 32 or 128; its keys are taken
+ * in `ranges` of `keys` positions (the last one to the end), which are joined.
+ * The prefix's are 0 unless it is a part, with pairs all are 0. */
+enum { KV_WAY_ENTRIES = 0, KV_WAY_PARTS = 1, KV_WAY_PAIRS = 2 };
+typedef struct {
+    int32_t way;
+    int32_t prefix_rows, prefix_ranges, prefix_keys;
+    int32_t tail_rows, tail_ranges, tail_keys;
+} kv_attention_plan;
+dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
+                                    int32_t shared_len, int32_t max_len, kv_attention_plan* plan);
+
 /* One denoising forward of a batch whose sequences live in pages: requests of
  * different lengths, or lookahead branches forked off one another.  Row i of
  * entry b is position len - seq + i of sequence seqs[b] (the last seq

@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     dllm_profile_begin, dllm_profile_end, dllm_mfma_ceiling,
     KvPages, kv_pages_init, kv_pages_grow, kv_pages_fork, kv_pages_free, kv_pages_compact,
     kv_pages_compact_workspace_bytes, kv_pages_write, kv_pages_attention, kv_pages_attention_workspace_bytes,
+    kv_pages_attention_plan,
     dllm_forward_pages, dllm_workspace_bytes_pages,
 )
 from .model import Model  # noqa: F401

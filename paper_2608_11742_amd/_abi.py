@@ -58,6 +58,11 @@ class Rows(C.Structure):
     _fields_ = [("p", vp), ("seq", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
 
 
+class AttentionPlan(C.Structure):
+    _fields_ = [(f, i32) for f in ("way", "prefix_rows", "prefix_ranges", "prefix_keys", "tail_rows", "tail_ranges",
+                                   "tail_keys")]
+
+
 class Probe(C.Structure):
     _fields_ = [("row", vp), ("token", vp), ("logit", vp), ("n", i32)]
 
@@ -109,6 +114,7 @@ SIGNATURES = {
     "kv_pages_attention_workspace_bytes": (sz, [C.POINTER(KvPagesC), i32, i32, i32]),
     "kv_pages_attention": (i32, [C.POINTER(KvPagesC), i32, vp, i32, i32, vp, i32, C.POINTER(Rows), C.POINTER(Rows),
                                  i32, i32, i32, i32, f32, vp, sz, vp]),
+    "kv_pages_attention_plan": (i32, [C.POINTER(KvPagesC), i32, i32, i32, i32, i32, C.POINTER(AttentionPlan)]),
     "dllm_profile_begin": (i32, [vp, i32]),
     "dllm_profile_begin_classes": (i32, [vp, i32, C.c_uint32]),
     "dllm_profile_end": (i32, [vp, C.POINTER(f32), C.POINTER(i32)]),
@@ -124,6 +130,7 @@ SIGNATURES = {
 
 SCHED_TOP_CONFIDENCE, SCHED_LOW_ENTROPY = 0, 1
 KV_PAGES_OK, KV_PAGES_ESEQ, KV_PAGES_ELEN, KV_PAGES_ESHARED, KV_PAGES_EFULL = 0, 1, 2, 3, 4
+KV_WAY_ENTRIES, KV_WAY_PARTS, KV_WAY_PAIRS = 0, 1, 2
 KV_MAX_PAGES, KV_MAX_SEQS, KV_MAX_POSITIONS = 1 << 20, 1024, 1 << 30
 
 

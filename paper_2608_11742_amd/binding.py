@@ -370,6 +370,16 @@ def kv_pages_attention(pages: KvPages, layer: int, seqs, q, out, ws, n_rows=None
                                     *_scratch(pages, ws), _page_stream(pages, stream)))
 
 
+def kv_pages_attention_plan(pages: KvPages, n: int, max_rows: int, n_heads: int, shared_len: int = 0,
+                            max_len: int | None = None):
+    """How kv_pages_attention divides a call of these sizes (way, and rows, ranges and keys of its parts)."""
+    if max_len is None:
+        max_len = pages.table.shape[1] * pages.page_len
+    plan = _abi.AttentionPlan()
+    _check(lib().kv_pages_attention_plan(pages._ref, n, max_rows, n_heads, shared_len, max_len, C.byref(plan)))
+    return plan
+
+
 def dllm_workspace_bytes_pages(handle, batch: int, seq: int, n_lm_pos: int) -> int:
     return lib().dllm_workspace_bytes_pages(handle, batch, seq, n_lm_pos)
 

@@ -1003,6 +1003,23 @@ dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const 
   return hip_check(paged_attention(a, static_cast<hipStream_t>(stream)), "kv_pages_attention");
 }
 
+dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
+                                    int32_t shared_len, int32_t max_len, kv_attention_plan* plan) {
+  dllm_status st = check_attention(pages, n, max_rows, n_heads, "kv_pages_attention_plan");
+  if (st != DLLM_OK) return st;
+  if (!plan) return fail(DLLM_EINVAL, "kv_pages_attention_plan: NULL plan");
+  if (shared_len < 0 || max_len < 0)
+    return fail(DLLM_ESHAPE, "kv_pages_attention_plan: shared_len %d max_len %d", shared_len, max_len);
+  PagedAttn a{};
+  a.p = *pages;
+  a.n = n;
+  a.max_rows = max_rows;
+  a.heads = n_heads;
+  a.shared_len = shared_len;
+  a.max_len = max_len;
+  *plan = paged_attention_plan(a);
+  return DLLM_OK;
+}
 
 dllm_status dllm_forward_pages(dllm_model* m, const int32_t* tokens, int32_t batch, int32_t seq,
                                const dllm_kv_pages* pages, const int32_t* seqs, int32_t prefix_seq,

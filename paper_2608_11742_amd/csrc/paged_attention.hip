@@ -1066,7 +1066,7 @@ void launch_parts(const Job& j, hipStream_t s) {
                      dim3(kThreads), 0, s, j, prefix);
 }
 
-// of bf16 models the prefix, whose rows are at least an entry's, never takes the lower mode
+// (a prefix never takes fewer rows than the tails, see divide)
 template <typename T, int HD>
 void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
@@ -1074,8 +1074,6 @@ void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
     if (prefix == ROWS128)
       return tail == ROWS32 ? launch_parts<T, HD, ROWS128, ROWS32>(j, s) : launch_parts<T, HD, ROWS128, ROWS16>(j, s);
   }
-  if constexpr (sizeof(T) == 4)
-    if (tail == ROWS32 && prefix == ROWS16) return launch_parts<T, HD, ROWS16, ROWS32>(j, s);
   if (tail == ROWS32) return launch_parts<T, HD, ROWS32, ROWS32>(j, s);
   return prefix == ROWS32 ? launch_parts<T, HD, ROWS32, ROWS16>(j, s) : launch_parts<T, HD, ROWS16, ROWS16>(j, s);
 }
@@ -1160,6 +1158,50 @@ double pairs_us(const PagedAttn& a, int rows, int64_t shared, double tail) {
   return std::ceil(all / (2 * kCus)) * (4.8 + u * (3.4 + (1.45 * shared + 3.5 * tail) / Pairs<128>::kKeys));
 }
 
+// how a call is taken: pairs, or a prefix (stacked) and tails
+struct Division {
+  bool pairs, stacked;
+  int mode_p, mode_t;
+  Part prefix, tail;
+  int64_t shared;   // whole pages of the prefix, as far as the caller knows
+};
+Division divide(const PagedAttn& a) {
+  Division d{};
+  const int dt = a.p.dtype, kvh = a.p.n_kv_heads, group = a.heads / kvh;
+  const int64_t most = int64_t(a.p.max_blocks) * a.p.page_len;
+  const int64_t shared = d.shared = std::min<int64_t>(a.shared_len, most) / a.p.page_len * a.p.page_len;
+  const int rows_t = a.max_rows * group, rows_p = a.n * rows_t;
+  const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
+  d.mode_p = d.mode_t = mode_of(dt, rows_t, a.n, kvh);
+  // lengths of the tails: the longest, and half of it on average
+  const int64_t longest = std::max<int64_t>(1, keys - shared);
+  const double mean = std::max<int64_t>(0, keys - shared) / 2.0;
+  d.prefix = Part{1, 0, kTile};
+  d.tail = plan_part(d.mode_t, rows_t, a.n, kvh, std::max(keys, shared));
+  if (shared == 0) return d;
+  const Cost none{0, 0};
+  const double own = parts_us(a, d.mode_t, cost_of(a, d.mode_t, d.tail, a.n, shared + mean), none, d.tail.ranges);
+  const int mode = mode_of(dt, rows_p, 1, kvh);
+  const Part tail = plan_part(d.mode_t, rows_t, a.n, kvh, longest);
+  // what the tails take by themselves, at 5 TB/s
+  const double tail_us =
+      double(a.n) * tail.row_tiles * kvh * mean * 2 * a.p.head_dim * (dt == DLLM_BF16 ? 2 : 4) / 5e6;
+  const Part prefix = plan_part(mode, rows_p, 1, kvh, shared, tail_us);
+  const double parts = parts_us(a, d.mode_t, cost_of(a, mode, prefix, 1, double(shared)),
+                                cost_of(a, d.mode_t, tail, a.n, mean), prefix.ranges + tail.ranges);
+  // (of fewer rows than half a block most of a pair would be empty; a prefix
+  // in 16 rows over tails in 32, which only fp32 could ask for, has at least as
+  // many row tiles as the entries by themselves and costs more than they do)
+  d.pairs = dt == DLLM_BF16 && rows_t >= 16 && pairs_us(a, rows_t, shared, mean) < std::min(own, parts);
+  d.stacked = !d.pairs && parts < own && mode >= d.mode_t;
+  if (d.stacked) {
+    d.prefix = prefix;
+    d.tail = tail;
+    d.mode_p = mode;
+  }
+  return d;
+}
+
 }  // namespace
 
 hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
@@ -1167,51 +1209,41 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   j.a = a;
   j.scale_log2 = a.scale * 1.4426950408889634f;
   j.group = a.heads / a.p.n_kv_heads;
-  const int dt = a.p.dtype, kvh = a.p.n_kv_heads;
-  const int64_t most = int64_t(a.p.max_blocks) * a.p.page_len;
-  const int64_t shared = std::min<int64_t>(a.shared_len, most) / a.p.page_len * a.p.page_len;
-  const int rows_t = a.max_rows * j.group, rows_p = a.n * rows_t;
-  const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
-  const int mode_t = mode_of(dt, rows_t, a.n, kvh);
-  const int hd = a.p.head_dim;
-  // lengths of the tails: the longest, and half of it on average
-  const int64_t longest = std::max<int64_t>(1, keys - shared);
-  const double mean = std::max<int64_t>(0, keys - shared) / 2.0;
-  j.prefix = Part{1, 0, kTile};
-  j.tail = plan_part(mode_t, rows_t, a.n, kvh, std::max(keys, shared));
-  int mode_p = mode_t;
-  if (shared > 0) {
-    const Cost none{0, 0};
-    const double own = parts_us(a, mode_t, cost_of(a, mode_t, j.tail, a.n, shared + mean), none, j.tail.ranges);
-    const int mode = mode_of(dt, rows_p, 1, kvh);
-    const Part tail = plan_part(mode_t, rows_t, a.n, kvh, longest);
-    // what the tails take by themselves, at 5 TB/s
-    const double tail_us = double(a.n) * tail.row_tiles * kvh * mean * 2 * hd * (dt == DLLM_BF16 ? 2 : 4) / 5e6;
-    const Part prefix = plan_part(mode, rows_p, 1, kvh, shared, tail_us);
-    const double parts = parts_us(a, mode_t, cost_of(a, mode, prefix, 1, double(shared)),
-                                  cost_of(a, mode_t, tail, a.n, mean), prefix.ranges + tail.ranges);
-    // (of fewer rows than half a block most of a pair would be empty)
-    if (dt == DLLM_BF16 && rows_t >= 16 && pairs_us(a, rows_t, shared, mean) < std::min(own, parts)) {
-      j.direct = true;
-      const int grid = blocks_of(kvh, cdiv(a.n * cdiv(rows_t, 32), 2));
-      if (hd == 128) hipLaunchKernelGGL(pairs_kernel<128>, dim3(grid), dim3(Pairs<128>::kPairThreads), 0, s, j);
-      else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
-      return hipGetLastError();
-    }
-    j.stacked = parts < own;
-    if (j.stacked) {
-      j.prefix = prefix;
-      j.tail = tail;
-      mode_p = mode;
-    }
+  const Division d = divide(a);
+  const int kvh = a.p.n_kv_heads, hd = a.p.head_dim;
+  if (d.pairs) {
+    j.direct = true;
+    const int grid = blocks_of(kvh, cdiv(a.n * cdiv(a.max_rows * j.group, 32), 2));
+    if (hd == 128) hipLaunchKernelGGL(pairs_kernel<128>, dim3(grid), dim3(Pairs<128>::kPairThreads), 0, s, j);
+    else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
+    return hipGetLastError();
   }
-  if (shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
+  j.prefix = d.prefix;
+  j.tail = d.tail;
+  j.stacked = d.stacked;
+  if (d.shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
-  if (dt == DLLM_BF16)
-    a.p.head_dim == 128 ? launch<bf16_t, 128>(j, mode_p, mode_t, s) : launch<bf16_t, 64>(j, mode_p, mode_t, s);
+  if (a.p.dtype == DLLM_BF16)
+    hd == 128 ? launch<bf16_t, 128>(j, d.mode_p, d.mode_t, s) : launch<bf16_t, 64>(j, d.mode_p, d.mode_t, s);
   else
-    a.p.head_dim == 128 ? launch<float, 128>(j, mode_p, mode_t, s) : launch<float, 64>(j, mode_p, mode_t, s);
+    hd == 128 ? launch<float, 128>(j, d.mode_p, d.mode_t, s) : launch<float, 64>(j, d.mode_p, d.mode_t, s);
   return hipGetLastError();
+}
+
+kv_attention_plan paged_attention_plan(const PagedAttn& a) {
+  const Division d = divide(a);
+  kv_attention_plan p{};
+  p.way = d.pairs ? KV_WAY_PAIRS : d.stacked ? KV_WAY_PARTS : KV_WAY_ENTRIES;
+  if (d.pairs) return p;
+  if (d.stacked) {
+    p.prefix_rows = rows_of(d.mode_p);
+    p.prefix_ranges = d.prefix.ranges;
+    p.prefix_keys = d.prefix.range;
+  }
+  p.tail_rows = rows_of(d.mode_t);
+  p.tail_ranges = d.tail.ranges;
+  p.tail_keys = d.tail.range;
+  return p;
 }
 
 }  // namespace dllm
