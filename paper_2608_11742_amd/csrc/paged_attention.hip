@@ -8,7 +8,10 @@
 //   prefix   the positions that the whole batch shares.  The rows of all
 //            entries (and of the query heads of one key head) are stacked, so
 //            that a key tile is read once for all of them.
-//   tail     each entry's own positions after them, for its own rows.
+//   tail     each entry's own positions after them, for its own rows.  The
+//            tail of an entry that ends inside the prefix starts with the key
+//            range that it ends in: a weight of 0 would not cancel values past
+//            its end that are infinite or no number, and a tail's are cut there.
 // and each of the two over workgroups by ranges of keys, where there are few
 // rows.  Every range leaves a record per row, and a merge joins them in order;
 // with one range in all the workgroup writes the output itself.  Where the
@@ -98,6 +101,10 @@ __device__ __forceinline__ Entry entry_of(const PagedAttn& a, int b) {
   e.rows = a.n_rows ? min(max(a.n_rows[b], 0), a.max_rows) : a.max_rows;
   return e;
 }
+// of the `shared` positions, those that the entry takes with the others', which are in steps of `range`
+__device__ __forceinline__ int stacked_of(const Entry& e, int shared, int range) {
+  return e.held >= shared ? shared : e.held / range * range;
+}
 // positions that row i of the entry sees
 __device__ __forceinline__ int limit_of(const PagedAttn& a, const Entry& e, int i) {
   return a.causal ? max(0, min(e.held, e.held - e.rows + i + 1)) : e.held;
@@ -156,10 +163,10 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
   const Entry e = entry_of(a, b);
   w.row0 = b * per + it.tile * tile_rows;
   w.row_end = (b + 1) * per;
-  w.k0 = (j.stacked ? s : 0) + r * part.range;
+  w.k0 = (j.stacked ? stacked_of(e, s, j.prefix.range) : 0) + r * part.range;
   w.k1 = r + 1 == part.ranges ? e.held : min(w.k0 + part.range, e.held);
   w.part = j.prefix.ranges + r;
-  w.split = j.stacked ? 0 : s;
+  w.split = s;
   w.before = table_row(a, a.prefix_seq);
   w.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
   // an entry without positions still has its rows set to 0 where nothing is joined
@@ -782,7 +789,10 @@ struct Pairs {
     const Entry e = entry_of(a, b);
     Share prefix{}, tail{};
     prefix.before = prefix.after = table_row(a, a.prefix_seq);
-    tail.before = tail.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
+    const int own_from = __builtin_amdgcn_readfirstlane(stacked_of(e, s, kKeys));
+    tail.split = s;
+    tail.before = prefix.before;
+    tail.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
     const typename L::Copier copier(a, head, wave & 3, s), own_keys(a, head, 0, e.held);
     const int first = kTile * tile;   // of this wave's tile in a step
     const uint32_t lds0 = lds_address(smem) + tile * L::BYTES;
@@ -810,6 +820,7 @@ struct Pairs {
         copier.issue(k0 + kKeys + first, id, lds0 + (slot ^ 1) * (2 * L::BYTES));
         copier.pages_at(prefix, k0 + 2 * kKeys + first, id);
       }
+      if (k0 >= own_from) continue;   // the entry ends in this step, or before it
       const int h = way & 1, keys = k0 + 32 * way;
       u32x4 kf[1][L::QS], vf[2][L::NDB], pf[2];
       f32x16 sc[1];
@@ -830,7 +841,7 @@ struct Pairs {
 
     // this block's own keys
     const int pmask = a.p.page_len - 1;
-    for (int k0 = s + 32 * way; k0 < e.held; k0 += kKeys) {
+    for (int k0 = own_from + 32 * way; k0 < e.held; k0 += kKeys) {
       const int p0 = own_keys.in_pool(tail.page(k0, own_keys.shift, own_keys.last_block));
       const int p1 = own_keys.in_pool(tail.page(k0 + 16, own_keys.shift, own_keys.last_block));
       const int kr = L::key_of(fr);
@@ -955,7 +966,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   const int h = row % a.heads, t = row / a.heads, b = in ? t / a.max_rows : 0, i = t % a.max_rows;
   const Entry e = entry_of(a, b);
   const bool live = in && i < e.rows;
-  const int s = j.stacked ? shared_of(a) : 0, lim = limit_of(a, e, i);
+  const int s = j.stacked ? stacked_of(e, shared_of(a), j.prefix.range) : 0, lim = limit_of(a, e, i);
   const int np = live && j.prefix.ranges ? (min(lim, s) + j.prefix.range - 1) / j.prefix.range : 0;
   const int nt = live && lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
   const size_t stride = size_t(a.n) * a.max_rows * a.heads * record(HD);

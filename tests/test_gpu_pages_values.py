@@ -1,0 +1,81 @@
+"""Infinities and numbers that are none in keys and values of the paged cache:
+what a sequence does not hold may not reach it."""
+import pytest
+import torch
+
+from tests.pages_ways import WAYS, ENTRIES, division
+from tests.test_gpu_pages import hold, ints, new_pages, poison, queries
+from tests.test_gpu_pages_ways import TYPES, batch
+
+pytestmark = pytest.mark.gpu
+P = pytest.importorskip("paper_2608_11742_amd")
+
+DEV = "cuda:0"
+
+# entries by themselves, in 16, 32 and 128 rows
+ALONE = [
+    ("f32", 64, 16, 4, 2, 4, 5, 67, 60, ENTRIES, 0, 16, False, False),
+    ("bf16", 64, 32, 2, 2, 4, 6, 96, 40, ENTRIES, 0, 16, False, False),
+    ("bf16", 128, 16, 1, 1, 4, 20, 51, 42, ENTRIES, 0, 32, False, False),
+    ("bf16", 64, 16, 2, 2, 4, 70, 50, 120, ENTRIES, 0, 128, False, False),
+]
+
+
+def attention(kp, case, seqs, lens, q, counts, causal):
+    n, rows, heads = q.shape[:3]
+    out = torch.zeros(q.shape, dtype=q.dtype, device=DEV)
+    ws = torch.full((P.kv_pages_attention_workspace_bytes(kp, n, rows, heads),), 255, dtype=torch.uint8, device=DEV)
+    P.kv_pages_attention(kp, 1, ints(seqs), q, out, ws, n_rows=ints(counts), causal=causal, prefix_seq=0,
+                         shared_len=case[7], max_len=max(lens))
+    return out
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("what", ["inf", "nan"])
+@pytest.mark.parametrize("case", [c for c in WAYS + ALONE if c[5] >= 3 and c[7] >= 2 * c[2] + 4], ids=str)
+def test_prefix_past_the_end_of_a_shorter_entry(case, what, causal):
+    """Positions of the prefix past the end of the entries that end inside it:
+    what they hold may not reach those, however the call is divided."""
+    page, n, rows, prefix = case[2], case[5], case[6], case[7]
+    kp, seqs, lens = batch(case)
+    poison(kp)
+    assert division(P.kv_pages_attention_plan(kp, n, rows, case[3], prefix, max(lens))) == case[9:]
+    counts = [rows - i % 3 * (rows // 3) for i in range(n)]
+    q = queries(n, rows, case[3], case[1], TYPES[case[0]])
+    clean = attention(kp, case, seqs, lens, q, counts, causal)
+    assert clean.isfinite().all()
+    whole = prefix // page * page
+    short = lens[2]                                   # the shortest that is not empty
+    assert 0 < short < whole
+    table, bad = kp.table[0].tolist(), range(short, whole, 5)
+    at, slot = (torch.tensor(x, device=DEV) for x in ([table[pos // page] for pos in bad], [pos % page for pos in bad]))
+    kp.vt[:, at, :, :, slot] = float("-inf" if what == "inf" else "nan")
+    kp.vt[:, at[::2], :, :, slot[::2]] = float("inf" if what == "inf" else "nan")
+    if what == "nan":
+        kp.k[:, at, :, slot] = float("nan")
+    got = attention(kp, case, seqs, lens, q, counts, causal)
+    for b in range(n):
+        if lens[b] <= short:
+            assert torch.equal(got[b], clean[b]), b
+        elif not causal:                              # all others see them
+            assert not got[b, :counts[b]].isfinite().any(), b
+
+
+@pytest.mark.parametrize("dtype,rows,lens", [("bf16", 3, [40, 70]), ("bf16", 20, [300, 33]), ("bf16", 140, [500, 200]),
+                                             ("f32", 7, [90, 17])])
+def test_infinities_that_are_seen(dtype, rows, lens):
+    """An infinite value makes its dim infinite, with its sign, in every row of
+    the sequence, two of opposite signs make it no number; the other dims and
+    the other sequence are as they were."""
+    case = (dtype, 64, 16, 2, 2, 2, rows, 0, max(lens))
+    kp = hold(new_pages(pages=90, seqs=2, blocks=32, dtype=TYPES[dtype]), lens)
+    poison(kp)
+    q = queries(2, rows, 2, 64, TYPES[dtype])
+    want = attention(kp, case, [0, 1], lens, q, [rows] * 2, False)
+    table = kp.table[0].tolist()
+    for dim, value, pos in ((3, "inf", lens[0] - 1), (9, "-inf", 5), (20, "inf", lens[0] // 2), (20, "-inf", 0)):
+        kp.vt[1, table[pos // 16], :, dim, pos % 16] = float(value)
+    got = attention(kp, case, [0, 1], lens, q, [rows] * 2, False)
+    want[0, :, :, 3], want[0, :, :, 9], want[0, :, :, 20] = float("inf"), float("-inf"), float("nan")
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got.nan_to_num(nan=0.0, posinf=1e9, neginf=-1e9), want.nan_to_num(nan=0.0, posinf=1e9, neginf=-1e9))
