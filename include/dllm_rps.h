@@ -334,7 +334,8 @@ dllm_status kv_pages_compact(const dllm_kv_pages* pages, int32_t* n_used, void* 
 /* Keys and values of the last n_rows[b] positions of sequence seqs[b] into
  * their pages of one layer (n_rows NULL: max_rows each; outside 0 .. max_rows:
  * clamped), 1 <= n <= KV_MAX_SEQS.  k (post-RoPE) and v have n_kv_heads heads
- * and the model's type.  Row i is position len - n_rows[b] + i.  Not written:
+ * and the model's type; values of bf16 models are saturated to +-65504, a NaN
+ * stays one.  Row i is position len - n_rows[b] + i.  Not written:
  * rows of a sequence outside 0 .. max_seqs-1, rows before position 0 and rows
  * whose page another sequence holds too.  Of a sequence listed twice the last
  * entry is written. */

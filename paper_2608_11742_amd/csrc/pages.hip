@@ -431,6 +431,17 @@ __global__ __launch_bounds__(kCopyThreads) void compact_apply_kernel(dllm_kv_pag
 constexpr int kWriteThreads = 256;
 constexpr int kWriteTile = 64;   // positions per workgroup, from a multiple of 64: pages are cut there too
 
+// values as the pages of bf16 models hold them: rounded to binary16, past its
+// range the largest of their sign (what saturating first gives), a NaN as it is
+// (the median that saturates elsewhere returns the lowest of the others for one)
+__device__ __forceinline__ uint32_t pack_values(float a, float b) {
+  typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+  const half2v most = {65504, 65504}, v = __builtin_bit_cast(half2v, pack_f16x2(a, b));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_maximum(__builtin_elementwise_minimum(v, most), -most));
+}
+__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_value(bf16_t* p, float v) { p->bits = uint16_t(pack_values(v, 0.f)); }
+
 __device__ __forceinline__ int row_count(const int32_t* n_rows, int b, int max_rows) {
   return n_rows ? min(max(n_rows[b], 0), max_rows) : max_rows;
 }
@@ -530,7 +541,7 @@ __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(dllm_kv_page
       if (full) {
         if constexpr (sizeof(TV) == 2) {
           *reinterpret_cast<u32x4*>(dst) =
-              u32x4{pack_vt2(x[0], x[1]), pack_vt2(x[2], x[3]), pack_vt2(x[4], x[5]), pack_vt2(x[6], x[7])};
+              u32x4{pack_values(x[0], x[1]), pack_values(x[2], x[3]), pack_values(x[4], x[5]), pack_values(x[6], x[7])};
         } else {
           reinterpret_cast<f32x4*>(dst)[0] = f32x4{x[0], x[1], x[2], x[3]};
           reinterpret_cast<f32x4*>(dst)[1] = f32x4{x[4], x[5], x[6], x[7]};
@@ -538,7 +549,7 @@ __global__ __launch_bounds__(kWriteThreads) void pages_write_kernel(dllm_kv_page
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (at + i >= from - t0 && at + i < to - t0) store_vt(dst + i, x[i]);
+          if (at + i >= from - t0 && at + i < to - t0) store_value(dst + i, x[i]);
       }
     }
   }

@@ -79,3 +79,23 @@ def test_infinities_that_are_seen(dtype, rows, lens):
     want[0, :, :, 3], want[0, :, :, 9], want[0, :, :, 20] = float("inf"), float("-inf"), float("nan")
     assert torch.equal(got.isnan(), want.isnan())
     assert torch.equal(got.nan_to_num(nan=0.0, posinf=1e9, neginf=-1e9), want.nan_to_num(nan=0.0, posinf=1e9, neginf=-1e9))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 5, 40])
+def test_write_keeps_what_is_no_number(dtype, rows):
+    """Values go in as they are, binary16 saturated for bf16; a NaN stays one."""
+    kp = hold(new_pages(pages=20, heads=2, seqs=2, blocks=8, dtype=TYPES[dtype]), [rows + 3, rows + 8])
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.empty(2, rows, 2, 64, dtype=TYPES[dtype], device=DEV).normal_(generator=g) for _ in range(2))
+    special = [float("nan"), float("inf"), float("-inf"), 1e6, -1e6, 65504.0, -65504.0, 0.0, 65536.0, 1e-7, -1e-6, -1e-9]
+    v[:, :, 0, :12] = torch.tensor(special, device=DEV).to(TYPES[dtype])
+    v[0, rows // 2, 1, 5] = k[0, rows // 2, 1, 6] = float("nan")
+    P.kv_pages_write(kp, 1, ints([0, 1]), k, v)
+    for s, m in enumerate([rows + 3, rows + 8]):
+        pos = torch.arange(m - rows, m)
+        page, slot = kp.table[s].cpu().long()[pos // 16], pos % 16
+        got, keys = kp.vt[1, page.to(DEV), :, :, slot.to(DEV)], kp.k[1, page.to(DEV), :, slot.to(DEV)]
+        want = v[s].float().clamp(-65504, 65504).half() if dtype == "bf16" else v[s]
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+        assert torch.equal(keys.isnan(), k[s].isnan()) and torch.equal(keys.nan_to_num(nan=0.0), k[s].nan_to_num(nan=0.0))
