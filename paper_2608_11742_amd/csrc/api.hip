@@ -877,6 +877,39 @@ dllm_status check_rows(const dllm_rows* r, int dtype, const char* who, const cha
 
 constexpr int kMaxBatchRows = 1 << 20;   // rows of one entry
 
+// Whether two of the n * rows * heads rows of hd elements share one.  Strides
+// that nest (each at least what the smaller ones reach over) cannot; for others
+// the distances of all pairs are gone through: of two dims one by one, of the
+// third the nearest multiple (at most 2^19 steps, as the sizes' product is at most 2^26).
+bool rows_overlap(const dllm_rows& r, int n, int rows, int heads, int64_t hd) {
+  struct Dim {
+    int64_t stride, size;
+  } d[3] = {{r.seq, n}, {r.row, rows}, {r.head, heads}};
+  for (Dim& x : d)
+    if (x.size == 1) x.stride = 0;
+  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  int64_t reach = hd;
+  bool nested = true;
+  for (const Dim& x : d) {
+    nested = nested && (x.size == 1 || x.stride >= reach);
+    reach += x.stride * (x.size - 1);
+  }
+  if (nested) return false;
+  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.size < b.size; });
+  const Dim &a = d[0], &b = d[1], &c = d[2];
+  for (int64_t i = 0; i < a.size; ++i)
+    for (int64_t j = i ? 1 - b.size : 0; j < b.size; ++j) {
+      const int64_t t = i * a.stride + j * b.stride;   // k of the third: |t - k stride| < hd, not all of i, j, k 0
+      if (c.stride == 0) {
+        if (std::abs(t) < hd && (i || j || c.size > 1)) return true;
+        continue;
+      }
+      for (int64_t k = t / c.stride - 1; k <= t / c.stride + 1; ++k)
+        if (std::abs(k) < c.size && (i || j || k) && std::abs(t - k * c.stride) < hd) return true;
+    }
+  return false;
+}
+
 }  // namespace
 
 dllm_status kv_pages_init(const dllm_kv_pages* pages, dllm_stream stream) {
@@ -984,6 +1017,7 @@ dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const 
   if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "kv_pages_attention: ws NULL or not 16-byte aligned");
   const size_t need = paged_attention_workspace(*pages, n, max_rows, n_heads);
   if (ws_bytes < need) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, need);
+  if (rows_overlap(*out, n, max_rows, n_heads, hd)) return fail(DLLM_ESHAPE, "kv_pages_attention: rows of out overlap");
   PagedAttn a{};
   a.p = *pages;
   a.layer = layer;

@@ -99,3 +99,25 @@ def test_write_keeps_what_is_no_number(dtype, rows):
         want = v[s].float().clamp(-65504, 65504).half() if dtype == "bf16" else v[s]
         assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
         assert torch.equal(keys.isnan(), k[s].isnan()) and torch.equal(keys.nan_to_num(nan=0.0), k[s].nan_to_num(nan=0.0))
+
+
+@pytest.mark.parametrize("sizes,strides", [
+    ((2, 2, 1), (128, 192, 0)),           # entries and rows between one another, none on another
+    ((2, 3, 2), (64, 256, 128)),          # entries innermost
+    ((3, 2, 2), (192, 576, 64)),          # heads, entries, rows
+    ((2, 5, 2), (320, 64, 640)),          # rows innermost
+    ((2, 2, 2), (136, 208, 416)),         # gaps
+])
+def test_rows_of_any_order_that_do_not_overlap(sizes, strides):
+    n, rows, heads = sizes
+    kp = hold(new_pages(seqs=3, pages=60, blocks=20, heads=1), [300, 64, 290])
+    q = queries(n, rows, heads, 64, torch.bfloat16)
+    case = (0,) * 7 + (0,)
+    want = attention(kp, case, list(range(n)), [300], q, [rows] * n, False)
+    buf = torch.full((4096,), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = buf.as_strided((n, rows, heads, 64), (*strides, 1))
+    ws = torch.empty(P.kv_pages_attention_workspace_bytes(kp, n, rows, heads), dtype=torch.uint8, device=DEV)
+    P.kv_pages_attention(kp, 1, ints(list(range(n))), q, out, ws, max_len=300)
+    assert torch.equal(out, want)
+    out.fill_(7.0)
+    assert bool((buf == 7).all())
