@@ -263,8 +263,8 @@ dllm_status vocab_entropy_topk_noalloc(const void* hidden, const void* w_lm, int
  * The caller allocates the arrays (k and vt 16-byte aligned) and calls
  * kv_pages_init once.  A page that is not full is held by one sequence only.
  * Requirements: head_dim in {64, 128}, page_len in {16, 32, 64, 128, 256},
- * n_pages <= KV_MAX_PAGES, max_seqs <= KV_MAX_SEQS, n_kv_heads <= 1024,
- * max_blocks * page_len <= KV_MAX_POSITIONS.
+ * n_pages <= KV_MAX_PAGES, max_seqs <= KV_MAX_SEQS, n_kv_heads <= KV_MAX_HEADS,
+ * n_layers <= KV_MAX_LAYERS, max_blocks * page_len <= KV_MAX_POSITIONS.
  *
  * Workspaces are 16-byte aligned.
  *
@@ -274,6 +274,10 @@ dllm_status vocab_entropy_topk_noalloc(const void* hidden, const void* w_lm, int
 #define KV_MAX_PAGES (1 << 20)
 #define KV_MAX_SEQS 1024
 #define KV_MAX_POSITIONS (1 << 30)
+#define KV_MAX_HEADS 1024
+#define KV_MAX_LAYERS 65536
+#define KV_MAX_ROWS (1 << 20)         /* rows of one entry of a batch */
+#define KV_MAX_HEAD_ROWS (1 << 26)    /* entries * rows * query heads of an attention */
 enum {
     KV_PAGES_OK = 0,
     KV_PAGES_ESEQ = 1,      /* a sequence outside 0 .. max_seqs-1, listed twice, or a fork's target not empty */
@@ -294,7 +298,7 @@ typedef struct {
 
 /* Rows of a batch: row i of entry b and head h starts at element
  * b * seq + i * row + h * head of p and holds head_dim contiguous elements.
- * p and the strides (in bytes) are multiples of 16; strides are >= 0. */
+ * p and the strides (in bytes) are multiples of 16; strides are 0 .. 2^40. */
 typedef struct {
     void* p;
     int64_t seq, row, head;
@@ -333,12 +337,12 @@ dllm_status kv_pages_compact(const dllm_kv_pages* pages, int32_t* n_used, void* 
 
 /* Keys and values of the last n_rows[b] positions of sequence seqs[b] into
  * their pages of one layer (n_rows NULL: max_rows each; outside 0 .. max_rows:
- * clamped), 1 <= n <= KV_MAX_SEQS.  k (post-RoPE) and v have n_kv_heads heads
- * and the model's type; values of bf16 models are saturated to +-65504, a NaN
- * stays one.  Row i is position len - n_rows[b] + i.  Not written:
- * rows of a sequence outside 0 .. max_seqs-1, rows before position 0 and rows
- * whose page another sequence holds too.  Of a sequence listed twice the last
- * entry is written. */
+ * clamped), 1 <= n <= KV_MAX_SEQS, 1 <= max_rows <= KV_MAX_ROWS.  k (post-RoPE)
+ * and v have n_kv_heads heads and the model's type; values of bf16 models are
+ * saturated to +-65504, a NaN stays one.  Row i is position len - n_rows[b] +
+ * i.  Not written: rows of a sequence outside 0 .. max_seqs-1, rows before
+ * position 0 and rows whose page another sequence holds too.  Of a sequence
+ * listed twice the last entry is written. */
 dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
                            int32_t max_rows, const int32_t* n_rows, const dllm_rows* k, const dllm_rows* v,
                            dllm_stream stream);
@@ -346,11 +350,12 @@ dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int3
 /* Attention of a batch over one layer of its pages, the prefix that the batch
  * shares computed once for all: softmax(scale q k^T) v for n_rows[b] rows of
  * entry b (n_rows as in kv_pages_write) over the positions of sequence
- * seqs[b]; 1 <= n <= KV_MAX_SEQS, 1 <= max_rows.
- *   q, out       rows of n_heads heads, a multiple of n_kv_heads: head h reads
- *                key head h / (n_heads / n_kv_heads).  out rows from n_rows[b]
- *                on are left as they were; out and q do not overlap, and no
- *                two rows of out do.
+ * seqs[b]; 1 <= n <= KV_MAX_SEQS, 1 <= max_rows <= KV_MAX_ROWS,
+ * n * max_rows * n_heads <= KV_MAX_HEAD_ROWS, 0 < scale < infinity.
+ *   q, out       rows of n_heads heads, a multiple of n_kv_heads and at most
+ *                KV_MAX_HEADS: head h reads key head h / (n_heads /
+ *                n_kv_heads).  out rows from n_rows[b] on are left as they
+ *                were; out and q do not overlap, and no two rows of out do.
  *   prefix_seq, shared_len   the whole pages among the first min(shared_len,
  *                len[prefix_seq]) positions of sequence prefix_seq (a host
  *                value) are read from its table for every entry, once for the
@@ -393,11 +398,13 @@ dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32
  * entry b is position len - seq + i of sequence seqs[b] (the last seq
  * positions it holds, so it is grown by seq first; position ids are clamped to
  * 0 .. max_pos-1).  In every layer the rows' keys and values are written as by
- * kv_pages_write and the rows attend, not causally, to all positions of their
- * sequence as by kv_pages_attention (prefix_seq, shared_len and max_len as
- * there).  kv_pages_free with keep takes the positions back.
+ * kv_pages_write (values as in dllm_kv_cache) and the rows attend, not
+ * causally, to all positions of their sequence as by kv_pages_attention
+ * (prefix_seq, shared_len and max_len as there).  kv_pages_free with keep takes
+ * the positions back.
  *   pages    of the model's type, layers, heads and head_dim.
- *   seqs     [batch] int32, batch <= KV_MAX_SEQS.
+ *   seqs     [batch] int32, batch <= KV_MAX_SEQS,
+ *            batch * seq * n_heads <= KV_MAX_HEAD_ROWS.
  *   lm_pos   [n_lm_pos] rows of an entry (0 .. seq-1); row_scale [seq] too.
  *   Other arguments and the output as dllm_forward. */
 size_t dllm_workspace_bytes_pages(const dllm_model* m, int32_t batch, int32_t seq, int32_t n_lm_pos);

@@ -132,6 +132,7 @@ SCHED_TOP_CONFIDENCE, SCHED_LOW_ENTROPY = 0, 1
 KV_PAGES_OK, KV_PAGES_ESEQ, KV_PAGES_ELEN, KV_PAGES_ESHARED, KV_PAGES_EFULL = 0, 1, 2, 3, 4
 KV_WAY_ENTRIES, KV_WAY_PARTS, KV_WAY_PAIRS = 0, 1, 2
 KV_MAX_PAGES, KV_MAX_SEQS, KV_MAX_POSITIONS = 1 << 20, 1024, 1 << 30
+KV_MAX_HEADS, KV_MAX_LAYERS, KV_MAX_ROWS, KV_MAX_HEAD_ROWS = 1024, 65536, 1 << 20, 1 << 26
 
 
 def load(path: str = LIB_PATH):

@@ -848,7 +848,7 @@ dllm_status check_pages(const dllm_kv_pages* p, const char* who) {
     return fail(DLLM_ESHAPE, "%s: head_dim %d not in {64, 128}", who, p->head_dim);
   if (p->page_len < 16 || p->page_len > 256 || (p->page_len & (p->page_len - 1)))
     return fail(DLLM_ESHAPE, "%s: page_len %d not in {16, 32, 64, 128, 256}", who, p->page_len);
-  if (p->n_layers < 1 || p->n_layers > 65536 || p->n_kv_heads < 1 || p->n_kv_heads > 1024 || p->n_pages < 1 ||
+  if (p->n_layers < 1 || p->n_layers > KV_MAX_LAYERS || p->n_kv_heads < 1 || p->n_kv_heads > KV_MAX_HEADS || p->n_pages < 1 ||
       p->n_pages > KV_MAX_PAGES || p->max_seqs < 1 || p->max_seqs > KV_MAX_SEQS || p->max_blocks < 1 ||
       p->max_blocks > KV_MAX_POSITIONS / p->page_len)
     return fail(DLLM_ESHAPE, "%s: %d layers, %d pages, %d heads, %d sequences of %d pages", who, p->n_layers,
@@ -874,8 +874,6 @@ dllm_status check_rows(const dllm_rows* r, int dtype, const char* who, const cha
     return fail(DLLM_EINVAL, "%s: %s needs 16-byte aligned rows", who, name);
   return DLLM_OK;
 }
-
-constexpr int kMaxBatchRows = 1 << 20;   // rows of one entry
 
 // Whether two of the n * rows * heads rows of hd elements share one.  Strides
 // that nest (each at least what the smaller ones reach over) cannot; for others
@@ -970,7 +968,7 @@ dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int3
   if (st == DLLM_OK) st = check_rows(v, pages->dtype, "kv_pages_write", "v");
   if (st != DLLM_OK) return st;
   if (layer < 0 || layer >= pages->n_layers) return fail(DLLM_ESHAPE, "kv_pages_write: layer %d", layer);
-  if (max_rows < 1 || max_rows > kMaxBatchRows) return fail(DLLM_ESHAPE, "kv_pages_write: max_rows %d", max_rows);
+  if (max_rows < 1 || max_rows > KV_MAX_ROWS) return fail(DLLM_ESHAPE, "kv_pages_write: max_rows %d", max_rows);
   return hip_check(pages_write(*pages, layer, seqs, n, max_rows, n_rows, *k, *v, static_cast<hipStream_t>(stream)),
                    "kv_pages_write");
 }
@@ -982,10 +980,10 @@ dllm_status check_attention(const dllm_kv_pages* pages, int32_t n, int32_t max_r
   dllm_status st = check_pages(pages, who);
   if (st != DLLM_OK) return st;
   if (n < 1 || n > KV_MAX_SEQS) return fail(DLLM_ESHAPE, "%s: %d entries outside 1..%d", who, n, KV_MAX_SEQS);
-  if (max_rows < 1 || max_rows > kMaxBatchRows) return fail(DLLM_ESHAPE, "%s: max_rows %d", who, max_rows);
-  if (n_heads < 1 || n_heads > 1024 || n_heads % pages->n_kv_heads)
+  if (max_rows < 1 || max_rows > KV_MAX_ROWS) return fail(DLLM_ESHAPE, "%s: max_rows %d", who, max_rows);
+  if (n_heads < 1 || n_heads > KV_MAX_HEADS || n_heads % pages->n_kv_heads)
     return fail(DLLM_ESHAPE, "%s: %d heads over %d key heads", who, n_heads, pages->n_kv_heads);
-  if (int64_t(n) * max_rows * n_heads > (int64_t(1) << 26))
+  if (int64_t(n) * max_rows * n_heads > KV_MAX_HEAD_ROWS)
     return fail(DLLM_ESHAPE, "%s: %d x %d rows of %d heads", who, n, max_rows, n_heads);
   return DLLM_OK;
 }

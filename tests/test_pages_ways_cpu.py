@@ -82,3 +82,28 @@ def test_plan_refusals(abi):
     assert ask(n=0) == 2 and ask(n=1025) == 2 and ask(rows=0) == 2 and ask(heads=3) == 2
     assert ask(shared=-1) == 2 and ask(most=-1) == 2
     assert lib.kv_pages_attention_plan(None, 2, 3, 4, 16, 64, C.byref(plan)) == 1
+
+
+def test_limits_of_the_header(abi):
+    """Every KV_MAX_ number of the header is the binding's, and is the last value that is taken."""
+    import re
+    _abi, lib = abi
+    text = open(os.path.join(ROOT, "include", "dllm_rps.h")).read()
+    limits = {k: eval(v) for k, v in re.findall(r"#define (KV_MAX_\w+) +([()\d <]+\d\)?)", text)}
+    assert len(limits) == 7
+    for name, value in limits.items():
+        assert getattr(_abi, name) == value, name
+
+    def ask(n=1, rows=1, heads=1, kv=1, **kw):
+        p = pages(_abi, "bf16", 64, 16, kv, 8)
+        for field, value in kw.items():
+            setattr(p, field, value)
+        return lib.kv_pages_attention_plan(C.byref(p), n, rows, heads, 0, 64, C.byref(_abi.AttentionPlan()))
+
+    for kw in [dict(n=1024), dict(rows=1 << 20), dict(heads=1024), dict(heads=1024, kv=1024), dict(n_pages=1 << 20),
+               dict(max_seqs=1024), dict(n_layers=65536), dict(max_blocks=1 << 26), dict(n=64, rows=1 << 20),
+               dict(n=1024, rows=64, heads=1024)]:
+        assert ask(**kw) == 0, kw
+        name, value = list(kw.items())[-1]
+        over = {**kw, name: value + 1}
+        assert ask(**over) == 2, over
