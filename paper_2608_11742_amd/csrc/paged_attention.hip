@@ -1020,11 +1020,13 @@ constexpr int kMaxRanges = 64;
 
 // How `groups` sets of stacked rows per key head are taken.  fp32 products
 // cost an eighth of the bf16 rate, so there 32 rows, which halve what is
-// read, are only worth it where 16 fill the chip twice over (1000 positions, 16
-// key heads of 64, 16 / 32 rows a workgroup: 16 x 32 rows 32 us / 34, 16 x 64
-// 57 / 49).  bf16 takes the wide kernel from 33 rows on (narrow / wide: 8 x 40
-// rows over 1000 positions 39 us / 34, 16 x 48 over 2000 143 / 113, but 4 x 64
-// over 300 12 / 14).
+// read, are only taken where 16 fill the chip twice over (1000 positions, 16
+// key heads of 64, 16 / 32 rows a workgroup: 8 x 32 rows 21 us / 24, 16 x 64
+// 65 / 51, 32 x 32 67 / 53; at 16 x 32, which fill it once, 37 / 29, so there
+// the border lies too high).  bf16 takes the wide kernel from 33 rows on
+// (narrow / wide, 32 heads of 128: 8 x 40 rows over 1000 positions 39 us / 32,
+// 16 x 48 over 2000 140 / 103, 16 x 33 over 1000 69 / 52, but 4 x 64 over 300 12
+// / 14 and 4 x 33 over 1000 22 / 24: few rows over few keys lose 2 us to it).
 int mode_of(int dtype, int rows, int64_t groups, int kv_heads) {
   if (dtype == DLLM_BF16) return rows > kNarrowRows ? ROWS128 : rows > 16 ? ROWS32 : ROWS16;
   return rows > 16 && cdiv(rows, 16) * groups * kv_heads >= 4 * kCus ? ROWS32 : ROWS16;
@@ -1037,21 +1039,25 @@ int64_t most_ranges(int mode, int64_t items) {
   return std::min<int64_t>(kMaxRanges, (wgs + items - 1) / items);
 }
 
-constexpr int kStep = kWaves * kTile;   // keys that a narrow workgroup takes at a time, about 1 us
+// the unit in which plan_part counts: what a narrow workgroup of 16 bf16 rows
+// (of heads of 64: 32 too) takes at a time; fp32 and wider ones take a half or a
+// quarter of it a step (Narrow::KS)
+constexpr int kStep = kWaves * kTile;
 
 // Rows stacked per key head, in `groups` separate sets (entries of a tail).
 // Two workgroups fit a CU.  Narrow parts are bound by memory: as many ranges
 // as fill the chip, and where they are long ones of 24 tiles, so that batches
 // of unlike lengths come out even.  Joining them costs 3 us, so parts of up to
-// two steps are not divided, nor parts of up to six that have a workgroup for
-// every CU (single tokens of 8 key heads: 8 over 500 positions whole 11.7 us,
-// over 520 divided 12.2, over 1000 whole 19.2, divided 13.2; 32 over 1000 23.5
-// and 26.7, over 1500 33.3 and 36.0).
+// two kStep are not divided, nor parts of up to six that have a workgroup for
+// every CU (single tokens of 8 key heads, whole / divided: 8 over 500 positions
+// 11.8 us / 12.6, over 520 13.3 / 13.0, over 1000 19.4 / 13.3; 1 over 1000 18.6 /
+// 11.6; 32 over 600 17.0 / 20.5, over 1000 23.1 / 26.9, over 1500 32.0 / 35.7).
 // Wide ones take one workgroup a CU, which leaves the other slot to the tails,
 // and two where ranges stay long enough for the second to gain more than its
 // records cost to join; beside tails that take `beside_us` by themselves, only
 // as many as end by then (14 us and 1.2 us a tile: 64 single tokens over 8000
-// shared positions and up to 1500 of their own, 16 ranges 60 us, 8 ranges 49).
+// shared positions and up to 1500 of their own, 16 ranges 58 us, 8 ranges 47, the
+// rule's 6 50, 4 ranges 62).
 Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys, double beside_us = 0.0) {
   Part p;
   p.row_tiles = cdiv(rows, rows_of(mode));
@@ -1128,14 +1134,14 @@ namespace {
 // Three ways to take a batch over a shared prefix: every entry by itself, from
 // position 0 on; the prefix and the tails as parts, joined; pairs.  The one of the
 // least estimated time is taken (measured, us, heads of 128, entries / parts /
-// pairs: 32 heads, 16 x 32 rows over 64 positions 10.4 / 21.8 / 10.8, over 256
-// 16.4 / 22.8 / 12.1, over 1024 38 / 31 / 21, over 8000 - / 96 / 96, over 30000
-// 1013 / 321 / 380; 16 x 128 over 1024 53 / 83 / 83; 16 x 40 over 128 15 / 28 /
-// 20, over 4096 147 / 86 / 102; 64 x 32 over 64 32 / 60 / 41, over 4096 461 / 186
-// / 203; 8 key heads, 32 single tokens over 500 13.7 / 19.0, over 1000 20.9 /
-// 16.8; fp32, 16 heads of 64, 7 x 19 over 203 10.0 / 13.4, 7 x 4 over 1000 18.5 /
-// 12.6).  Of 118 batches of this kind all but a few were within 10% of the best
-// of the three.
+// pairs: 32 heads, 16 x 32 rows over 64 positions 10.5 / 22.4 / 11.3, over 128
+// 12.8 / 21.8 / 10.6, over 1024 38 / 31 / 22, over 8000 247 / 98 / 97, over 30000
+// 1000 / 313 / 366; 16 x 128 over 1024 53 / 83 / 81; 16 x 40 over 128 15 / 28 /
+// 19, over 4096 151 / 87 / 106; 64 x 32 over 64 32 / 61 / 43, over 4096 462 / 200
+// / 204; 8 key heads, 32 single tokens over 500 19.6 / 22.4, over 1000 26.2 /
+// 20.6; fp32, 16 heads of 64, 7 x 19 over 203 10.3 / 13.8, 7 x 4 over 1000 19.7 /
+// 14.4).  Of 92 batches of this kind all but three were within 10% of the best
+// of the three, those within 16%.
 //
 // Estimated times, in us on a whole MI355X:
 //   work   of a part where the chip is full of it: keys and values of narrow

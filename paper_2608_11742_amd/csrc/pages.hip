@@ -452,7 +452,7 @@ __device__ __forceinline__ int row_count(const int32_t* n_rows, int b, int max_r
 // up once, by the first lanes.  With kT the values come transposed ([dim][row],
 // v.row elements a dim) in the type of the pages and are only shifted into place.
 // Bound by memory: 16 x 512 rows of 32 heads of 128, 268 MB read and written, in
-// 54 us, 64 x 512 in 257 (4.2 TB/s).  A sequence's rows take one tile more than
+// 55 us, 64 x 512 in 257 (4.2 TB/s).  A sequence's rows take one tile more than
 // they fill if they start inside one.  Workgroups go to the 8 XCDs in turn: with
 // the tiles of a head first, the second of two would leave every other XCD idle,
 // so there the heads come first (64 x 32 rows 26 us -> 21, 64 x 64 equal); with
