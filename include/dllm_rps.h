@@ -355,7 +355,8 @@ dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int3
  *   q, out       rows of n_heads heads, a multiple of n_kv_heads and at most
  *                KV_MAX_HEADS: head h reads key head h / (n_heads /
  *                n_kv_heads).  out rows from n_rows[b] on are left as they
- *                were; out and q do not overlap, and no two rows of out do.
+ *                were; out and q do not overlap, and no two rows that are
+ *                written do.
  *   prefix_seq, shared_len   the whole pages among the first min(shared_len,
  *                len[prefix_seq]) positions of sequence prefix_seq (a host
  *                value) are read from its table for every entry, once for the

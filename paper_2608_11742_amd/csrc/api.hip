@@ -1015,7 +1015,9 @@ dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const 
   if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "kv_pages_attention: ws NULL or not 16-byte aligned");
   const size_t need = paged_attention_workspace(*pages, n, max_rows, n_heads);
   if (ws_bytes < need) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, need);
-  if (rows_overlap(*out, n, max_rows, n_heads, hd)) return fail(DLLM_ESHAPE, "kv_pages_attention: rows of out overlap");
+  // which rows of ragged entries are written is known on the device alone
+  if (!n_rows && rows_overlap(*out, n, max_rows, n_heads, hd))
+    return fail(DLLM_ESHAPE, "kv_pages_attention: rows of out overlap");
   PagedAttn a{};
   a.p = *pages;
   a.layer = layer;

@@ -121,3 +121,18 @@ def test_rows_of_any_order_that_do_not_overlap(sizes, strides):
     assert torch.equal(out, want)
     out.fill_(7.0)
     assert bool((buf == 7).all())
+
+
+@pytest.mark.parametrize("hd,rows", [(64, 5), (128, 40)])
+def test_ragged_rows_one_after_another(hd, rows):
+    """Entries closer to one another than max_rows: their n_rows rows fill the output without a gap."""
+    kp = hold(new_pages(seqs=3, pages=60, blocks=20, heads=1, hd=hd), [300, 64, 290])
+    q = queries(3, rows, 2, hd, torch.bfloat16)
+    counts = [rows // 2] * 3
+    want = attention(kp, (0,) * 8, [0, 1, 2], [300], q, counts, True)[:, :rows // 2]
+    buf = torch.full((3 * rows * 2 * hd,), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = buf.as_strided((3, rows, 2, hd), (rows // 2 * 2 * hd, 2 * hd, hd, 1))
+    ws = torch.empty(P.kv_pages_attention_workspace_bytes(kp, 3, rows, 2), dtype=torch.uint8, device=DEV)
+    P.kv_pages_attention(kp, 1, ints([0, 1, 2]), q, out, ws, n_rows=ints(counts), causal=True, max_len=300)
+    m = want.numel()
+    assert torch.equal(buf[:m].view_as(want), want) and bool((buf[m:] == 7).all())

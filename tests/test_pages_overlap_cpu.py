@@ -21,11 +21,11 @@ def attend():
     lib = _abi.load()
     p = _abi.KvPagesC(FAKE, FAKE, FAKE, FAKE, FAKE, 2, 10, 1, 64, 16, 4, 8, 1)
 
-    def call(n, rows, heads, seq, row, head):
+    def call(n, rows, heads, seq, row, head, n_rows=None):
         q, out = _abi.Rows(FAKE, 1 << 20, 1 << 10, 64), _abi.Rows(FAKE, seq, row, head)
         ws = lib.kv_pages_attention_workspace_bytes(C.byref(p), n, rows, heads)
         assert ws > 0
-        status = lib.kv_pages_attention(C.byref(p), 0, FAKE, n, rows, None, heads, C.byref(q), C.byref(out), 0, 0, 64,
+        status = lib.kv_pages_attention(C.byref(p), 0, FAKE, n, rows, n_rows, heads, C.byref(q), C.byref(out), 0, 0, 64,
                                         0, 1.0, FAKE, ws, None)
         return status, lib.dllm_last_error()
 
@@ -52,6 +52,12 @@ def test_overlapping_rows_are_refused(attend, n, rows, heads, seq, row, head):
     assert status == 2 and b"overlap" in text
     if n * rows * heads < 1 << 17:
         assert overlap(n, rows, heads, seq, row, head)
+
+
+def test_heads_of_ragged_entries(attend):
+    """Which rows n_rows lets be written is known on the device: heads that overlap can be told."""
+    for n, rows, heads, seq, row, head in [(2, 4, 4, 1024, 512, 56), (1, 1, 2, 64, 64, 8)]:
+        assert attend(n, rows, heads, seq, row, head, FAKE)[0] == 2
 
 
 def test_random_overlapping_rows_are_refused(attend):
