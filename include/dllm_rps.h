@@ -278,12 +278,14 @@ dllm_status vocab_entropy_topk_noalloc(const void* hidden, const void* w_lm, int
 #define KV_MAX_LAYERS 65536
 #define KV_MAX_ROWS (1 << 20)         /* rows of one entry of a batch */
 #define KV_MAX_HEAD_ROWS (1 << 26)    /* entries * rows * query heads of an attention */
+#define KV_TREE_MAX_ROWS 1024         /* rows of a tree of drafted tokens, and of a path through it */
 enum {
     KV_PAGES_OK = 0,
     KV_PAGES_ESEQ = 1,      /* a sequence outside 0 .. max_seqs-1, listed twice, or a fork's target not empty */
     KV_PAGES_ELEN = 2,      /* a negative count, more than max_blocks pages, or more positions than are held */
     KV_PAGES_ESHARED = 3,   /* a cut inside a page that another sequence holds too */
-    KV_PAGES_EFULL = 4      /* fewer free pages than needed */
+    KV_PAGES_EFULL = 4,     /* fewer free pages than needed */
+    KV_PAGES_EPATH = 5      /* a path that does not ascend within its rows */
 };
 
 typedef struct {
@@ -393,6 +395,123 @@ typedef struct {
 } kv_attention_plan;
 dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
                                     int32_t shared_len, int32_t max_len, kv_attention_plan* plan);
+
+/* ------------------------------------------------- rotary positions, drafts
+ *
+ * Models whose queries and keys are normed by head, rotated in part, in pairs
+ * or at scaled frequencies, and tokens that are drafted as a tree and verified
+ * over the paged cache in one forward:
+ *   kv_pages_grow          the tree's rows after what a sequence holds
+ *   kv_pages_tree          what each row sees of the tree, and its position
+ *   kv_pages_append        a layer's rotated keys and values into the pages
+ *   kv_pages_attention_tree
+ *   kv_pages_accept        the accepted rows kept, the others given back */
+
+/* The rotation of a head to position p, after a norm if `norm` is set:
+ *   y = x / sqrt(mean(x^2) + eps) * gain       over the head's head_dim elements
+ *   (y_a, y_b) -> amplitude (cos(t) y_a - sin(t) y_b, sin(t) y_a + cos(t) y_b)
+ * with t = p * freq[j] for pair j < dim / 2: elements (j, j + dim / 2), or with
+ * DLLM_ROTARY_PAIRS (2 j, 2 j + 1).  Elements from dim on are not rotated.
+ * Angles are reduced in 64 bits, the rest is computed in 32 and rounded once.
+ *   freq     device [dim / 2], radians a position; may be NULL with dim 0.
+ *   q_gain, k_gain   device [head_dim], 16-byte aligned, NULL: ones; read with
+ *            norm only.
+ * head_dim in {64, 128}, dim a multiple of 16 in 0 .. head_dim; with norm eps > 0. */
+typedef enum { DLLM_ROTARY_HALVES = 0, DLLM_ROTARY_PAIRS = 1 } dllm_rotary_layout;
+typedef struct {
+    const double* freq;
+    const float* q_gain;
+    const float* k_gain;
+    int32_t head_dim, dim, layout, norm;
+    float amplitude, eps;
+} dllm_rotary;
+
+/* Frequencies freq[j] = base^(-2 j / dim) (host arrays, dim / 2 entries, dim
+ * even and at least 2), scaled for contexts `factor` >= 1 times as long:
+ *   DLLM_ROTARY_LINEAR  all divided by factor
+ *   DLLM_ROTARY_BASE    of base * factor^(dim / (dim - 2)): the highest stands,
+ *                       the lowest is divided by factor (dim 2: unscaled)
+ *   DLLM_ROTARY_RAMP    by turns r within original_len positions: those of r >=
+ *                       fast stand, those of r <= slow are divided by factor,
+ *                       between them both are mixed by (r - slow) / (fast - slow)
+ *                       (YaRN; 0 <= slow < fast)
+ * amplitude receives 1, and for the ramp 0.1 ln(factor) + 1, that method's
+ * factor on the rotated queries and keys.  A host function. */
+typedef enum { DLLM_ROTARY_PLAIN = 0, DLLM_ROTARY_LINEAR = 1, DLLM_ROTARY_BASE = 2, DLLM_ROTARY_RAMP = 3 } dllm_rotary_scaling;
+dllm_status dllm_rotary_frequencies(int32_t dim, double base, int32_t scaling, double factor, double original_len,
+                                    double slow, double fast, double* freq, float* amplitude);
+
+/* Queries and keys normed and rotated: rows i < n_rows[b] (NULL: max_rows each;
+ * outside 0 .. max_rows: clamped) of entry b, q_heads and k_heads heads each
+ * (either 0: its rows are not looked at), 1 <= n <= KV_MAX_SEQS, 1 <= max_rows <=
+ * KV_MAX_ROWS, n * max_rows * (q_heads + k_heads) <= KV_MAX_HEAD_ROWS, at most
+ * KV_MAX_HEADS heads of a kind.
+ *   pos      [n][max_rows] positions, or NULL: row i has pos_offset + i.
+ *   q_out, k_out   may be q and k (the same rows: pointer and strides); other
+ *            rows that are written overlap neither one another nor any input.
+ * Rows from n_rows[b] on are left as they were. */
+dllm_status rotary_rows(const dllm_rotary* rot, int32_t dtype, const int32_t* pos, int32_t pos_offset, int32_t n,
+                        int32_t max_rows, const int32_t* n_rows, int32_t q_heads, const dllm_rows* q,
+                        const dllm_rows* q_out, int32_t k_heads, const dllm_rows* k, const dllm_rows* k_out,
+                        dllm_stream stream);
+
+/* kv_pages_write of keys that are normed and rotated on the way, and of values
+ * as they are; n, max_rows and n_rows as there, and the same rows are written.
+ *   pos      [n][max_rows] positions of the rotation, NULL: those of the rows,
+ *            len - n_rows[b] + i (a row of a tree has its depth's, kv_pages_tree).
+ *   q, q_out   nullable (n_heads 0): queries of n_heads heads at the same
+ *            positions, rotated into q_out (which may be q, as in rotary_rows).
+ *            Rows of a sequence outside 0 .. max_seqs-1 and from n_rows[b] on
+ *            are left as they were; those of an entry whose sequence is listed
+ *            again, or whose page is held twice, are written. */
+dllm_status kv_pages_append(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                            int32_t max_rows, const int32_t* n_rows, const dllm_rotary* rot, const int32_t* pos,
+                            int32_t n_heads, const dllm_rows* q, const dllm_rows* q_out, const dllm_rows* k,
+                            const dllm_rows* v, dllm_stream stream);
+
+/* Trees of drafted tokens, the last n_rows[b] positions of sequence seqs[b]
+ * (n, n_rows as in kv_pages_write, 1 <= max_rows <= KV_TREE_MAX_ROWS): row i follows
+ * row parent[b][i] < i of its entry, or the positions before the tree if
+ * parent[b][i] is not one of 0 .. i-1 (a root).
+ *   parent   [n][max_rows]
+ *   mask     [n][max_rows][(max_rows + 31) / 32]: bit j % 32 of word j / 32 is
+ *            set where row i sees row j, itself or one it follows.
+ *   pos      nullable [n][max_rows]: the row's position, len - n_rows[b] and the
+ *            number of rows that it follows.
+ * Rows from n_rows[b] on are left as they were; a sequence outside 0 ..
+ * max_seqs-1 counts as empty. */
+dllm_status kv_pages_tree(const dllm_kv_pages* pages, const int32_t* seqs, int32_t n, int32_t max_rows,
+                          const int32_t* n_rows, const int32_t* parent, uint32_t* mask, int32_t* pos,
+                          dllm_stream stream);
+
+/* kv_pages_attention of the last n_rows[b] positions of sequence seqs[b], where
+ * row i sees the positions before them and those of the rows j that its mask
+ * names (laid out as by kv_pages_tree, of any pattern; bits from n_rows[b] on
+ * are not looked at); max_rows <= KV_TREE_MAX_ROWS.  Values that a row does not see
+ * do not reach it, whatever they are.  A row that sees no position is 0.
+ * Values that it does see are multiplied by weights of up to 2^15 before the
+ * sums are divided: fp32 ones of 2^112 and more come out infinite.
+ * Everything else, the workspace (kv_pages_attention_workspace_bytes) and the
+ * plan (kv_pages_attention_plan) as there. */
+dllm_status kv_pages_attention_tree(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                                    int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
+                                    const dllm_rows* out, const uint32_t* mask, int32_t prefix_seq,
+                                    int32_t shared_len, int32_t max_len, float scale, void* ws, size_t ws_bytes,
+                                    dllm_stream stream);
+
+/* Of the last n_rows[i] positions of sequence seqs[i] (NULL: max_rows each),
+ * the rows path[i][0 .. n_path[i]-1] are kept, in that order, in every layer:
+ * their keys and values move to the first of these positions, and what is past
+ * them is given back as by kv_pages_free.  max_rows as in kv_pages_write, path
+ * [n][max_path], 1 <= max_path <= KV_TREE_MAX_ROWS.  `status` as for the other calls
+ * that change tables, checked before anything moves: KV_PAGES_ELEN also where
+ * n_rows is outside 0 .. max_rows or n_path outside 0 .. min(n_rows, max_path),
+ * KV_PAGES_ESHARED where a row would move into, or the cut fall inside, a page
+ * that another sequence holds too. */
+size_t kv_pages_accept_workspace_bytes(const dllm_kv_pages* pages, int32_t n, int32_t max_path);
+dllm_status kv_pages_accept(const dllm_kv_pages* pages, const int32_t* seqs, int32_t n, int32_t max_rows,
+                            const int32_t* n_rows, const int32_t* path, int32_t max_path, const int32_t* n_path,
+                            int32_t* status, void* ws, size_t ws_bytes, dllm_stream stream);
 
 /* One denoising forward of a batch whose sequences live in pages: requests of
  * different lengths, or lookahead branches forked off one another.  Row i of

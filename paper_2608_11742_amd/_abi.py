@@ -25,7 +25,7 @@ PROF_NAMES = ("embed", "rmsnorm", "gemm_qkv", "attention", "gemm_o", "gemm_gateu
 STATUS = {0: "DLLM_OK", 1: "DLLM_EINVAL", 2: "DLLM_ESHAPE", 3: "DLLM_EDTYPE", 4: "DLLM_ENOMEM",
           5: "DLLM_EHIP", 6: "DLLM_EUNSUPPORTED"}
 
-i32, f32, vp, sz = C.c_int32, C.c_float, C.c_void_p, C.c_size_t
+i32, f32, f64, vp, sz = C.c_int32, C.c_float, C.c_double, C.c_void_p, C.c_size_t
 
 
 class ModelDesc(C.Structure):
@@ -61,6 +61,11 @@ class Rows(C.Structure):
 class AttentionPlan(C.Structure):
     _fields_ = [(f, i32) for f in ("way", "prefix_rows", "prefix_ranges", "prefix_keys", "tail_rows", "tail_ranges",
                                    "tail_keys")]
+
+
+class RotaryC(C.Structure):
+    _fields_ = [("freq", vp), ("q_gain", vp), ("k_gain", vp), ("head_dim", i32), ("dim", i32), ("layout", i32),
+                ("norm", i32), ("amplitude", f32), ("eps", f32)]
 
 
 class Probe(C.Structure):
@@ -115,6 +120,16 @@ SIGNATURES = {
     "kv_pages_attention": (i32, [C.POINTER(KvPagesC), i32, vp, i32, i32, vp, i32, C.POINTER(Rows), C.POINTER(Rows),
                                  i32, i32, i32, i32, f32, vp, sz, vp]),
     "kv_pages_attention_plan": (i32, [C.POINTER(KvPagesC), i32, i32, i32, i32, i32, C.POINTER(AttentionPlan)]),
+    "dllm_rotary_frequencies": (i32, [i32, f64, i32, f64, f64, f64, f64, C.POINTER(f64), C.POINTER(f32)]),
+    "rotary_rows": (i32, [C.POINTER(RotaryC), i32, vp, i32, i32, i32, vp, i32, C.POINTER(Rows), C.POINTER(Rows), i32,
+                          C.POINTER(Rows), C.POINTER(Rows), vp]),
+    "kv_pages_append": (i32, [C.POINTER(KvPagesC), i32, vp, i32, i32, vp, C.POINTER(RotaryC), vp, i32, C.POINTER(Rows),
+                              C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), vp]),
+    "kv_pages_tree": (i32, [C.POINTER(KvPagesC), vp, i32, i32, vp, vp, vp, vp, vp]),
+    "kv_pages_attention_tree": (i32, [C.POINTER(KvPagesC), i32, vp, i32, i32, vp, i32, C.POINTER(Rows), C.POINTER(Rows),
+                                      vp, i32, i32, i32, f32, vp, sz, vp]),
+    "kv_pages_accept_workspace_bytes": (sz, [C.POINTER(KvPagesC), i32, i32]),
+    "kv_pages_accept": (i32, [C.POINTER(KvPagesC), vp, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
     "dllm_profile_begin": (i32, [vp, i32]),
     "dllm_profile_begin_classes": (i32, [vp, i32, C.c_uint32]),
     "dllm_profile_end": (i32, [vp, C.POINTER(f32), C.POINTER(i32)]),
@@ -130,9 +145,13 @@ SIGNATURES = {
 
 SCHED_TOP_CONFIDENCE, SCHED_LOW_ENTROPY = 0, 1
 KV_PAGES_OK, KV_PAGES_ESEQ, KV_PAGES_ELEN, KV_PAGES_ESHARED, KV_PAGES_EFULL = 0, 1, 2, 3, 4
+KV_PAGES_EPATH = 5
 KV_WAY_ENTRIES, KV_WAY_PARTS, KV_WAY_PAIRS = 0, 1, 2
 KV_MAX_PAGES, KV_MAX_SEQS, KV_MAX_POSITIONS = 1 << 20, 1024, 1 << 30
 KV_MAX_HEADS, KV_MAX_LAYERS, KV_MAX_ROWS, KV_MAX_HEAD_ROWS = 1024, 65536, 1 << 20, 1 << 26
+KV_TREE_MAX_ROWS = 1024
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_RAMP = 0, 1, 2, 3
 
 
 def load(path: str = LIB_PATH):

@@ -380,6 +380,158 @@ def kv_pages_attention_plan(pages: KvPages, n: int, max_rows: int, n_heads: int,
     return plan
 
 
+# ---------------------------------------------------------------- rotary positions, drafts
+
+_SCALINGS = {None: _abi.ROTARY_PLAIN, "linear": _abi.ROTARY_LINEAR, "base": _abi.ROTARY_BASE, "ramp": _abi.ROTARY_RAMP}
+_LAYOUTS = {"halves": _abi.ROTARY_HALVES, "pairs": _abi.ROTARY_PAIRS}
+
+
+def dllm_rotary_frequencies(dim: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
+                            original_len: float = 4096.0, slow: float = 1.0, fast: float = 32.0):
+    """(frequencies in radians a position, amplitude) of a rotation of dim elements; scaling "linear", "base" or "ramp"."""
+    freq, amplitude = (C.c_double * max(1, dim // 2))(), C.c_float()
+    _check(lib().dllm_rotary_frequencies(dim, base, _SCALINGS[scaling], factor, original_len, slow, fast, freq,
+                                         C.byref(amplitude)))
+    return list(freq), float(amplitude.value)
+
+
+class Rotary:
+    """Rotation of heads to their positions, after a norm by head (dllm_rotary).
+
+    dim: rotated elements of a head (default all), layout "halves" or "pairs",
+    scaling as in dllm_rotary_frequencies; freq [dim / 2] gives other
+    frequencies, amplitude another factor.  norm: heads are normed first, with
+    gains q_gain and k_gain [head_dim] where given."""
+
+    def __init__(self, head_dim: int, dim: int | None = None, base: float = 10000.0, layout: str = "halves",
+                 scaling: str | None = None, factor: float = 1.0, original_len: float = 4096.0, slow: float = 1.0,
+                 fast: float = 32.0, freq=None, amplitude: float | None = None, norm: bool = False, eps: float = 1e-5,
+                 q_gain=None, k_gain=None, device="cuda"):
+        dim = head_dim if dim is None else dim
+        if layout not in _LAYOUTS or scaling not in _SCALINGS:
+            raise ValueError("layout is halves or pairs, scaling None, linear, base or ramp")
+        if head_dim not in (64, 128) or not 0 <= dim <= head_dim or dim % 16:
+            raise ValueError("head_dim is 64 or 128, dim a multiple of 16 up to it")
+        if not norm and (q_gain is not None or k_gain is not None):
+            raise ValueError("gains belong to a norm")
+        own = 1.0
+        if freq is None and dim:
+            freq, own = dllm_rotary_frequencies(dim, base, scaling, factor, original_len, slow, fast)
+        if freq is not None and len(freq) != dim // 2:
+            raise ValueError("one frequency for every pair of rotated elements")
+        self.freq = torch.as_tensor(freq if dim else [0.0], dtype=torch.float64).to(device).contiguous()
+        self.device, self._index = self.freq.device, self.freq.get_device()
+        self.q_gain, self.k_gain = q_gain, k_gain
+        for g in (q_gain, k_gain):
+            if g is not None and (g.dtype != torch.float32 or tuple(g.shape) != (head_dim,) or not g.is_contiguous()
+                                  or g.device != self.device):
+                raise ValueError("gains are contiguous fp32 tensors [head_dim] beside the frequencies")
+        self.head_dim, self.dim, self.amplitude = head_dim, dim, own if amplitude is None else amplitude
+        self._c = _abi.RotaryC(self.freq.data_ptr(), _p(q_gain), _p(k_gain), head_dim, dim, _LAYOUTS[layout], int(norm),
+                               self.amplitude, eps)
+        self._ref = C.byref(self._c)
+
+
+def _positions(owner, t, n: int, rows: int):
+    """Address of an int32 list [entries, rows] beside the owner's arrays."""
+    if t is None:
+        return None
+    if t.dtype is not _I32 or t.get_device() != owner._index or t.shape != (n, rows) or not t.is_contiguous():
+        raise ValueError("positions and parents are contiguous int32 tensors [entries, rows], beside the other arrays")
+    return t.data_ptr()
+
+
+def _turned(owner, x, out, dtype, n: int, rows: int, name: str):
+    """x and out [n, rows, heads, head_dim] as heads and two dllm_rows; none without x."""
+    if x is None:
+        return 0, None, None
+    if out is None or out.shape != x.shape or x.dim() != 4 or x.shape[:2] != (n, rows) or x.shape[3] != owner.head_dim:
+        raise ValueError(f"{name} and its output are [entries, rows, heads, head_dim], of the same entries, rows and head_dim")
+    heads, at = x.shape[2], []
+    for t in (x, out):
+        seq, row, head, one = t.stride()
+        if one != 1 or t.dtype is not dtype or t.get_device() != owner._index:
+            raise ValueError(f"{name} must have contiguous rows, one type, and the device of the other arrays")
+        at.append(_Rows(t.data_ptr(), seq if n > 1 else 0, row if rows > 1 else 0, head if heads > 1 else 0))
+    return heads, at[0], at[1]
+
+
+_DTYPES = {torch.bfloat16: DLLM_BF16, torch.float32: DLLM_F32}
+
+
+def rotary_rows(rot: Rotary, q, q_out, k=None, k_out=None, pos=None, pos_offset: int = 0, n_rows=None, stream=None):
+    """q [entries, rows, heads, head_dim] (and k, with heads of its own) normed and rotated into q_out (and k_out);
+    pos [entries, rows], or row i is at pos_offset + i.  The outputs may be the inputs."""
+    x = k if q is None else q
+    n, rows = x.shape[:2]
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError("rows are bf16 or fp32")
+    hq, qi, qo = _turned(rot, q, q_out, x.dtype, n, rows, "q")
+    hk, ki, ko = _turned(rot, k, k_out, x.dtype, n, rows, "k")
+    _check(lib().rotary_rows(rot._ref, dtype, _positions(rot, pos, n, rows), pos_offset, n, rows, _ids(rot, n_rows, n),
+                             hq, qi, qo, hk, ki, ko, _page_stream(rot, stream)))
+
+
+def kv_pages_append(pages: KvPages, layer: int, seqs, k, v, rot: Rotary, q=None, q_out=None, pos=None, n_rows=None,
+                    stream=None):
+    """kv_pages_write with k normed and rotated on the way; q [entries, rows, heads, head_dim] likewise into q_out.
+    pos [entries, rows]: positions of the rotation, by default those of the rows."""
+    n, rows, heads, hd = shape = k.shape
+    if v.shape != shape or heads != pages.n_kv_heads or hd != pages.head_dim:
+        raise ValueError("k and v need the pages' heads and head_dim and the same shape")
+    if rot._index != pages._index:
+        raise ValueError("the rotation is on another device than the pages")
+    hq, qi, qo = _turned(pages, q, q_out, pages.dtype, n, rows, "q")
+    _check(lib().kv_pages_append(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n), rot._ref,
+                                 _positions(pages, pos, n, rows), hq, qi, qo, _rows(pages, k, n, rows, heads, "k"),
+                                 _rows(pages, v, n, rows, heads, "v"), _page_stream(pages, stream)))
+
+
+def _mask(pages: KvPages, mask, n: int, rows: int):
+    if (mask.dtype is not _I32 or mask.get_device() != pages._index or mask.shape != (n, rows, (rows + 31) // 32)
+            or not mask.is_contiguous()):
+        raise ValueError("a mask is a contiguous int32 tensor [entries, rows, words of 32 rows] beside the pages")
+    return mask.data_ptr()
+
+
+def kv_pages_tree(pages: KvPages, seqs, parent, mask, pos=None, n_rows=None, stream=None):
+    """parent [entries, rows]: the row that each drafted row follows, or -1.  Written: mask [entries, rows,
+    (rows + 31) // 32], the rows that each sees, as bits; pos [entries, rows], the rows' positions."""
+    n, rows = parent.shape
+    _check(lib().kv_pages_tree(pages._ref, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n),
+                               _positions(pages, parent, n, rows), _mask(pages, mask, n, rows),
+                               _positions(pages, pos, n, rows), _page_stream(pages, stream)))
+
+
+def kv_pages_attention_tree(pages: KvPages, layer: int, seqs, q, out, mask, ws, n_rows=None, prefix_seq: int = 0,
+                            shared_len: int = 0, max_len: int | None = None, scale: float | None = None, stream=None):
+    """kv_pages_attention of the last rows of each sequence, which see what is before them and the rows in their mask."""
+    n, rows, heads, hd = shape = q.shape
+    if out.shape != shape or hd != pages.head_dim:
+        raise ValueError("q and out need the pages' head_dim and the same shape")
+    if max_len is None:
+        max_len = pages.table.shape[1] * pages.page_len
+    _check(lib().kv_pages_attention_tree(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n), heads,
+                                         _rows(pages, q, n, rows, heads, "q"), _rows(pages, out, n, rows, heads, "out"),
+                                         _mask(pages, mask, n, rows), prefix_seq, shared_len, max_len,
+                                         pages._scale if scale is None else scale, *_scratch(pages, ws),
+                                         _page_stream(pages, stream)))
+
+
+def kv_pages_accept_workspace_bytes(pages: KvPages, n: int, max_path: int) -> int:
+    return lib().kv_pages_accept_workspace_bytes(pages._ref, n, max_path)
+
+
+def kv_pages_accept(pages: KvPages, seqs, path, n_path, status, ws, rows: int, n_rows=None, stream=None):
+    """Of the last n_rows[i] (or `rows`) positions of seqs[i] those of the rows path[i][:n_path[i]], which ascend, are
+    kept, in every layer, and the others given back."""
+    n, max_path = path.shape
+    _check(lib().kv_pages_accept(pages._ref, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n),
+                                 _positions(pages, path, n, max_path), max_path, _ids(pages, n_path, n),
+                                 _ids(pages, status, 1), *_scratch(pages, ws), _page_stream(pages, stream)))
+
+
 def dllm_workspace_bytes_pages(handle, batch: int, seq: int, n_lm_pos: int) -> int:
     return lib().dllm_workspace_bytes_pages(handle, batch, seq, n_lm_pos)
 

@@ -995,29 +995,32 @@ size_t kv_pages_attention_workspace_bytes(const dllm_kv_pages* pages, int32_t n,
   return paged_attention_workspace(*pages, n, max_rows, n_heads);
 }
 
-dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
-                               int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
-                               const dllm_rows* out, int32_t prefix_seq, int32_t shared_len, int32_t max_len,
-                               int32_t causal, float scale, void* ws, size_t ws_bytes, dllm_stream stream) {
-  dllm_status st = check_attention(pages, n, max_rows, n_heads, "kv_pages_attention");
-  if (st == DLLM_OK) st = check_entries(seqs, n, "kv_pages_attention");
-  if (st == DLLM_OK) st = check_rows(q, pages->dtype, "kv_pages_attention", "q");
-  if (st == DLLM_OK) st = check_rows(out, pages->dtype, "kv_pages_attention", "out");
+namespace {
+
+// both attentions: checks and launch (mask NULL: full or causal rows)
+dllm_status attend(const char* who, const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                   int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q, const dllm_rows* out,
+                   bool causal, const uint32_t* mask, int32_t prefix_seq, int32_t shared_len, int32_t max_len,
+                   float scale, void* ws, size_t ws_bytes, dllm_stream stream) {
+  dllm_status st = check_attention(pages, n, max_rows, n_heads, who);
+  if (st == DLLM_OK) st = check_entries(seqs, n, who);
+  if (st == DLLM_OK) st = check_rows(q, pages->dtype, who, "q");
+  if (st == DLLM_OK) st = check_rows(out, pages->dtype, who, "out");
   if (st != DLLM_OK) return st;
   const int64_t hd = pages->head_dim;
   if ((n > 1 && out->seq < hd) || (max_rows > 1 && out->row < hd) || (n_heads > 1 && out->head < hd))
-    return fail(DLLM_ESHAPE, "kv_pages_attention: rows of out overlap");
-  if (layer < 0 || layer >= pages->n_layers) return fail(DLLM_ESHAPE, "kv_pages_attention: layer %d", layer);
-  if (shared_len < 0 || max_len < 0) return fail(DLLM_ESHAPE, "kv_pages_attention: shared_len %d max_len %d", shared_len, max_len);
+    return fail(DLLM_ESHAPE, "%s: rows of out overlap", who);
+  if (layer < 0 || layer >= pages->n_layers) return fail(DLLM_ESHAPE, "%s: layer %d", who, layer);
+  if (shared_len < 0 || max_len < 0) return fail(DLLM_ESHAPE, "%s: shared_len %d max_len %d", who, shared_len, max_len);
   if (shared_len > 0 && (prefix_seq < 0 || prefix_seq >= pages->max_seqs))
-    return fail(DLLM_EINVAL, "kv_pages_attention: prefix_seq %d outside 0..%d", prefix_seq, pages->max_seqs - 1);
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(DLLM_EINVAL, "kv_pages_attention: scale must be finite and > 0");
-  if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "kv_pages_attention: ws NULL or not 16-byte aligned");
+    return fail(DLLM_EINVAL, "%s: prefix_seq %d outside 0..%d", who, prefix_seq, pages->max_seqs - 1);
+  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(DLLM_EINVAL, "%s: scale must be finite and > 0", who);
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "%s: ws NULL or not 16-byte aligned", who);
   const size_t need = paged_attention_workspace(*pages, n, max_rows, n_heads);
   if (ws_bytes < need) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, need);
   // which rows of ragged entries are written is known on the device alone
   if (!n_rows && rows_overlap(*out, n, max_rows, n_heads, hd))
-    return fail(DLLM_ESHAPE, "kv_pages_attention: rows of out overlap");
+    return fail(DLLM_ESHAPE, "%s: rows of out overlap", who);
   PagedAttn a{};
   a.p = *pages;
   a.layer = layer;
@@ -1031,10 +1034,34 @@ dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const 
   a.prefix_seq = prefix_seq;
   a.shared_len = shared_len;
   a.max_len = max_len;
-  a.causal = causal != 0;
+  a.causal = causal;
+  a.mask = mask;
+  a.words = (max_rows + 31) / 32;
   a.scale = scale;
   a.part = static_cast<float*>(ws);
-  return hip_check(paged_attention(a, static_cast<hipStream_t>(stream)), "kv_pages_attention");
+  return hip_check(paged_attention(a, static_cast<hipStream_t>(stream)), who);
+}
+
+}  // namespace
+
+dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                               int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
+                               const dllm_rows* out, int32_t prefix_seq, int32_t shared_len, int32_t max_len,
+                               int32_t causal, float scale, void* ws, size_t ws_bytes, dllm_stream stream) {
+  return attend("kv_pages_attention", pages, layer, seqs, n, max_rows, n_rows, n_heads, q, out, causal != 0, nullptr,
+                prefix_seq, shared_len, max_len, scale, ws, ws_bytes, stream);
+}
+
+dllm_status kv_pages_attention_tree(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                                    int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
+                                    const dllm_rows* out, const uint32_t* mask, int32_t prefix_seq,
+                                    int32_t shared_len, int32_t max_len, float scale, void* ws, size_t ws_bytes,
+                                    dllm_stream stream) {
+  const char* who = "kv_pages_attention_tree";
+  if (!mask) return fail(DLLM_EINVAL, "%s: NULL mask", who);
+  if (max_rows > KV_TREE_MAX_ROWS) return fail(DLLM_ESHAPE, "%s: max_rows %d > %d", who, max_rows, KV_TREE_MAX_ROWS);
+  return attend(who, pages, layer, seqs, n, max_rows, n_rows, n_heads, q, out, false, mask, prefix_seq, shared_len,
+                max_len, scale, ws, ws_bytes, stream);
 }
 
 dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
@@ -1077,6 +1104,180 @@ dllm_status dllm_forward_pages(dllm_model* m, const int32_t* tokens, int32_t bat
   const Paging pg{pages, seqs, prefix_seq, shared_len, max_len};
   return forward_impl(m, tokens, batch, seq, 0, nullptr, nullptr, lm_pos, n_lm_pos, row_scale, scale, probe, out, ws,
                       ws_bytes, stream, nullptr, &pg);
+}
+
+// ---------------------------------------------------------------- rotary positions, drafts
+
+dllm_status dllm_rotary_frequencies(int32_t dim, double base, int32_t scaling, double factor, double original_len,
+                                    double slow, double fast, double* freq, float* amplitude) {
+  const char* who = "dllm_rotary_frequencies";
+  if (!freq || !amplitude) return fail(DLLM_EINVAL, "%s: NULL freq or amplitude", who);
+  if (dim < 2 || dim % 2) return fail(DLLM_ESHAPE, "%s: dim %d", who, dim);
+  if (!(base > 0.0) || !std::isfinite(base)) return fail(DLLM_EINVAL, "%s: base must be finite and > 0", who);
+  if (scaling < DLLM_ROTARY_PLAIN || scaling > DLLM_ROTARY_RAMP) return fail(DLLM_EINVAL, "%s: scaling %d", who, scaling);
+  if (scaling != DLLM_ROTARY_PLAIN && !(factor >= 1.0 && std::isfinite(factor)))
+    return fail(DLLM_EINVAL, "%s: factor must be finite and at least 1", who);
+  if (scaling == DLLM_ROTARY_RAMP &&
+      !(original_len > 0.0 && std::isfinite(original_len) && slow >= 0.0 && fast > slow && std::isfinite(fast)))
+    return fail(DLLM_EINVAL, "%s: a ramp needs original_len > 0 and 0 <= slow < fast", who);
+  constexpr double kTurn = 6.283185307179586;
+  if (scaling == DLLM_ROTARY_BASE && dim > 2) base *= std::pow(factor, double(dim) / (dim - 2));
+  for (int32_t j = 0; j < dim / 2; ++j) {
+    double f = std::pow(base, -2.0 * j / dim);
+    if (scaling == DLLM_ROTARY_LINEAR) f /= factor;
+    if (scaling == DLLM_ROTARY_RAMP) {
+      const double stay = std::min(1.0, std::max(0.0, (original_len * f / kTurn - slow) / (fast - slow)));
+      f *= stay + (1.0 - stay) / factor;
+    }
+    freq[j] = f;
+  }
+  *amplitude = scaling == DLLM_ROTARY_RAMP ? float(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return DLLM_OK;
+}
+
+namespace {
+
+dllm_status check_rotary(const dllm_rotary* r, const char* who) {
+  if (!r) return fail(DLLM_EINVAL, "%s: NULL rot", who);
+  if (r->head_dim != 64 && r->head_dim != 128)
+    return fail(DLLM_ESHAPE, "%s: head_dim %d not in {64, 128}", who, r->head_dim);
+  if (r->dim < 0 || r->dim > r->head_dim || r->dim % 16)
+    return fail(DLLM_ESHAPE, "%s: dim %d is no multiple of 16 in 0..%d", who, r->dim, r->head_dim);
+  if (r->layout != DLLM_ROTARY_HALVES && r->layout != DLLM_ROTARY_PAIRS)
+    return fail(DLLM_EINVAL, "%s: layout %d", who, r->layout);
+  if (r->dim > 0 && (!r->freq || reinterpret_cast<uintptr_t>(r->freq) % 8))
+    return fail(DLLM_EINVAL, "%s: freq NULL or not 8-byte aligned", who);
+  if (!std::isfinite(r->amplitude)) return fail(DLLM_EINVAL, "%s: amplitude must be finite", who);
+  if (r->norm && (!(r->eps > 0.f) || !std::isfinite(r->eps)))
+    return fail(DLLM_EINVAL, "%s: eps must be finite and > 0", who);
+  if (r->norm && (reinterpret_cast<uintptr_t>(r->q_gain) | reinterpret_cast<uintptr_t>(r->k_gain)) % 16)
+    return fail(DLLM_EINVAL, "%s: gains need 16-byte alignment", who);
+  return DLLM_OK;
+}
+
+// rows that are rotated into `out`: in place, or to rows that do not overlap
+dllm_status check_turned(const dllm_rows* in, const dllm_rows* out, int dtype, int n, int max_rows, bool ragged,
+                         int heads, int head_dim, const char* who, const char* name) {
+  dllm_status st = check_rows(in, dtype, who, name);
+  if (st == DLLM_OK) st = check_rows(out, dtype, who, name);
+  if (st != DLLM_OK) return st;
+  if (in->p == out->p && ((n > 1 && in->seq != out->seq) || (max_rows > 1 && in->row != out->row) ||
+                          (heads > 1 && in->head != out->head)))
+    return fail(DLLM_EINVAL, "%s: %s in place needs the same strides in and out", who, name);
+  if ((n > 1 && out->seq < head_dim) || (max_rows > 1 && out->row < head_dim) || (heads > 1 && out->head < head_dim) ||
+      (!ragged && rows_overlap(*out, n, max_rows, heads, head_dim)))
+    return fail(DLLM_ESHAPE, "%s: output rows of %s overlap", who, name);
+  return DLLM_OK;
+}
+
+dllm_status check_sizes(int32_t n, int32_t max_rows, int32_t q_heads, int32_t k_heads, const char* who) {
+  if (n < 1 || n > KV_MAX_SEQS) return fail(DLLM_ESHAPE, "%s: %d entries outside 1..%d", who, n, KV_MAX_SEQS);
+  if (max_rows < 1 || max_rows > KV_MAX_ROWS) return fail(DLLM_ESHAPE, "%s: max_rows %d", who, max_rows);
+  if (q_heads < 0 || q_heads > KV_MAX_HEADS || k_heads < 0 || k_heads > KV_MAX_HEADS || q_heads + k_heads < 1 ||
+      int64_t(n) * max_rows * (q_heads + k_heads) > KV_MAX_HEAD_ROWS)
+    return fail(DLLM_ESHAPE, "%s: %d x %d rows of %d and %d heads", who, n, max_rows, q_heads, k_heads);
+  return DLLM_OK;
+}
+
+}  // namespace
+
+dllm_status rotary_rows(const dllm_rotary* rot, int32_t dtype, const int32_t* pos, int32_t pos_offset, int32_t n,
+                        int32_t max_rows, const int32_t* n_rows, int32_t q_heads, const dllm_rows* q,
+                        const dllm_rows* q_out, int32_t k_heads, const dllm_rows* k, const dllm_rows* k_out,
+                        dllm_stream stream) {
+  const char* who = "rotary_rows";
+  dllm_status st = check_rotary(rot, who);
+  if (st != DLLM_OK) return st;
+  if (dtype != DLLM_F32 && dtype != DLLM_BF16) return fail(DLLM_EDTYPE, "%s: dtype %d", who, dtype);
+  st = check_sizes(n, max_rows, q_heads, k_heads, who);
+  if (st == DLLM_OK && q_heads)
+    st = check_turned(q, q_out, dtype, n, max_rows, n_rows != nullptr, q_heads, rot->head_dim, who, "q");
+  if (st == DLLM_OK && k_heads)
+    st = check_turned(k, k_out, dtype, n, max_rows, n_rows != nullptr, k_heads, rot->head_dim, who, "k");
+  if (st != DLLM_OK) return st;
+  RotaryRows a{};
+  a.rot = *rot;
+  a.pos = pos;
+  a.pos_offset = pos_offset;
+  a.n = n;
+  a.max_rows = max_rows;
+  a.n_rows = n_rows;
+  a.q_heads = q_heads;
+  a.k_heads = k_heads;
+  if (q_heads) a.q = *q, a.q_out = *q_out;
+  if (k_heads) a.k = *k, a.k_out = *k_out;
+  return hip_check(dllm::rotary_rows(dtype, a, static_cast<hipStream_t>(stream)), who);
+}
+
+dllm_status kv_pages_append(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
+                            int32_t max_rows, const int32_t* n_rows, const dllm_rotary* rot, const int32_t* pos,
+                            int32_t n_heads, const dllm_rows* q, const dllm_rows* q_out, const dllm_rows* k,
+                            const dllm_rows* v, dllm_stream stream) {
+  const char* who = "kv_pages_append";
+  dllm_status st = check_pages(pages, who);
+  if (st == DLLM_OK) st = check_entries(seqs, n, who);
+  if (st == DLLM_OK) st = check_rotary(rot, who);
+  if (st != DLLM_OK) return st;
+  if (rot->head_dim != pages->head_dim)
+    return fail(DLLM_ESHAPE, "%s: rotation of heads of %d, pages of %d", who, rot->head_dim, pages->head_dim);
+  st = check_sizes(n, max_rows, n_heads, pages->n_kv_heads, who);
+  if (st == DLLM_OK) st = check_rows(k, pages->dtype, who, "k");
+  if (st == DLLM_OK) st = check_rows(v, pages->dtype, who, "v");
+  if (st == DLLM_OK && n_heads)
+    st = check_turned(q, q_out, pages->dtype, n, max_rows, n_rows != nullptr, n_heads, rot->head_dim, who, "q");
+  if (st != DLLM_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers) return fail(DLLM_ESHAPE, "%s: layer %d", who, layer);
+  RotaryRows a{};
+  a.rot = *rot;
+  a.pos = pos;
+  a.n = n;
+  a.max_rows = max_rows;
+  a.n_rows = n_rows;
+  a.q_heads = n_heads;
+  a.k_heads = pages->n_kv_heads;
+  if (n_heads) a.q = *q, a.q_out = *q_out;
+  a.k = *k;
+  return hip_check(pages_append(*pages, layer, seqs, a, *v, static_cast<hipStream_t>(stream)), who);
+}
+
+dllm_status kv_pages_tree(const dllm_kv_pages* pages, const int32_t* seqs, int32_t n, int32_t max_rows,
+                          const int32_t* n_rows, const int32_t* parent, uint32_t* mask, int32_t* pos,
+                          dllm_stream stream) {
+  const char* who = "kv_pages_tree";
+  dllm_status st = check_pages(pages, who);
+  if (st == DLLM_OK) st = check_entries(seqs, n, who);
+  if (st != DLLM_OK) return st;
+  if (!parent || !mask) return fail(DLLM_EINVAL, "%s: NULL parent or mask", who);
+  if (max_rows < 1 || max_rows > KV_TREE_MAX_ROWS)
+    return fail(DLLM_ESHAPE, "%s: max_rows %d outside 1..%d", who, max_rows, KV_TREE_MAX_ROWS);
+  return hip_check(pages_tree(*pages, seqs, n, max_rows, n_rows, parent, mask, pos, static_cast<hipStream_t>(stream)),
+                   who);
+}
+
+size_t kv_pages_accept_workspace_bytes(const dllm_kv_pages* pages, int32_t n, int32_t max_path) {
+  if (check_pages(pages, "kv_pages_accept_workspace_bytes") != DLLM_OK || n < 1 || n > KV_MAX_SEQS || max_path < 1 ||
+      max_path > KV_TREE_MAX_ROWS)
+    return 0;
+  return size_t(n) * max_path * sizeof(int32_t);
+}
+
+dllm_status kv_pages_accept(const dllm_kv_pages* pages, const int32_t* seqs, int32_t n, int32_t max_rows,
+                            const int32_t* n_rows, const int32_t* path, int32_t max_path, const int32_t* n_path,
+                            int32_t* status, void* ws, size_t ws_bytes, dllm_stream stream) {
+  const char* who = "kv_pages_accept";
+  dllm_status st = check_pages(pages, who);
+  if (st == DLLM_OK) st = check_entries(seqs, n, who);
+  if (st != DLLM_OK) return st;
+  if (!path || !n_path || !status) return fail(DLLM_EINVAL, "%s: NULL path, n_path or status", who);
+  if (max_rows < 1 || max_rows > KV_MAX_ROWS) return fail(DLLM_ESHAPE, "%s: max_rows %d", who, max_rows);
+  if (max_path < 1 || max_path > KV_TREE_MAX_ROWS)
+    return fail(DLLM_ESHAPE, "%s: max_path %d outside 1..%d", who, max_path, KV_TREE_MAX_ROWS);
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 16) return fail(DLLM_EINVAL, "%s: ws NULL or not 16-byte aligned", who);
+  const size_t need = kv_pages_accept_workspace_bytes(pages, n, max_path);
+  if (ws_bytes < need) return fail(DLLM_ENOMEM, "workspace %zu < %zu bytes", ws_bytes, need);
+  return hip_check(pages_accept(*pages, seqs, n, max_rows, n_rows, path, max_path, n_path, status, ws,
+                                static_cast<hipStream_t>(stream)),
+                   who);
 }
 
 }  // extern "C"

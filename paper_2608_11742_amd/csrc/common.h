@@ -78,6 +78,17 @@ __device__ __forceinline__ uint32_t pack_vt2(float a, float b) { return pack_f16
 __device__ __forceinline__ void store_vt(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_vt(bf16_t* p, float v) { p->bits = uint16_t(pack_vt2(v, 0.f)); }
 
+// values as the pages of bf16 models hold them: rounded to binary16, past its
+// range the largest of their sign (what saturating first gives), a NaN as it is
+// (the median that saturates elsewhere returns the lowest of the others for one)
+__device__ __forceinline__ uint32_t pack_values(float a, float b) {
+  typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+  const half2v most = {65504, 65504}, v = __builtin_bit_cast(half2v, pack_f16x2(a, b));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_maximum(__builtin_elementwise_minimum(v, most), -most));
+}
+__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_value(bf16_t* p, float v) { p->bits = uint16_t(pack_values(v, 0.f)); }
+
 // silu(g) = g / (1 + e^-g) with the hardware base-2 exponential
 __device__ __forceinline__ float silu(float g) {
   return g / (1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g));

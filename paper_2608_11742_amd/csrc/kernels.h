@@ -154,6 +154,30 @@ hipError_t pages_write_vt(const dllm_kv_pages& p, int layer, const int32_t* seqs
 hipError_t pages_rope_rows(const dllm_kv_pages& p, const int32_t* seqs, int n, int rows, int max_pos,
                            const float2* rope, int half, float2* out, hipStream_t s);
 
+// the rows of accepted paths moved, the others given back (see kv_pages_accept); ws: n * max_path words
+hipError_t pages_accept(const dllm_kv_pages& p, const int32_t* seqs, int n, int max_rows, const int32_t* n_rows,
+                        const int32_t* path, int max_path, const int32_t* n_path, int32_t* status, void* ws,
+                        hipStream_t s);
+
+// masks and positions of drafted trees (tree.hip)
+hipError_t pages_tree(const dllm_kv_pages& p, const int32_t* seqs, int n, int max_rows, const int32_t* n_rows,
+                      const int32_t* parent, uint32_t* mask, int32_t* pos, hipStream_t s);
+
+// queries and keys normed and rotated (rotary.hip)
+struct RotaryRows {
+  dllm_rotary rot;
+  const int32_t* pos;      // nullable: pos_offset + row (an append: the rows' own)
+  int pos_offset;
+  int n, max_rows;
+  const int32_t* n_rows;   // nullable: max_rows each
+  int q_heads, k_heads;
+  dllm_rows q, q_out, k, k_out;
+};
+hipError_t rotary_rows(int dtype, const RotaryRows& a, hipStream_t s);
+// the same with the keys, and values as they are, into the pages (k_out is not used)
+hipError_t pages_append(const dllm_kv_pages& p, int layer, const int32_t* seqs, const RotaryRows& a, const dllm_rows& v,
+                        hipStream_t s);
+
 // attention over the pages of one layer (paged_attention.hip)
 struct PagedAttn {
   dllm_kv_pages p;
@@ -164,6 +188,8 @@ struct PagedAttn {
   dllm_rows q, out;
   int prefix_seq, shared_len, max_len;
   bool causal;
+  const uint32_t* mask;    // nullable: which of an entry's rows each of them sees, `words` a row
+  int words;
   float scale;
   float* part;             // workspace of paged_attention_workspace bytes
 };

@@ -49,6 +49,7 @@
 // sums l and products o are held in 32 bits; wide and pairs sum the weights as
 // rounded, narrow before.
 #include <algorithm>
+#include <climits>
 
 #include "common.h"
 #include "kernels.h"
@@ -101,9 +102,16 @@ __device__ __forceinline__ Entry entry_of(const PagedAttn& a, int b) {
   e.rows = a.n_rows ? min(max(a.n_rows[b], 0), a.max_rows) : a.max_rows;
   return e;
 }
+// positions that all rows of the entry see, from the first on (the rest: its tail's)
+template <bool TREE>
+__device__ __forceinline__ int common_of(const Entry& e) {
+  return TREE ? max(e.held - e.rows, 0) : e.held;
+}
 // of the `shared` positions, those that the entry takes with the others', which are in steps of `range`
+template <bool TREE>
 __device__ __forceinline__ int stacked_of(const Entry& e, int shared, int range) {
-  return e.held >= shared ? shared : e.held / range * range;
+  const int held = common_of<TREE>(e);
+  return held >= shared ? shared : held / range * range;
 }
 // positions that row i of the entry sees
 __device__ __forceinline__ int limit_of(const PagedAttn& a, const Entry& e, int i) {
@@ -141,6 +149,7 @@ __device__ __forceinline__ Item item_of(int x, int row_tiles) {
 int blocks_of(int items, int row_tiles) { return cdiv(items, 8) * 8 * row_tiles; }
 
 // False if the share is empty.
+template <bool TREE>
 __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, int tile_rows, Share& w) {
   const PagedAttn& a = j.a;
   const int per = a.max_rows * j.group;   // stacked rows of one entry
@@ -163,7 +172,7 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
   const Entry e = entry_of(a, b);
   w.row0 = b * per + it.tile * tile_rows;
   w.row_end = (b + 1) * per;
-  w.k0 = (j.stacked ? stacked_of(e, s, j.prefix.range) : 0) + r * part.range;
+  w.k0 = (j.stacked ? stacked_of<TREE>(e, s, j.prefix.range) : 0) + r * part.range;
   w.k1 = r + 1 == part.ranges ? e.held : min(w.k0 + part.range, e.held);
   w.part = j.prefix.ranges + r;
   w.split = s;
@@ -212,13 +221,87 @@ __device__ __forceinline__ float quad_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// ---------------------------------------------------------------- trees
+//
+// A tree's keys are in the tails alone, a few of the last steps, where a row
+// sees what its mask names: its words give the bits of a step's keys.  A value
+// that one row must not see is there for the others, and a weight of 0 would not
+// cancel it if it is infinite or no number.  Such values, looked for in these
+// steps only, are taken out before the product; where there were any, a pass
+// over the steps' values at the end brings them to the rows that see them: two
+// products with the masks in place of the weights count per row and dim those
+// that are +inf or NaN and those that are -inf or NaN.
+
+// bits of the keys k0 .. k0 + 63 that row i of entry b sees: those before the
+// tree's first position `root` (negative where the sequence is shorter than its
+// rows), of the tree those in its mask, none from `end` on
+__device__ __forceinline__ uint64_t seen_of(const PagedAttn& a, int b, int i, int root, int end, int k0) {
+  const uint32_t* row = a.mask + (size_t(b) * a.max_rows + i) * a.words;
+  auto word = [&](int j) { return j < a.words ? row[j] : 0u; };
+  const int t = k0 - root, j = max(t, 0) >> 5, shift = t & 31;
+  const uint64_t w = uint64_t(word(j + 1)) << 32 | word(j);
+  uint64_t bits;
+  if (t >= 0) bits = w >> shift | (shift ? uint64_t(word(j + 2)) << (64 - shift) : 0);
+  else bits = t <= -64 ? ~uint64_t(0) : w << -t | ~(~uint64_t(0) << -t);
+  const int left = end - k0;
+  return left >= 64 ? bits : left <= 0 ? 0 : bits & ~(~uint64_t(0) << left);
+}
+
+// of a word of values: 1 in the places of those that are +inf or NaN (up), -inf or NaN (down)
+struct Wild {
+  uint32_t up, down;
+};
+template <bool kHalf>
+__device__ __forceinline__ Wild wild_of(uint32_t w) {
+  if constexpr (kHalf) {
+    Wild x{0, 0};
+#pragma unroll
+    for (int s = 0; s < 32; s += 16) {
+      const uint32_t v = w >> s & 0xffffu, e = v & 0x7fffu;
+      if (e > 0x7c00u || v == 0x7c00u) x.up |= 0x3c00u << s;
+      if (e > 0x7c00u || v == 0xfc00u) x.down |= 0x3c00u << s;
+    }
+    return x;
+  } else {
+    const uint32_t e = w & 0x7fffffffu;
+    return Wild{e > 0x7f800000u || w == 0x7f800000u ? 0x3f800000u : 0u,
+                e > 0x7f800000u || w == 0xff800000u ? 0x3f800000u : 0u};
+  }
+}
+// the top bit of each value of a word that is infinite or no number: its
+// exponent, all ones, carries into it
+template <bool kHalf>
+__device__ __forceinline__ uint32_t wild_bits(uint32_t w) {
+  return kHalf ? ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u : ((w & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+}
+// those values as 0
+template <bool kHalf>
+__device__ __forceinline__ uint32_t tame(uint32_t w) {
+  const uint32_t x = wild_bits<kHalf>(w);
+  return w & ~(kHalf ? (x >> 15) * 0xffffu : uint32_t(int32_t(x) >> 31));
+}
+// what counts of `up` and `down` add to an output
+__device__ __forceinline__ float wild_sum(bool up, bool down) {
+  return (up ? INFINITY : 0.f) + (down ? -INFINITY : 0.f);
+}
+// the low bits of x as 1s and 0s of a chunk of 8 binary16 or 4 fp32 values
+template <bool kHalf>
+__device__ __forceinline__ u32x4 ones_of(uint32_t x) {
+  u32x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    y[i] = kHalf ? (x >> (2 * i) & 1 ? 0x3c00u : 0u) | (x >> (2 * i + 1) & 1 ? 0x3c000000u : 0u)
+                 : (x >> i & 1 ? 0x3f800000u : 0u);
+  return y;
+}
+
 // ---------------------------------------------------------------- narrow
 
 // NQB blocks of 16 rows.  A key step is KS keys in blocks of 16; bf16 keys of
 // a 32-key half are gathered so that output element i of lane group g in
 // block kk is key 8 g + 4 kk + i: the lane's 8 probabilities of the half are 8
 // consecutive keys, one 16-byte chunk of a V^T row.
-template <typename T, int HD, int NQB>
+template <typename T, int HD, int NQB, bool TREE>
 struct Narrow {
   static constexpr bool kHalf = sizeof(T) == 2;
   static constexpr int E = 16 / int(sizeof(T));             // elements per chunk
@@ -256,12 +339,22 @@ struct Narrow {
     RowAt at[NQB];
     u32x4 qf[NQB][QS];
     int lim[NQB], rows[NQB];
+    int root = 0;   // position of the tree's first row
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
       at[qb] = row_at(j, min(w.row0 + 16 * qb + fr, w.row_end - 1));
       const Entry e = entry_of(a, at[qb].b);
       lim[qb] = min(limit_of(a, e, at[qb].i), w.k1);
       rows[qb] = e.rows;
+      root = e.held - e.rows;
+    }
+    // keys up to `end` are in the steps on their way, those of a tree (from its 16-key group on) in others
+    int end = w.k1;
+    if constexpr (TREE) {
+      root = __builtin_amdgcn_readfirstlane(root);
+      end = min(max(max(root, 0) & ~15, w.k0), w.k1);
+#pragma unroll
+      for (int qb = 0; qb < NQB; ++qb) lim[qb] = min(lim[qb], end);
     }
 
     // table entries of a step's 16-key groups (past the last key: its page
@@ -304,25 +397,9 @@ struct Narrow {
       for (int db = 0; db < NDB; ++db) o[db][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    int k0 = w.k0 + wave * KS;
-    int id[NB];
-    if (k0 < w.k1) {
-      pages_at(k0, id);
-      load_k(k0, id);
-    }
-#pragma unroll
-    for (int qb = 0; qb < NQB; ++qb) {
-      const T* q = static_cast<const T*>(a.q.p) + at[qb].b * a.q.seq + at[qb].i * a.q.row +
-                   (kvh * j.group + at[qb].g) * a.q.head;
-#pragma unroll
-      for (int st = 0; st < QS; ++st) qf[qb][st] = *reinterpret_cast<const u32x4*>(q + (4 * st + g) * E);
-    }
-    if (k0 < w.k1) load_v(k0, id);
-    for (; k0 < w.k1; k0 += kWaves * KS) {
-      const int next = k0 + kWaves * KS;
-      const bool more = next < w.k1;
-      if (more) pages_at(next, id);
-      f32x4 sc[NB][NQB];
+    // the parts of a step, on the fragments loaded
+    typedef f32x4 Scores[NB][NQB];
+    auto score = [&](Scores& sc) {
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
@@ -331,19 +408,8 @@ struct Narrow {
 #pragma unroll
           for (int st = 0; st < QS; ++st) Mfma<T>::run(sc[kb][qb], kf[kb][st], qf[qb][st]);
         }
-      if (more) load_k(next, id);
-      bool all = true;
-#pragma unroll
-      for (int qb = 0; qb < NQB; ++qb) all = all && k0 + KS <= lim[qb];
-      if (!__all(all)) {
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
-#pragma unroll
-          for (int qb = 0; qb < NQB; ++qb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (k0 + key_of(kb, 4 * g + i) >= lim[qb]) sc[kb][qb][i] = -INFINITY;
-      }
+    };
+    auto softmax = [&](Scores& sc) {
       bool moved = false;
       float alpha[NQB];
 #pragma unroll
@@ -375,18 +441,21 @@ struct Narrow {
 #pragma unroll
           for (int db = 0; db < NDB; ++db) o[db][qb] *= alpha[qb];
       }
-      if (k0 + KS > w.k1) {   // values past the last key: whatever they are, times 0
+    };
+    // values past the last key: whatever they are, times 0
+    auto cut_values = [&](int k0) {
 #pragma unroll
-        for (int c = 0; c < NV; ++c) {
-          const int left = w.k1 - (k0 + (4 * c + g) * E);   // valid elements of this lane's chunks
+      for (int c = 0; c < NV; ++c) {
+        const int left = end - (k0 + (4 * c + g) * E);   // valid elements of this lane's chunks
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t keep = kHalf ? (left > 2 * x + 1 ? ~0u : left > 2 * x ? 0xffffu : 0u) : (left > x ? ~0u : 0u);
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t keep = kHalf ? (left > 2 * x + 1 ? ~0u : left > 2 * x ? 0xffffu : 0u) : (left > x ? ~0u : 0u);
 #pragma unroll
-            for (int db = 0; db < NDB; ++db) vf[db][c][x] &= keep;
-          }
+          for (int db = 0; db < NDB; ++db) vf[db][c][x] &= keep;
         }
       }
+    };
+    auto multiply = [&](const Scores& sc) {
 #pragma unroll
       for (int c = 0; c < NV; ++c)
 #pragma unroll
@@ -406,7 +475,126 @@ struct Narrow {
             else Mfma<float>::run(o[db][qb], vf[db][c], pf);
           }
         }
+    };
+
+    int k0 = w.k0 + wave * KS;
+    int id[NB];
+    if (k0 < end) {
+      pages_at(k0, id);
+      load_k(k0, id);
+    }
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      const T* q = static_cast<const T*>(a.q.p) + at[qb].b * a.q.seq + at[qb].i * a.q.row +
+                   (kvh * j.group + at[qb].g) * a.q.head;
+#pragma unroll
+      for (int st = 0; st < QS; ++st) qf[qb][st] = *reinterpret_cast<const u32x4*>(q + (4 * st + g) * E);
+    }
+    if (k0 < end) load_v(k0, id);
+    for (; k0 < end; k0 += kWaves * KS) {
+      const int next = k0 + kWaves * KS;
+      const bool more = next < end;
+      if (more) pages_at(next, id);
+      Scores sc;
+      score(sc);
+      if (more) load_k(next, id);
+      bool all = true;
+#pragma unroll
+      for (int qb = 0; qb < NQB; ++qb) all = all && k0 + KS <= lim[qb];
+      if (!__all(all)) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+          for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (k0 + key_of(kb, 4 * g + i) >= lim[qb]) sc[kb][qb][i] = -INFINITY;
+      }
+      softmax(sc);
+      if (k0 + KS > end) cut_values(k0);
+      multiply(sc);
       if (more) load_v(next, id);
+    }
+
+    if constexpr (TREE) {
+      // the tree's keys, which few steps hold: the first is the wave's whose turn it would be
+      const int steps = (max(end - w.k0, 0) + KS - 1) / KS, first = end + ((wave - steps) & (kWaves - 1)) * KS;
+      end = w.k1;
+      bool any_wild = false;
+      for (k0 = first; k0 < end; k0 += kWaves * KS) {
+        pages_at(k0, id);
+        load_k(k0, id);
+        constexpr bool kLate = !kHalf && NQB == 2;   // K and V together would spill
+        if (!kLate) load_v(k0, id);
+        Scores sc;
+        score(sc);
+        if (kLate) load_v(k0, id);
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          const uint64_t seen = seen_of(a, at[qb].b, at[qb].i, root, end, k0);
+#pragma unroll
+          for (int kb = 0; kb < NB; ++kb) {
+            const uint32_t bits = uint32_t(seen >> key_of(kb, 4 * g));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!(bits >> i & 1)) sc[kb][qb][i] = -INFINITY;
+          }
+        }
+        softmax(sc);
+        if (k0 + KS > end) cut_values(k0);
+        uint32_t wild = 0;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) wild |= wild_bits<kHalf>(vf[db][c][x]);
+        if (__any(wild)) {
+          any_wild = true;
+#pragma unroll
+          for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                asm volatile("" : "+v"(vf[db][c][x]));   // else what was found above is kept, a register a word
+                vf[db][c][x] = tame<kHalf>(vf[db][c][x]);
+              }
+        }
+        multiply(sc);
+      }
+      for (k0 = any_wild ? first : end; k0 < end; k0 += kWaves * KS) {
+        pages_at(k0, id);
+        load_v(k0, id);
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          const uint64_t seen = seen_of(a, at[qb].b, at[qb].i, root, end, k0);
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) {
+            f32x4 up = f32x4{0.f, 0.f, 0.f, 0.f}, down = up;
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+              const u32x4 sees = ones_of<kHalf>(uint32_t(seen >> ((4 * c + g) * E)));
+              u32x4 wu, wd;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const Wild y = wild_of<kHalf>(vf[db][c][x]);
+                wu[x] = y.up;
+                wd[x] = y.down;
+              }
+              if constexpr (kHalf) {
+                MfmaF16::run(up, wu, sees);
+                MfmaF16::run(down, wd, sees);
+              } else {
+                Mfma<float>::run(up, wu, sees);
+                Mfma<float>::run(down, wd, sees);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[db][qb][i] += wild_sum(up[i] > 0.f, down[i] > 0.f);
+          }
+        }
+      }
     }
 
     // join the waves' states, 16 rows at a time: wave w sums dim blocks w, w + 4, ..
@@ -434,7 +622,8 @@ struct Narrow {
       }
       const int row = w.row0 + 16 * qb + fr;
       const bool live = row < w.row_end && at[qb].i < rows[qb];
-      const float inv = lim[qb] > 0 ? 1.f / sum : 0.f;
+      const bool any = TREE ? sum != 0.f : lim[qb] > 0;   // the row sees a position
+      const float inv = any ? 1.f / sum : 0.f;
       T* out = static_cast<T*>(a.out.p) + at[qb].b * a.out.seq + at[qb].i * a.out.row +
                (kvh * j.group + at[qb].g) * a.out.head;
       float* rec = record_of(j, w.part, at[qb], kvh, HD);
@@ -447,7 +636,7 @@ struct Narrow {
         if (!live) continue;
         if (j.direct) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) store_f(out + 16 * db + 4 * g + i, lim[qb] > 0 ? x[i] * inv : 0.f);
+          for (int i = 0; i < 4; ++i) store_f(out + 16 * db + 4 * g + i, any ? x[i] * inv : 0.f);
         } else {
           *reinterpret_cast<f32x4*>(rec + 16 * db + 4 * g) = x;
         }
@@ -557,6 +746,25 @@ struct Tile {
       *p = x;
     }
   }
+  // whether any of the tile's values is infinite or no number, as one thread of `threads` finds it
+  __device__ __forceinline__ static bool wild_values(const uint8_t* sv, int t, int threads) {
+    uint32_t wild = 0;
+    for (int c = t; c < HD * 8; c += threads) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(sv + 16 * c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wild |= wild_bits<true>(x[i]);
+    }
+    return wild != 0;
+  }
+  __device__ __forceinline__ static void tame_values(uint8_t* sv, int t, int threads) {
+    for (int c = t; c < HD * 8; c += threads) {
+      u32x4* p = reinterpret_cast<u32x4*>(sv + 16 * c);
+      u32x4 x = *p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = tame<true>(x[i]);
+      *p = x;
+    }
+  }
   __device__ __forceinline__ static u32x4 key_chunk(const uint8_t* sk, int h, int st, int lane) {
     const int r = 32 * h + key_of(lane & 31);
     return *reinterpret_cast<const u32x4*>(sk + r * RB + (((2 * st + (lane >> 5)) ^ kswz(r)) << 4));
@@ -634,6 +842,52 @@ struct Rows32 {
     }
     l += sum;
   }
+  // scores of keys that the row does not see (bit: key of the block)
+  template <int H>
+  __device__ __forceinline__ static void hide(f32x16 (&sc)[H], uint64_t seen) {
+    const int f = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const uint32_t bits = uint32_t(seen >> (32 * h)) >> (8 * f);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(bits >> (16 * (i >> 3) + (i & 7)) & 1)) sc[h][i] = -INFINITY;
+    }
+  }
+  // What the products left out (see trees): infinite values and NaN among keys
+  // k0 .., 32 of every `step`, that row i of entry b sees, straight from memory.
+  __device__ __forceinline__ void bring_wild(const PagedAttn& a, const typename L::Copier& keys, const Share& w, int b,
+                                             int i, int root, int end, int k0, int step) {
+    const int fr = threadIdx.x & 31, f = (threadIdx.x >> 5) & 1, pmask = a.p.page_len - 1;
+    for (; k0 < w.k1; k0 += step) {
+      const uint32_t seen = uint32_t(seen_of(a, b, i, root, end, k0));
+#pragma unroll
+      for (int db = 0; db < L::NDB; ++db) {
+        f32x16 up, down;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) up[e] = down[e] = 0.f;
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          const int page = keys.in_pool(w.page(k0 + 16 * st, keys.shift, keys.last_block));
+          const u32x4 v = *reinterpret_cast<const u32x4*>(keys.V + page * keys.page_bytes +
+                                                          ((k0 + 16 * st + 8 * f) & pmask) * 2 +
+                                                          size_t(32 * db + fr) * (a.p.page_len * 2));
+          u32x4 wu, wd;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const Wild y = wild_of<true>(v[x]);
+            wu[x] = y.up;
+            wd[x] = y.down;
+          }
+          const half8 sees = __builtin_bit_cast(half8, ones_of<true>(seen >> (16 * st + 8 * f)));
+          up = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, wu), sees, up, 0, 0, 0);
+          down = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, wd), sees, down, 0, 0, 0);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] += wild_sum(up[e] > 0.f, down[e] > 0.f);
+      }
+    }
+  }
   // 2^(score - ref) in binary16, and their sum as rounded
   template <int H>
   __device__ __forceinline__ static float weights(const f32x16 (&sc)[H], float scale_log2, float ref, u32x4 (&pf)[2 * H]) {
@@ -662,7 +916,7 @@ struct Rows32 {
 // their way, whose copies are half as many a row; the same in two groups that
 // take turns at matrix and vector work.  64 rows a wave, alone on its SIMD with
 // products and softmax in one stream, took 350.
-template <int HD>
+template <int HD, bool TREE>
 struct Wide {
   using L = Tile<HD>;
   using Copier = typename L::Copier;
@@ -682,12 +936,14 @@ struct Wide {
     rows.begin();
     const Entry entry = entry_of(a, at.b);
     const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
+    const int root = TREE ? __builtin_amdgcn_readfirstlane(entry.held - entry.rows) : 0;   // the tree's first position
 
     int id[4];
     copier.pages_at(w, w.k0, id);
     if (w.k0 < w.k1) copier.issue(w.k0, id, lds0);
     copier.pages_at(w, w.k0 + kTile, id);
     int slot = 0;
+    bool any_wild = false;
     for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
       wait_vmcnt<0>();
       barrier_lds();   // tile k0 has landed; the other slot has been read
@@ -699,6 +955,12 @@ struct Wide {
       } else if (k0 + kTile < w.k1) {
         copier.issue(k0 + kTile, id, lds0 + (slot ^ 1) * L::BYTES);
         copier.pages_at(w, k0 + 2 * kTile, id);
+      }
+      const bool masked = TREE && k0 + kTile > root;
+      if (masked && __syncthreads_or(L::wild_values(sv, tid, kThreads))) {
+        any_wild = true;
+        L::tame_values(sv, tid, kThreads);
+        __syncthreads();
       }
       // every K fragment is on its way before the first product waits for one,
       // half of the V fragments before the softmax
@@ -715,7 +977,8 @@ struct Wide {
 #pragma unroll
         for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, st, db, lane);
       __builtin_amdgcn_sched_barrier(0);
-      rows.softmax(sc, k0, lim, j.scale_log2, pf);
+      if (masked) Rows32<HD>::hide(sc, seen_of(a, at.b, at.i, root, lim, k0));
+      rows.softmax(sc, k0, masked ? INT_MAX : lim, j.scale_log2, pf);
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
 #pragma unroll
@@ -726,7 +989,10 @@ struct Wide {
         }
       }
     }
+    if (TREE && any_wild)   // from the first tile that held keys of the tree
+      rows.bring_wild(a, copier, w, at.b, at.i, root, lim, w.k0 + max(root - w.k0, 0) / kTile * kTile, 32);
     const float l = pair_sum(rows.l);
+    const bool any = TREE ? l != 0.f : lim_row > 0;   // the row sees a position
     if (w.row0 + 32 * wave + fr >= w.row_end || at.i >= entry.rows) return;
     // element i of block db: dim 32 db + 8 (i / 4) + 4 f + i % 4
     if (j.direct) {
@@ -737,7 +1003,7 @@ struct Wide {
       for (int db = 0; db < L::NDB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          store_f(out + 32 * db + 8 * (i >> 2) + 4 * f + (i & 3), lim_row > 0 ? rows.o[db][i] * inv : 0.f);
+          store_f(out + 32 * db + 8 * (i >> 2) + 4 * f + (i & 3), any ? rows.o[db][i] * inv : 0.f);
     } else {
       float* rec = record_of(j, w.part, at, w.head, HD);
 #pragma unroll
@@ -762,7 +1028,7 @@ struct Wide {
 // the prefix is in LDS at a time; waves 0 .. 3 copy and use the first, 4 .. 7 the
 // second.  A tail's keys are few and used by one block alone: their fragments
 // come straight from memory.  The four states of a block are joined through LDS.
-template <int HD>
+template <int HD, bool TREE>
 struct Pairs {
   using L = Tile<HD>;
   static constexpr int kWays = 4;
@@ -789,7 +1055,7 @@ struct Pairs {
     const Entry e = entry_of(a, b);
     Share prefix{}, tail{};
     prefix.before = prefix.after = table_row(a, a.prefix_seq);
-    const int own_from = __builtin_amdgcn_readfirstlane(stacked_of(e, s, kKeys));
+    const int own_from = __builtin_amdgcn_readfirstlane(stacked_of<TREE>(e, s, kKeys));
     tail.split = s;
     tail.before = prefix.before;
     tail.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
@@ -841,6 +1107,8 @@ struct Pairs {
 
     // this block's own keys
     const int pmask = a.p.page_len - 1;
+    const int root = __builtin_amdgcn_readfirstlane(e.held - e.rows);   // the tree's first position
+    bool any_wild = false;
     for (int k0 = own_from + 32 * way; k0 < e.held; k0 += kKeys) {
       const int p0 = own_keys.in_pool(tail.page(k0, own_keys.shift, own_keys.last_block));
       const int p1 = own_keys.in_pool(tail.page(k0 + 16, own_keys.shift, own_keys.last_block));
@@ -867,11 +1135,31 @@ struct Pairs {
         }
       }
       rows.scores(kf, sc);
-      rows.softmax(sc, k0, limit, j.scale_log2, pf);
+      const bool masked = TREE && k0 + 32 > root;
+      if (masked) {
+        Rows32<HD>::hide(sc, seen_of(a, b, i, root, limit, k0));
+        uint32_t wild = 0;
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int db = 0; db < L::NDB; ++db)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              wild |= wild_bits<true>(vf[st][db][c]);
+              vf[st][db][c] = tame<true>(vf[st][db][c]);
+            }
+        any_wild = any_wild || __any(wild);
+      }
+      rows.softmax(sc, k0, masked ? INT_MAX : limit, j.scale_log2, pf);
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int db = 0; db < L::NDB; ++db) rows.add(db, vf[st][db], pf[st]);
+    }
+    if (TREE && any_wild) {   // from this way's first step that held keys of the tree
+      tail.k1 = e.held;
+      const int first_own = own_from + 32 * way, steps = max(root - first_own - 31 + kKeys - 1, 0) / kKeys;
+      rows.bring_wild(a, own_keys, tail, b, i, root, limit, first_own + steps * kKeys, kKeys);
     }
 
     // join the ways, two dim blocks at a time: way v sums 8 of a lane's 32 elements
@@ -900,6 +1188,7 @@ struct Pairs {
         l += xs[(v * STATE + 33) * kWave] * wt[v];
       }
       const float inv = 1.f / l;
+      const bool any = TREE ? l != 0.f : limit > 0;   // the row sees a position
 #pragma unroll
       for (int c = 0; c < 8; c += 4) {
         const int c0 = 8 * way + c;   // element c0 % 16 of block d2 + c0 / 16
@@ -911,17 +1200,17 @@ struct Pairs {
         if (live) {
 #pragma unroll
           for (int u = 0; u < 4; ++u)
-            store_f(out + 32 * (d2 + (c0 >> 4)) + 2 * (c0 & 15) + 4 * f + u, limit > 0 ? y[u] * inv : 0.f);
+            store_f(out + 32 * (d2 + (c0 >> 4)) + 2 * (c0 & 15) + 4 * f + u, any ? y[u] * inv : 0.f);
         }
       }
     }
   }
 };
 
-template <int HD>
-__global__ __launch_bounds__(Pairs<HD>::kPairThreads, 2) void pairs_kernel(Job j) {
-  __shared__ __attribute__((aligned(16))) uint8_t smem[Pairs<HD>::SMEM];
-  Pairs<HD>::run(j, blockIdx.x, smem);
+template <int HD, bool TREE>
+__global__ __launch_bounds__((Pairs<HD, TREE>::kPairThreads), 2) void pairs_kernel(Job j) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[Pairs<HD, TREE>::SMEM];
+  Pairs<HD, TREE>::run(j, blockIdx.x, smem);
 }
 
 // ---------------------------------------------------------------- launch
@@ -930,23 +1219,23 @@ __global__ __launch_bounds__(Pairs<HD>::kPairThreads, 2) void pairs_kernel(Job j
 enum { ROWS16 = 1, ROWS32 = 2, ROWS128 = 3 };
 constexpr int rows_of(int mode) { return mode == ROWS16 ? 16 : mode == ROWS32 ? 32 : 128; }
 
-template <typename T, int HD, int MODE> struct Taker;
-template <typename T, int HD> struct Taker<T, HD, ROWS16> : Narrow<T, HD, 1> {};
-template <typename T, int HD> struct Taker<T, HD, ROWS32> : Narrow<T, HD, 2> {};
-template <int HD> struct Taker<bf16_t, HD, ROWS128> : Wide<HD> {};
+template <typename T, int HD, int MODE, bool TREE> struct Taker;
+template <typename T, int HD, bool TREE> struct Taker<T, HD, ROWS16, TREE> : Narrow<T, HD, 1, TREE> {};
+template <typename T, int HD, bool TREE> struct Taker<T, HD, ROWS32, TREE> : Narrow<T, HD, 2, TREE> {};
+template <int HD, bool TREE> struct Taker<bf16_t, HD, ROWS128, TREE> : Wide<HD, TREE> {};
 
-// both parts in one launch: prefix workgroups, then the tails'
-template <typename T, int HD, int PREFIX, int TAIL>
+// both parts in one launch: prefix workgroups, then the tails' (trees are in those alone)
+template <typename T, int HD, int PREFIX, int TAIL, bool TREE>
 __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Job j, int prefix_blocks) {
-  using P = Taker<T, HD, PREFIX>;
-  using U = Taker<T, HD, TAIL>;
+  using P = Taker<T, HD, PREFIX, false>;
+  using U = Taker<T, HD, TAIL, TREE>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[P::SMEM > U::SMEM ? P::SMEM : U::SMEM];
   Share w;
   const int x = blockIdx.x;
   if (x < prefix_blocks) {
-    if (share_of(j, x, true, rows_of(PREFIX), w)) P::run(j, w, smem);
+    if (share_of<TREE>(j, x, true, rows_of(PREFIX), w)) P::run(j, w, smem);
   } else {
-    if (share_of(j, x - prefix_blocks, false, rows_of(TAIL), w)) U::run(j, w, smem);
+    if (share_of<TREE>(j, x - prefix_blocks, false, rows_of(TAIL), w)) U::run(j, w, smem);
   }
 }
 
@@ -955,7 +1244,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Job j, int prefi
 // out[row] = sum_r o_r 2^(m_r - m) / sum_r l_r 2^(m_r - m) over the ranges that
 // hold positions the row sees; HD / 4 lanes a row and slice, slice c takes the
 // ranges c, c + slices, .., and the slices are joined in order.
-template <typename T, int HD>
+template <typename T, int HD, bool TREE>
 __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   constexpr int kLanes = HD / 4;
   __shared__ __attribute__((aligned(16))) float part[kThreads / kLanes][HD + 4];
@@ -966,7 +1255,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   const int h = row % a.heads, t = row / a.heads, b = in ? t / a.max_rows : 0, i = t % a.max_rows;
   const Entry e = entry_of(a, b);
   const bool live = in && i < e.rows;
-  const int s = j.stacked ? stacked_of(e, shared_of(a), j.prefix.range) : 0, lim = limit_of(a, e, i);
+  const int s = j.stacked ? stacked_of<TREE>(e, shared_of(a), j.prefix.range) : 0, lim = limit_of(a, e, i);
   const int np = live && j.prefix.ranges ? (min(lim, s) + j.prefix.range - 1) / j.prefix.range : 0;
   const int nt = live && lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
   const size_t stride = size_t(a.n) * a.max_rows * a.heads * record(HD);
@@ -1010,7 +1299,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   if (!live) return;
   T* out = static_cast<T*>(a.out.p) + b * a.out.seq + i * a.out.row + h * a.out.head + c;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) store_f(out + x, lim > 0 ? o[x] / l : 0.f);
+  for (int x = 0; x < 4; ++x) store_f(out + x, (TREE ? l != 0.f : lim > 0) ? o[x] / l : 0.f);
 }
 
 // ---------------------------------------------------------------- host
@@ -1074,37 +1363,37 @@ Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys, d
   return p;
 }
 
-template <typename T, int HD, int PREFIX, int TAIL>
+template <typename T, int HD, int PREFIX, int TAIL, bool TREE>
 void launch_parts(const Job& j, hipStream_t s) {
   const int kvh = j.a.p.n_kv_heads;
   const int prefix = j.prefix.ranges ? blocks_of(j.prefix.ranges * kvh, j.prefix.row_tiles) : 0;
   const int tail = blocks_of(j.a.n * j.tail.ranges * kvh, j.tail.row_tiles);
-  hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL>), dim3(prefix + tail),
+  hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL, TREE>), dim3(prefix + tail),
                      dim3(kThreads), 0, s, j, prefix);
 }
 
 // (a prefix never takes fewer rows than the tails, see divide)
-template <typename T, int HD>
+template <typename T, int HD, bool TREE>
 void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (tail == ROWS128) return launch_parts<T, HD, ROWS128, ROWS128>(j, s);
+    if (tail == ROWS128) return launch_parts<T, HD, ROWS128, ROWS128, TREE>(j, s);
     if (prefix == ROWS128)
-      return tail == ROWS32 ? launch_parts<T, HD, ROWS128, ROWS32>(j, s) : launch_parts<T, HD, ROWS128, ROWS16>(j, s);
+      return tail == ROWS32 ? launch_parts<T, HD, ROWS128, ROWS32, TREE>(j, s) : launch_parts<T, HD, ROWS128, ROWS16, TREE>(j, s);
   }
-  if (tail == ROWS32) return launch_parts<T, HD, ROWS32, ROWS32>(j, s);
-  return prefix == ROWS32 ? launch_parts<T, HD, ROWS32, ROWS16>(j, s) : launch_parts<T, HD, ROWS16, ROWS16>(j, s);
+  if (tail == ROWS32) return launch_parts<T, HD, ROWS32, ROWS32, TREE>(j, s);
+  return prefix == ROWS32 ? launch_parts<T, HD, ROWS32, ROWS16, TREE>(j, s) : launch_parts<T, HD, ROWS16, ROWS16, TREE>(j, s);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool TREE>
 void launch(const Job& j, int prefix, int tail, hipStream_t s) {
-  launch_modes<T, HD>(j, prefix, tail, s);
+  launch_modes<T, HD, TREE>(j, prefix, tail, s);
   if (j.direct) return;
   // rows of many ranges take several groups of lanes each: the records of a
   // row come in turn, four at a time
   constexpr int kGroups = kThreads / (HD / 4);
   const int ranges = j.prefix.ranges + j.tail.ranges;
   const int slices = ranges <= 4 ? 1 : ranges <= 8 ? 2 : ranges <= 16 ? 4 : 8;
-  hipLaunchKernelGGL((join_kernel<T, HD>), dim3(cdiv(j.a.n * j.a.max_rows * j.a.heads, kGroups / slices)),
+  hipLaunchKernelGGL((join_kernel<T, HD, TREE>), dim3(cdiv(j.a.n * j.a.max_rows * j.a.heads, kGroups / slices)),
                      dim3(kThreads), 0, s, j, slices);
 }
 
@@ -1172,7 +1461,7 @@ double parts_us(const PagedAttn& a, int mode, Cost x, Cost y, int records) {
 // the prefix, then of the tail
 double pairs_us(const PagedAttn& a, int rows, int64_t shared, double tail) {
   const double u = a.p.head_dim / 128.0, all = double(a.n) * cdiv(rows, 32) * a.p.n_kv_heads;
-  return std::ceil(all / (2 * kCus)) * (4.8 + u * (3.4 + (1.45 * shared + 3.5 * tail) / Pairs<128>::kKeys));
+  return std::ceil(all / (2 * kCus)) * (4.8 + u * (3.4 + (1.45 * shared + 3.5 * tail) / Pairs<128, false>::kKeys));
 }
 
 // how a call is taken: pairs, or a prefix (stacked) and tails
@@ -1221,7 +1510,10 @@ Division divide(const PagedAttn& a) {
 
 }  // namespace
 
-hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
+namespace {
+
+template <bool TREE>
+hipError_t attend(const PagedAttn& a, hipStream_t s) {
   Job j{};
   j.a = a;
   j.scale_log2 = a.scale * 1.4426950408889634f;
@@ -1231,8 +1523,9 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   if (d.pairs) {
     j.direct = true;
     const int grid = blocks_of(kvh, cdiv(a.n * cdiv(a.max_rows * j.group, 32), 2));
-    if (hd == 128) hipLaunchKernelGGL(pairs_kernel<128>, dim3(grid), dim3(Pairs<128>::kPairThreads), 0, s, j);
-    else hipLaunchKernelGGL(pairs_kernel<64>, dim3(grid), dim3(Pairs<64>::kPairThreads), 0, s, j);
+    constexpr int kPairThreads = Pairs<128, TREE>::kPairThreads;
+    if (hd == 128) hipLaunchKernelGGL((pairs_kernel<128, TREE>), dim3(grid), dim3(kPairThreads), 0, s, j);
+    else hipLaunchKernelGGL((pairs_kernel<64, TREE>), dim3(grid), dim3(kPairThreads), 0, s, j);
     return hipGetLastError();
   }
   j.prefix = d.prefix;
@@ -1241,11 +1534,15 @@ hipError_t paged_attention(const PagedAttn& a, hipStream_t s) {
   if (d.shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
   if (a.p.dtype == DLLM_BF16)
-    hd == 128 ? launch<bf16_t, 128>(j, d.mode_p, d.mode_t, s) : launch<bf16_t, 64>(j, d.mode_p, d.mode_t, s);
+    hd == 128 ? launch<bf16_t, 128, TREE>(j, d.mode_p, d.mode_t, s) : launch<bf16_t, 64, TREE>(j, d.mode_p, d.mode_t, s);
   else
-    hd == 128 ? launch<float, 128>(j, d.mode_p, d.mode_t, s) : launch<float, 64>(j, d.mode_p, d.mode_t, s);
+    hd == 128 ? launch<float, 128, TREE>(j, d.mode_p, d.mode_t, s) : launch<float, 64, TREE>(j, d.mode_p, d.mode_t, s);
   return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t paged_attention(const PagedAttn& a, hipStream_t s) { return a.mask ? attend<true>(a, s) : attend<false>(a, s); }
 
 kv_attention_plan paged_attention_plan(const PagedAttn& a) {
   const Division d = divide(a);

@@ -352,6 +352,67 @@ __global__ __launch_bounds__(256) void free_apply_kernel(dllm_kv_pages p, const 
   for (int j = first + blockIdx.x * 256 + threadIdx.x; j < p.max_blocks; j += gridDim.x * 256) drop_entry(p, s, j);
 }
 
+// Acceptance plan: checks, the pages of the rows that are kept (`from`, [n][max_path])
+// before the tables are cut; accept_kernel moves the rows.  Paths and their pages
+// are gone through by all threads together.
+__global__ __launch_bounds__(kPlanThreads) void pages_accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs,
+                                                                    int n, int max_rows,
+                                                                    const int32_t* __restrict__ n_rows,
+                                                                    const int32_t* __restrict__ path, int max_path,
+                                                                    const int32_t* __restrict__ n_path, int32_t* from,
+                                                                    int32_t* status, bool drop_here) {
+  __shared__ PlanShared sh;
+  __shared__ int rows_of[KV_MAX_SEQS];
+  const int tid = threadIdx.x;
+  int err = kNoError, s = -1, first = 0, rows = 0, m = 0, held = 0;
+  const int want = tid < n ? seqs[tid] : 0, want_m = tid < n ? n_path[tid] : 0;
+  const int want_r = n_rows && tid < n ? n_rows[tid] : max_rows;
+  plan_begin(sh);
+  if (tid < n) {
+    s = check_seq(p, want, sh, err);
+    if (err == kNoError) {
+      held = held_of(p, s);
+      rows = want_r;
+      m = want_m;
+      first = held - rows;
+      if (rows < 0 || rows > max_rows || first < 0 || m < 0 || m > min(rows, max_path)) err = KV_PAGES_ELEN;
+    }
+  }
+  sh.seq[tid] = s;
+  sh.first[tid] = first;
+  sh.off[tid] = m;
+  rows_of[tid] = rows;
+  err = plan_error(err, sh);
+  __syncthreads();   // every thread has read the first check's error before the second adds to it
+  if (err == kNoError) {
+    auto page_of = [&](int i, int pos) { return p.table[size_t(sh.seq[i]) * p.max_blocks + pos / p.page_len]; };
+    auto shared = [&](int page) { return page >= 0 && page < p.n_pages && p.refs[page] > 1; };
+    for (int t = tid; t < n * max_path; t += kPlanThreads) {
+      const int i = t / max_path, j = t % max_path;
+      if (j >= sh.off[i]) continue;
+      const int r = path[t], before = j ? path[t - 1] : -1;
+      if (r <= before || r >= rows_of[i]) {
+        err = min(err, int(KV_PAGES_EPATH));
+        continue;
+      }
+      from[t] = page_of(i, sh.first[i] + r);
+      if (r != j && shared(page_of(i, sh.first[i] + j))) err = min(err, int(KV_PAGES_ESHARED));
+    }
+    if (tid < n && first + m < held && (first + m) % p.page_len && shared(page_of(tid, first + m)))
+      err = min(err, int(KV_PAGES_ESHARED));
+    err = plan_error(err, sh);
+  }
+  if (err == kNoError) {
+    if (tid < n) p.len[s] = first + m;
+    if (drop_here)
+      for (int t = tid; t < n * p.max_blocks; t += kPlanThreads) {
+        const int i = t / p.max_blocks, j = t % p.max_blocks;
+        if (j >= blocks_of(sh.first[i] + sh.off[i], p.page_len)) drop_entry(p, sh.seq[i], j);
+      }
+  }
+  if (tid == 0) *status = err == kNoError ? KV_PAGES_OK : err;
+}
+
 // Compaction plan in the workspace: [0] pages moved, then their new ids by
 // old id (from n_used on), the old ids and the new ones by rank.
 struct CompactPlan {
@@ -426,21 +487,66 @@ __global__ __launch_bounds__(kCopyThreads) void compact_apply_kernel(dllm_kv_pag
   }
 }
 
+// Rows of accepted paths to their places.  Every thread moves one strand of an
+// entry, layer and head: 16 bytes of the keys' rows, or one dim of the values,
+// along the whole path.  A row's place is never behind where it comes from and
+// rows ascend, so a strand that reads some rows, in order, and then writes them
+// overwrites none that it still has to read; strands do not meet.
+constexpr int kMoveThreads = 256;
+constexpr int kMoveRows = 8;
+template <typename T, int HD>
+__global__ __launch_bounds__(kMoveThreads) void accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs, int n,
+                                                              int max_rows, const int32_t* __restrict__ n_rows,
+                                                              const int32_t* __restrict__ path, int max_path,
+                                                              const int32_t* __restrict__ n_path,
+                                                              const int32_t* __restrict__ from, int key_wgs,
+                                                              const int32_t* __restrict__ status) {
+  constexpr int E = 16 / int(sizeof(T)), CK = HD / E;
+  if (*status != KV_PAGES_OK) return;
+  const bool keys = int(blockIdx.x) < key_wgs;
+  const int64_t t = int64_t(keys ? blockIdx.x : blockIdx.x - key_wgs) * kMoveThreads + threadIdx.x;
+  const int strand = int(t % (keys ? CK : HD)), heads = p.n_kv_heads;
+  const int64_t item = t / (keys ? CK : HD);
+  const int h = int(item % heads), layer = int(item / heads % p.n_layers);
+  if (item / heads / p.n_layers >= n) return;
+  const int b = int(item / heads / p.n_layers);
+  const int s = seqs[b], m = n_path[b], first = p.len[s] - m;   // the length is the new one
+  const int32_t* pages = p.table + size_t(s) * p.max_blocks;
+  const int mask = p.page_len - 1;
+  // element 0 of the strand's head in a page
+  auto head_of = [&](int page) { return ((size_t(layer) * p.n_pages + page) * heads + h) * p.page_len * HD; };
+  auto at = [&](int page, int pos) {
+    const int slot = pos & mask;
+    return head_of(page) + (keys ? size_t(slot) * HD + strand * E : size_t(strand) * p.page_len + slot);
+  };
+  for (int j0 = 0; j0 < m; j0 += kMoveRows) {
+    u32x4 x[kMoveRows];
+    T y[kMoveRows];
+    bool move[kMoveRows];
+    size_t to[kMoveRows];
+#pragma unroll
+    for (int u = 0; u < kMoveRows; ++u) {
+      const int j = min(j0 + u, m - 1), r = path[size_t(b) * max_path + j];
+      const int a = from[size_t(b) * max_path + j], c = pages[(first + j) / p.page_len];
+      move[u] = j0 + u < m && r != j && a >= 0 && a < p.n_pages && c >= 0 && c < p.n_pages;
+      if (!move[u]) continue;
+      to[u] = at(c, first + j);
+      if (keys) x[u] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.k) + at(a, first + r));
+      else y[u] = static_cast<const T*>(p.vt)[at(a, first + r)];
+    }
+#pragma unroll
+    for (int u = 0; u < kMoveRows; ++u) {
+      if (!move[u]) continue;
+      if (keys) *reinterpret_cast<u32x4*>(static_cast<T*>(p.k) + to[u]) = x[u];
+      else static_cast<T*>(p.vt)[to[u]] = y[u];
+    }
+  }
+}
+
 // ---------------------------------------------------------------- rows
 
 constexpr int kWriteThreads = 256;
 constexpr int kWriteTile = 64;   // positions per workgroup, from a multiple of 64: pages are cut there too
-
-// values as the pages of bf16 models hold them: rounded to binary16, past its
-// range the largest of their sign (what saturating first gives), a NaN as it is
-// (the median that saturates elsewhere returns the lowest of the others for one)
-__device__ __forceinline__ uint32_t pack_values(float a, float b) {
-  typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-  const half2v most = {65504, 65504}, v = __builtin_bit_cast(half2v, pack_f16x2(a, b));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_maximum(__builtin_elementwise_minimum(v, most), -most));
-}
-__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_value(bf16_t* p, float v) { p->bits = uint16_t(pack_values(v, 0.f)); }
 
 __device__ __forceinline__ int row_count(const int32_t* n_rows, int b, int max_rows) {
   return n_rows ? min(max(n_rows[b], 0), max_rows) : max_rows;
@@ -605,6 +711,29 @@ hipError_t pages_free(const dllm_kv_pages& p, const int32_t* seqs, const int32_t
     hipLaunchKernelGGL(free_apply_kernel, dim3(std::min(cdiv(p.max_blocks, 256), 64), n), dim3(256), 0, s, p, seqs,
                        status);
   return hipGetLastError();
+}
+
+hipError_t pages_accept(const dllm_kv_pages& p, const int32_t* seqs, int n, int max_rows, const int32_t* n_rows,
+                        const int32_t* path, int max_path, const int32_t* n_path, int32_t* status, void* ws,
+                        hipStream_t s) {
+  int32_t* from = static_cast<int32_t*>(ws);
+  const bool here = int64_t(n) * p.max_blocks <= kDropHere;
+  hipLaunchKernelGGL(pages_accept_kernel, dim3(1), dim3(kPlanThreads), 0, s, p, seqs, n, max_rows, n_rows, path, max_path,
+                     n_path, from, status, here);
+  if (!here)
+    hipLaunchKernelGGL(free_apply_kernel, dim3(std::min(cdiv(p.max_blocks, 256), 64), n), dim3(256), 0, s, p, seqs,
+                       status);
+  auto launch = [&](auto kernel, int chunks) {
+    const int64_t items = int64_t(n) * p.n_layers * p.n_kv_heads;
+    const int64_t key_wgs = (items * chunks + kMoveThreads - 1) / kMoveThreads;
+    const int64_t wgs = key_wgs + (items * p.head_dim + kMoveThreads - 1) / kMoveThreads;
+    hipLaunchKernelGGL(kernel, dim3(uint32_t(wgs)), dim3(kMoveThreads), 0, s, p, seqs, n, max_rows, n_rows, path, max_path,
+                       n_path, from, int(key_wgs), status);
+    return hipGetLastError();
+  };
+  if (p.dtype == DLLM_BF16)
+    return p.head_dim == 128 ? launch(accept_kernel<bf16_t, 128>, 16) : launch(accept_kernel<bf16_t, 64>, 8);
+  return p.head_dim == 128 ? launch(accept_kernel<float, 128>, 32) : launch(accept_kernel<float, 64>, 16);
 }
 
 size_t pages_compact_workspace(int n_pages) { return (16 + 3 * size_t(n_pages)) * sizeof(int32_t); }
