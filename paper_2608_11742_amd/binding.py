@@ -445,15 +445,23 @@ def _turned(owner, x, out, dtype, n: int, rows: int, name: str):
     """x and out [n, rows, heads, head_dim] as heads and two dllm_rows; none without x."""
     if x is None:
         return 0, None, None
-    if out is None or out.shape != x.shape or x.dim() != 4 or x.shape[:2] != (n, rows) or x.shape[3] != owner.head_dim:
+    b, i, heads, hd = shape = x.shape
+    if b != n or i != rows or hd != owner.head_dim or out is None or out.shape != shape:
         raise ValueError(f"{name} and its output are [entries, rows, heads, head_dim], of the same entries, rows and head_dim")
-    heads, at = x.shape[2], []
-    for t in (x, out):
-        seq, row, head, one = t.stride()
-        if one != 1 or t.dtype is not dtype or t.get_device() != owner._index:
-            raise ValueError(f"{name} must have contiguous rows, one type, and the device of the other arrays")
-        at.append(_Rows(t.data_ptr(), seq if n > 1 else 0, row if rows > 1 else 0, head if heads > 1 else 0))
-    return heads, at[0], at[1]
+    index = owner._index
+    seq, row, head, one = x.stride()
+    seq_o, row_o, head_o, one_o = out.stride()
+    if (one != 1 or one_o != 1 or x.dtype is not dtype or out.dtype is not dtype or x.get_device() != index
+            or out.get_device() != index):
+        raise ValueError(f"{name} must have contiguous rows, one type, and the device of the other arrays")
+    # a dimension of one has no stride to speak of
+    if n == 1:
+        seq = seq_o = 0
+    if rows == 1:
+        row = row_o = 0
+    if heads == 1:
+        head = head_o = 0
+    return heads, _Rows(x.data_ptr(), seq, row, head), _Rows(out.data_ptr(), seq_o, row_o, head_o)
 
 
 _DTYPES = {torch.bfloat16: DLLM_BF16, torch.float32: DLLM_F32}
@@ -463,14 +471,18 @@ def rotary_rows(rot: Rotary, q, q_out, k=None, k_out=None, pos=None, pos_offset:
     """q [entries, rows, heads, head_dim] (and k, with heads of its own) normed and rotated into q_out (and k_out);
     pos [entries, rows], or row i is at pos_offset + i.  The outputs may be the inputs."""
     x = k if q is None else q
-    n, rows = x.shape[:2]
-    dtype = _DTYPES.get(x.dtype)
+    n, rows, _, _ = x.shape
+    t = x.dtype
+    dtype = _DTYPES.get(t)
     if dtype is None:
         raise ValueError("rows are bf16 or fp32")
-    hq, qi, qo = _turned(rot, q, q_out, x.dtype, n, rows, "q")
-    hk, ki, ko = _turned(rot, k, k_out, x.dtype, n, rows, "k")
-    _check(lib().rotary_rows(rot._ref, dtype, _positions(rot, pos, n, rows), pos_offset, n, rows, _ids(rot, n_rows, n),
-                             hq, qi, qo, hk, ki, ko, _page_stream(rot, stream)))
+    hq, qi, qo = _turned(rot, q, q_out, t, n, rows, "q")
+    hk, ki, ko = _turned(rot, k, k_out, t, n, rows, "k")
+    status = lib().rotary_rows(rot._ref, dtype, None if pos is None else _positions(rot, pos, n, rows), pos_offset, n, rows,
+                               None if n_rows is None else _ids(rot, n_rows, n), hq, qi, qo, hk, ki, ko,
+                               _page_stream(rot, stream))
+    if status:
+        _check(status)
 
 
 def kv_pages_append(pages: KvPages, layer: int, seqs, k, v, rot: Rotary, q=None, q_out=None, pos=None, n_rows=None,

@@ -80,6 +80,8 @@ struct Job {
   Part prefix, tail;
   bool stacked;       // the prefix is a part of its own; else each tail starts at position 0
   bool direct;        // one range in all: the output itself
+  bool by_length;     // the tails' ranges go to the entries by their lengths (see Slots),
+  int least;          // in steps of at least so many tiles
 };
 
 __device__ __forceinline__ int most_positions(const PagedAttn& a) { return a.p.max_blocks * a.p.page_len; }
@@ -128,7 +130,9 @@ __device__ __forceinline__ table_t table_row(const PagedAttn& a, int seq) {
 // group + query head) of key head `head`, keys k0 .. k1 - 1, record index.
 // Pages of positions before `split` are `before`'s, then `after`'s.
 struct Share {
-  int row0, row_end, head, k0, k1, part, split;
+  int row0, row_end, head, k0, k1, split;
+  int64_t rec0;   // of the share's records: that of row 0 of all entries would be here
+  Entry e;        // of a tail
   table_t before, after;
   __device__ __forceinline__ int page(int pos, int shift, int last_block) const {
     return (pos < split ? before : after)[min(pos >> shift, last_block)];
@@ -148,6 +152,49 @@ __device__ __forceinline__ Item item_of(int x, int row_tiles) {
 }
 int blocks_of(int items, int row_tiles) { return cdiv(items, 8) * 8 * row_tiles; }
 
+// v of the lane that `CTRL` moves here (0 where the rows of ROWS do not take part)
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int moved(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+// sums of v over the lanes up to each one
+__device__ __forceinline__ int wave_sums(int v) {
+  v += moved<0x111>(v);   // the lanes 1, 2, 4, 8 before it in its 16
+  v += moved<0x112>(v);
+  v += moved<0x114>(v);
+  v += moved<0x118>(v);
+  v += moved<0x142, 0xa>(v);   // the last of the 16 before, and of the 32
+  v += moved<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_sums(v), kWave - 1); }
+
+// The tails of trees are divided by what the entries hold: of the n * ranges
+// slots that a head and row tile have, an entry gets one for every `step` keys,
+// the least step with which all find a slot.  So one long entry among short
+// ones, or a max_len that is far off, leaves no workgroup without work.  Every
+// wave works it out from the lengths, a lane for each of up to 64 entries.
+struct Slots {
+  Entry e;                   // of this lane
+  int count, first, tiles;   // its slots, and the tiles in them
+};
+template <bool TREE>
+__device__ __forceinline__ Slots slots_of(const Job& j, int shared) {
+  const int lane = threadIdx.x & 63, all = j.a.n * j.tail.ranges;
+  Slots s{};
+  if (lane < j.a.n) {
+    s.e = entry_of(j.a, lane);
+    const int from = j.stacked ? stacked_of<TREE>(s.e, shared, j.prefix.range) : 0;
+    s.tiles = s.e.rows > 0 ? (s.e.held - from + kTile - 1) / kTile : 0;
+  }
+  int step = max((wave_total(s.tiles) + all - 1) / all, j.least), used;
+  // at most a slot too many an entry: the step grows until they fit
+  while (s.count = (s.tiles + step - 1) / step, used = wave_total(s.count), used > all)
+    step += max(1, int(int64_t(step) * (used - all) / all));
+  s.first = wave_sums(s.count) - s.count;
+  return s;
+}
+
 // False if the share is empty.
 template <bool TREE>
 __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, int tile_rows, Share& w) {
@@ -156,25 +203,43 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
   const Part& part = in_prefix ? j.prefix : j.tail;
   const Item it = item_of(x, part.row_tiles);
   w.head = it.item % a.p.n_kv_heads;
-  const int t = it.item / a.p.n_kv_heads, r = t % part.ranges, b = t / part.ranges;
+  const int t = it.item / a.p.n_kv_heads;
+  int r = t % part.ranges, b = t / part.ranges;
   if (b >= (in_prefix ? 1 : a.n)) return false;   // items are filled up to whole rounds of XCDs
   const int s = shared_of(a);
+  const int64_t rows_all = int64_t(a.n) * a.max_rows * a.heads;
   if (in_prefix) {
     w.row0 = it.tile * tile_rows;
     w.row_end = a.n * per;
     w.k0 = r * part.range;
     w.k1 = min(w.k0 + part.range, s);
-    w.part = r;
+    w.rec0 = r * rows_all;
     w.split = 0;
     w.before = w.after = table_row(a, a.prefix_seq);
     return w.k0 < w.k1;
   }
-  const Entry e = entry_of(a, b);
+  int range = part.range, ranges = part.ranges;
+  w.rec0 = (j.prefix.ranges + r) * rows_all;
+  if (TREE && j.by_length) {
+    const Slots z = slots_of<TREE>(j, s);
+    // slot t is of the last entry that starts at or before it (one without any starts where the next does)
+    b = __popcll(__ballot(int(threadIdx.x & 63) < a.n && z.first <= t)) - 1;
+    r = t - __builtin_amdgcn_readlane(z.first, b);
+    ranges = __builtin_amdgcn_readlane(z.count, b);
+    if (r >= ranges) return false;
+    const int tiles = __builtin_amdgcn_readlane(z.tiles, b);
+    range = (tiles + ranges - 1) / ranges * kTile;   // even
+    w.rec0 = j.prefix.ranges * rows_all + int64_t(t - b) * a.max_rows * a.heads;
+    w.e = Entry{__builtin_amdgcn_readlane(z.e.seq, b), __builtin_amdgcn_readlane(z.e.held, b),
+                __builtin_amdgcn_readlane(z.e.rows, b)};
+  } else {
+    w.e = entry_of(a, b);
+  }
+  const Entry& e = w.e;
   w.row0 = b * per + it.tile * tile_rows;
   w.row_end = (b + 1) * per;
-  w.k0 = (j.stacked ? stacked_of<TREE>(e, s, j.prefix.range) : 0) + r * part.range;
-  w.k1 = r + 1 == part.ranges ? e.held : min(w.k0 + part.range, e.held);
-  w.part = j.prefix.ranges + r;
+  w.k0 = (j.stacked ? stacked_of<TREE>(e, s, j.prefix.range) : 0) + r * range;
+  w.k1 = r + 1 == ranges ? e.held : min(w.k0 + range, e.held);
   w.split = s;
   w.before = table_row(a, a.prefix_seq);
   w.after = table_row(a, __builtin_amdgcn_readfirstlane(max(e.seq, 0)));
@@ -195,9 +260,9 @@ __device__ __forceinline__ RowAt row_at(const Job& j, int row) {
   return r;
 }
 
-__device__ __forceinline__ float* record_of(const Job& j, int part, const RowAt& r, int kvh, int hd) {
-  const size_t row = (size_t(r.b) * j.a.max_rows + r.i) * j.a.heads + kvh * j.group + r.g;
-  return j.a.part + (size_t(part) * j.a.n * j.a.max_rows * j.a.heads + row) * record(hd);
+__device__ __forceinline__ float* record_of(const Job& j, int64_t rec0, const RowAt& r, int kvh, int hd) {
+  const int64_t row = (int64_t(r.b) * j.a.max_rows + r.i) * j.a.heads + kvh * j.group + r.g;
+  return j.a.part + (rec0 + row) * record(hd);
 }
 
 // lane l's value of lanes l, l ^ 32 joined
@@ -343,7 +408,7 @@ struct Narrow {
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
       at[qb] = row_at(j, min(w.row0 + 16 * qb + fr, w.row_end - 1));
-      const Entry e = entry_of(a, at[qb].b);
+      const Entry e = TREE ? w.e : entry_of(a, at[qb].b);
       lim[qb] = min(limit_of(a, e, at[qb].i), w.k1);
       rows[qb] = e.rows;
       root = e.held - e.rows;
@@ -626,7 +691,7 @@ struct Narrow {
       const float inv = any ? 1.f / sum : 0.f;
       T* out = static_cast<T*>(a.out.p) + at[qb].b * a.out.seq + at[qb].i * a.out.row +
                (kvh * j.group + at[qb].g) * a.out.head;
-      float* rec = record_of(j, w.part, at[qb], kvh, HD);
+      float* rec = record_of(j, w.rec0, at[qb], kvh, HD);
       for (int db = wave; db < NDB; db += kWaves) {
         f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -934,7 +999,8 @@ struct Wide {
     rows.load_q(static_cast<const bf16_t*>(a.q.p) + at.b * a.q.seq + at.i * a.q.row +
                 (w.head * j.group + at.g) * a.q.head);
     rows.begin();
-    const Entry entry = entry_of(a, at.b);
+    const Entry entry = TREE ? w.e : entry_of(a, at.b);
+    const bool idle = w.row0 + 32 * wave >= w.row_end;   // none of the wave's rows is there: it only copies
     const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
     const int root = TREE ? __builtin_amdgcn_readfirstlane(entry.held - entry.rows) : 0;   // the tree's first position
 
@@ -962,6 +1028,7 @@ struct Wide {
         L::tame_values(sv, tid, kThreads);
         __syncthreads();
       }
+      if (idle) continue;
       // every K fragment is on its way before the first product waits for one,
       // half of the V fragments before the softmax
       u32x4 kf[2][L::QS], vf[2][L::NDB], pf[4];
@@ -1005,7 +1072,7 @@ struct Wide {
         for (int i = 0; i < 16; ++i)
           store_f(out + 32 * db + 8 * (i >> 2) + 4 * f + (i & 3), any ? rows.o[db][i] * inv : 0.f);
     } else {
-      float* rec = record_of(j, w.part, at, w.head, HD);
+      float* rec = record_of(j, w.rec0, at, w.head, HD);
 #pragma unroll
       for (int db = 0; db < L::NDB; ++db)
 #pragma unroll
@@ -1257,9 +1324,19 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   const bool live = in && i < e.rows;
   const int s = j.stacked ? stacked_of<TREE>(e, shared_of(a), j.prefix.range) : 0, lim = limit_of(a, e, i);
   const int np = live && j.prefix.ranges ? (min(lim, s) + j.prefix.range - 1) / j.prefix.range : 0;
-  const int nt = live && lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
+  int nt = live && lim > s ? min((lim - s + j.tail.range - 1) / j.tail.range, j.tail.ranges) : 0;
   const size_t stride = size_t(a.n) * a.max_rows * a.heads * record(HD);
   const float* rec = a.part + size_t(row) * record(HD);
+  // the tail's records: one after another like the prefix's, or slots of an entry's rows
+  const float* tails = rec + j.prefix.ranges * stride;
+  size_t tail_stride = stride;
+  if (TREE && j.by_length) {
+    const Slots z = slots_of<TREE>(j, shared_of(a));
+    const int count = __shfl(z.count, b, kWave), first = __shfl(z.first, b, kWave);
+    nt = live ? count : 0;
+    tail_stride = size_t(a.max_rows) * a.heads * record(HD);
+    tails += (int64_t(first) - b) * int64_t(tail_stride);
+  }
   float m = -INFINITY, l = 0.f;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   auto add = [&](float mr, float lr, f32x4 v) {
@@ -1276,7 +1353,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int r = min(r0 + u * slices, np + nt - 1);
-      const float* x = rec + (r < np ? r : j.prefix.ranges + r - np) * stride;
+      const float* x = r < np ? rec + r * stride : tails + (r - np) * tail_stride;
       mr[u] = x[HD];
       lr[u] = x[HD + 1];
       v[u] = *reinterpret_cast<const f32x4*>(x + c);
@@ -1533,6 +1610,8 @@ hipError_t attend(const PagedAttn& a, hipStream_t s) {
   j.stacked = d.stacked;
   if (d.shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
+  j.by_length = TREE && j.tail.ranges > 1 && a.n <= kWave;
+  j.least = 4;
   if (a.p.dtype == DLLM_BF16)
     hd == 128 ? launch<bf16_t, 128, TREE>(j, d.mode_p, d.mode_t, s) : launch<bf16_t, 64, TREE>(j, d.mode_p, d.mode_t, s);
   else

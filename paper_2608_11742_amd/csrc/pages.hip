@@ -487,59 +487,64 @@ __global__ __launch_bounds__(kCopyThreads) void compact_apply_kernel(dllm_kv_pag
   }
 }
 
-// Rows of accepted paths to their places.  Every thread moves one strand of an
-// entry, layer and head: 16 bytes of the keys' rows, or one dim of the values,
-// along the whole path.  A row's place is never behind where it comes from and
-// rows ascend, so a strand that reads some rows, in order, and then writes them
-// overwrites none that it still has to read; strands do not meet.
+// Rows of accepted paths to their places: a wave for an entry, layer and head, 8
+// rows of the path at a time.  Of the values 8 lanes take the rows of one dim
+// side by side, so that a load or store meets as few of the dims' lines as it
+// can; of the keys 16 bytes a lane.  A row's place is never behind where it comes
+// from and rows ascend: the rows of a step are read, in one instruction those of
+// a dim, before any is written, and no later step reads a place that is filled.
 constexpr int kMoveThreads = 256;
 constexpr int kMoveRows = 8;
 template <typename T, int HD>
 __global__ __launch_bounds__(kMoveThreads) void accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs, int n,
-                                                              int max_rows, const int32_t* __restrict__ n_rows,
                                                               const int32_t* __restrict__ path, int max_path,
                                                               const int32_t* __restrict__ n_path,
-                                                              const int32_t* __restrict__ from, int key_wgs,
+                                                              const int32_t* __restrict__ from,
                                                               const int32_t* __restrict__ status) {
-  constexpr int E = 16 / int(sizeof(T)), CK = HD / E;
-  if (*status != KV_PAGES_OK) return;
-  const bool keys = int(blockIdx.x) < key_wgs;
-  const int64_t t = int64_t(keys ? blockIdx.x : blockIdx.x - key_wgs) * kMoveThreads + threadIdx.x;
-  const int strand = int(t % (keys ? CK : HD)), heads = p.n_kv_heads;
-  const int64_t item = t / (keys ? CK : HD);
-  const int h = int(item % heads), layer = int(item / heads % p.n_layers);
-  if (item / heads / p.n_layers >= n) return;
-  const int b = int(item / heads / p.n_layers);
-  const int s = seqs[b], m = n_path[b], first = p.len[s] - m;   // the length is the new one
+  constexpr int E = 16 / int(sizeof(T)), CK = HD / E;     // elements of a chunk, chunks of a key
+  constexpr int KR = kWave / CK, NK = kMoveRows / KR;     // key rows of a load, loads of a step
+  constexpr int DV = kWave / kMoveRows, NV = HD / DV;     // dims of a load, loads of a step
+  const int lane = threadIdx.x & 63, heads = p.n_kv_heads;
+  const int item = blockIdx.x * (kMoveThreads / kWave) + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int h = item % heads, layer = item / heads % p.n_layers, b = item / heads / p.n_layers;
+  if (b >= n || *status != KV_PAGES_OK) return;
+  const int m = n_path[b], s = seqs[b], first = p.len[s] - m;   // the length is the new one
   const int32_t* pages = p.table + size_t(s) * p.max_blocks;
-  const int mask = p.page_len - 1;
-  // element 0 of the strand's head in a page
+  // element 0 of the head in a page
   auto head_of = [&](int page) { return ((size_t(layer) * p.n_pages + page) * heads + h) * p.page_len * HD; };
-  auto at = [&](int page, int pos) {
-    const int slot = pos & mask;
-    return head_of(page) + (keys ? size_t(slot) * HD + strand * E : size_t(strand) * p.page_len + slot);
-  };
   for (int j0 = 0; j0 < m; j0 += kMoveRows) {
-    u32x4 x[kMoveRows];
-    T y[kMoveRows];
-    bool move[kMoveRows];
-    size_t to[kMoveRows];
+    // row j0 + lane % 8 of the path: where it is, where it goes
+    const int j = min(j0 + lane % kMoveRows, m - 1), at = b * max_path + j;
+    const int r = path[at], a = from[at], c = pages[(first + j) / p.page_len];
+    const bool move = j0 + lane % kMoveRows < m && r != j && a >= 0 && a < p.n_pages && c >= 0 && c < p.n_pages;
+    if (!__any(move)) continue;
+    const int src = (first + r) & (p.page_len - 1), dst = (first + j) & (p.page_len - 1);
+    T* values = static_cast<T*>(p.vt);
+    const size_t v0 = head_of(max(a, 0)) + src, v1 = head_of(max(c, 0)) + dst, dim = size_t(lane / kMoveRows) * p.page_len;
+    T y[NV];
+    if (move) {
 #pragma unroll
-    for (int u = 0; u < kMoveRows; ++u) {
-      const int j = min(j0 + u, m - 1), r = path[size_t(b) * max_path + j];
-      const int a = from[size_t(b) * max_path + j], c = pages[(first + j) / p.page_len];
-      move[u] = j0 + u < m && r != j && a >= 0 && a < p.n_pages && c >= 0 && c < p.n_pages;
-      if (!move[u]) continue;
-      to[u] = at(c, first + j);
-      if (keys) x[u] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.k) + at(a, first + r));
-      else y[u] = static_cast<const T*>(p.vt)[at(a, first + r)];
+      for (int i = 0; i < NV; ++i) y[i] = values[v0 + dim + size_t(i) * DV * p.page_len];
+    }
+    u32x4 x[NK];
+    T* keys = static_cast<T*>(p.k);
+    size_t to[NK];
+    bool key_moves[NK];
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int u = i * KR + lane / CK, e = lane % CK * E;   // row of the step
+      key_moves[i] = __shfl(int(move), u, kWave);
+      const size_t k0 = head_of(max(__shfl(a, u, kWave), 0)) + size_t(__shfl(src, u, kWave)) * HD + e;
+      to[i] = head_of(max(__shfl(c, u, kWave), 0)) + size_t(__shfl(dst, u, kWave)) * HD + e;
+      if (key_moves[i]) x[i] = *reinterpret_cast<const u32x4*>(keys + k0);
+    }
+    if (move) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) values[v1 + dim + size_t(i) * DV * p.page_len] = y[i];
     }
 #pragma unroll
-    for (int u = 0; u < kMoveRows; ++u) {
-      if (!move[u]) continue;
-      if (keys) *reinterpret_cast<u32x4*>(static_cast<T*>(p.k) + to[u]) = x[u];
-      else static_cast<T*>(p.vt)[to[u]] = y[u];
-    }
+    for (int i = 0; i < NK; ++i)
+      if (key_moves[i]) *reinterpret_cast<u32x4*>(keys + to[i]) = x[i];
   }
 }
 
@@ -723,17 +728,14 @@ hipError_t pages_accept(const dllm_kv_pages& p, const int32_t* seqs, int n, int 
   if (!here)
     hipLaunchKernelGGL(free_apply_kernel, dim3(std::min(cdiv(p.max_blocks, 256), 64), n), dim3(256), 0, s, p, seqs,
                        status);
-  auto launch = [&](auto kernel, int chunks) {
-    const int64_t items = int64_t(n) * p.n_layers * p.n_kv_heads;
-    const int64_t key_wgs = (items * chunks + kMoveThreads - 1) / kMoveThreads;
-    const int64_t wgs = key_wgs + (items * p.head_dim + kMoveThreads - 1) / kMoveThreads;
-    hipLaunchKernelGGL(kernel, dim3(uint32_t(wgs)), dim3(kMoveThreads), 0, s, p, seqs, n, max_rows, n_rows, path, max_path,
-                       n_path, from, int(key_wgs), status);
+  auto launch = [&](auto kernel) {
+    const int64_t waves = int64_t(n) * p.n_layers * p.n_kv_heads, per = kMoveThreads / kWave;
+    hipLaunchKernelGGL(kernel, dim3(uint32_t((waves + per - 1) / per)), dim3(kMoveThreads), 0, s, p, seqs, n, path, max_path,
+                       n_path, from, status);
     return hipGetLastError();
   };
-  if (p.dtype == DLLM_BF16)
-    return p.head_dim == 128 ? launch(accept_kernel<bf16_t, 128>, 16) : launch(accept_kernel<bf16_t, 64>, 8);
-  return p.head_dim == 128 ? launch(accept_kernel<float, 128>, 32) : launch(accept_kernel<float, 64>, 16);
+  if (p.dtype == DLLM_BF16) return p.head_dim == 128 ? launch(accept_kernel<bf16_t, 128>) : launch(accept_kernel<bf16_t, 64>);
+  return p.head_dim == 128 ? launch(accept_kernel<float, 128>) : launch(accept_kernel<float, 64>);
 }
 
 size_t pages_compact_workspace(int n_pages) { return (16 + 3 * size_t(n_pages)) * sizeof(int32_t); }
