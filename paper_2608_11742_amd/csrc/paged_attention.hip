@@ -1087,6 +1087,119 @@ struct Wide {
   }
 };
 
+// ---------------------------------------------------------------- halves
+
+// 33 to 64 rows of a tree over one range of keys: wave w takes block w % 2 of 32
+// rows and half w / 2 of every tile's keys, so that no wave is without rows; the
+// two states of a block are joined through LDS.
+template <int HD>
+struct Halves {
+  using L = Tile<HD>;
+  using Copier = typename L::Copier;
+  static constexpr int RING = 2 * L::BYTES;
+  static constexpr int OWN = L::NDB / 2;            // dim blocks that a wave writes, after it has the other's
+  static constexpr int STATE = OWN * 16 + 2;        // floats a lane hands over
+  static constexpr int JOIN = kWaves * STATE * kWave * 4;
+  static constexpr int SMEM = RING > JOIN ? RING : JOIN;
+
+  __device__ static void run(const Job& j, const Share& w, uint8_t* smem) {
+    const PagedAttn& a = j.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int fr = lane & 31, f = lane >> 5, block = wave & 1, half = wave >> 1;
+    const uint32_t lds0 = lds_address(smem);
+    const Copier copier(a, w.head, wave, w.k1);
+    int id[4];
+    copier.pages_at(w, w.k0, id);
+    if (w.k0 < w.k1) copier.issue(w.k0, id, lds0);
+    copier.pages_at(w, w.k0 + kTile, id);
+
+    const RowAt at = row_at(j, min(w.row0 + 32 * block + fr, w.row_end - 1));
+    Rows32<HD> rows;
+    rows.load_q(static_cast<const bf16_t*>(a.q.p) + at.b * a.q.seq + at.i * a.q.row +
+                (w.head * j.group + at.g) * a.q.head);
+    rows.begin();
+    const int root = w.e.held - w.e.rows;   // the tree's first position
+
+    int slot = 0;
+    bool any_wild = false;
+    for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
+      wait_vmcnt<0>();
+      barrier_lds();   // tile k0 has landed; the other slot has been read
+      const uint8_t* sk = smem + slot * L::BYTES;
+      uint8_t* sv = smem + slot * L::BYTES + L::KB;
+      if (k0 + kTile > w.k1) {
+        L::zero_values(sv, tid, kThreads, w.k1 - k0);
+        barrier_lds();
+      } else if (k0 + kTile < w.k1) {
+        copier.issue(k0 + kTile, id, lds0 + (slot ^ 1) * L::BYTES);
+        copier.pages_at(w, k0 + 2 * kTile, id);
+      }
+      const bool masked = k0 + kTile > root;
+      if (masked && __syncthreads_or(L::wild_values(sv, tid, kThreads))) {
+        any_wild = true;
+        L::tame_values(sv, tid, kThreads);
+        __syncthreads();
+      }
+      const int keys = k0 + 32 * half;
+      u32x4 kf[1][L::QS], vf[2][L::NDB], pf[2];
+      f32x16 sc[1];
+#pragma unroll
+      for (int st = 0; st < L::QS; ++st) kf[0][st] = L::key_chunk(sk, half, st, lane);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, 2 * half + st, db, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      rows.scores(kf, sc);
+      if (masked) Rows32<HD>::hide(sc, seen_of(a, at.b, at.i, root, w.k1, keys));
+      rows.softmax(sc, keys, masked ? INT_MAX : w.k1, j.scale_log2, pf);
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int db = 0; db < L::NDB; ++db) rows.add(db, vf[st][db], pf[st]);
+    }
+    if (any_wild)   // from the first tile that held keys of the tree
+      rows.bring_wild(a, copier, w, at.b, at.i, root, w.k1, w.k0 + max(root - w.k0, 0) / kTile * kTile + 32 * half, kTile);
+
+    // the other half's state of the dim blocks that this wave writes
+    float* xs = reinterpret_cast<float*>(smem) + lane;
+    const float lsum = pair_sum(rows.l);
+    __syncthreads();   // the ring has been read
+    float* mine = xs + wave * (STATE * kWave);
+#pragma unroll
+    for (int c = 0; c < OWN * 16; ++c)
+      mine[c * kWave] = half ? rows.o[c >> 4][c & 15] : rows.o[OWN + (c >> 4)][c & 15];
+    mine[(STATE - 2) * kWave] = rows.m;
+    mine[(STATE - 1) * kWave] = lsum;
+    __syncthreads();
+    const float* other = xs + (wave ^ 2) * (STATE * kWave);
+    const float m1 = other[(STATE - 2) * kWave], top = fmaxf(rows.m, m1), ref = top == -INFINITY ? 0.f : top;
+    const float w0 = __builtin_amdgcn_exp2f(rows.m - ref), w1 = __builtin_amdgcn_exp2f(m1 - ref);
+    const float l = lsum * w0 + other[(STATE - 1) * kWave] * w1, inv = 1.f / l;
+    if (w.row0 + 32 * block + fr >= w.row_end || at.i >= w.e.rows) return;
+    bf16_t* out = static_cast<bf16_t*>(a.out.p) + at.b * a.out.seq + at.i * a.out.row + (w.head * j.group + at.g) * a.out.head;
+    float* rec = record_of(j, w.rec0, at, w.head, HD);
+#pragma unroll
+    for (int c = 0; c < OWN * 16; c += 4) {
+      f32x4 y;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        y[u] = (half ? rows.o[OWN + (c >> 4)][(c & 15) + u] : rows.o[c >> 4][(c & 15) + u]) * w0 + other[(c + u) * kWave] * w1;
+      const int dim = 32 * (half * OWN + (c >> 4)) + 2 * (c & 15) + 4 * f;
+      if (j.direct) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) store_f(out + dim + u, l != 0.f ? y[u] * inv : 0.f);
+      } else {
+        *reinterpret_cast<f32x4*>(rec + dim) = y;
+      }
+    }
+    if (!j.direct && half == 0 && f == 0) {
+      rec[HD] = top;
+      rec[HD + 1] = l;
+    }
+  }
+};
+
 // ---------------------------------------------------------------- pairs
 
 // Two blocks of 32 rows, each of one entry, over the shared prefix and then
@@ -1282,14 +1395,15 @@ __global__ __launch_bounds__((Pairs<HD, TREE>::kPairThreads), 2) void pairs_kern
 
 // ---------------------------------------------------------------- launch
 
-// how a part's rows are taken: 16 or 32 of them narrow, or 128 wide
-enum { ROWS16 = 1, ROWS32 = 2, ROWS128 = 3 };
-constexpr int rows_of(int mode) { return mode == ROWS16 ? 16 : mode == ROWS32 ? 32 : 128; }
+// how a part's rows are taken: 16 or 32 of them narrow, 64 in halves (tails of trees), or 128 wide
+enum { ROWS16 = 1, ROWS32 = 2, ROWS128 = 3, ROWS64 = 4 };
+constexpr int rows_of(int mode) { return mode == ROWS16 ? 16 : mode == ROWS32 ? 32 : mode == ROWS64 ? 64 : 128; }
 
 template <typename T, int HD, int MODE, bool TREE> struct Taker;
 template <typename T, int HD, bool TREE> struct Taker<T, HD, ROWS16, TREE> : Narrow<T, HD, 1, TREE> {};
 template <typename T, int HD, bool TREE> struct Taker<T, HD, ROWS32, TREE> : Narrow<T, HD, 2, TREE> {};
 template <int HD, bool TREE> struct Taker<bf16_t, HD, ROWS128, TREE> : Wide<HD, TREE> {};
+template <int HD> struct Taker<bf16_t, HD, ROWS64, true> : Halves<HD> {};
 
 // both parts in one launch: prefix workgroups, then the tails' (trees are in those alone)
 template <typename T, int HD, int PREFIX, int TAIL, bool TREE>
@@ -1453,6 +1567,9 @@ void launch_parts(const Job& j, hipStream_t s) {
 template <typename T, int HD, bool TREE>
 void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
+    if constexpr (TREE) {
+      if (tail == ROWS64) return launch_parts<T, HD, ROWS128, ROWS64, TREE>(j, s);
+    }
     if (tail == ROWS128) return launch_parts<T, HD, ROWS128, ROWS128, TREE>(j, s);
     if (prefix == ROWS128)
       return tail == ROWS32 ? launch_parts<T, HD, ROWS128, ROWS32, TREE>(j, s) : launch_parts<T, HD, ROWS128, ROWS16, TREE>(j, s);
@@ -1610,12 +1727,14 @@ hipError_t attend(const PagedAttn& a, hipStream_t s) {
   j.stacked = d.stacked;
   if (d.shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
+  // (a prefix over tails in halves has their rows of several entries)
+  const int mode_t = TREE && d.mode_t == ROWS128 && a.max_rows * j.group <= rows_of(ROWS64) ? ROWS64 : d.mode_t;
   j.by_length = TREE && j.tail.ranges > 1 && a.n <= kWave;
   j.least = 4;
   if (a.p.dtype == DLLM_BF16)
-    hd == 128 ? launch<bf16_t, 128, TREE>(j, d.mode_p, d.mode_t, s) : launch<bf16_t, 64, TREE>(j, d.mode_p, d.mode_t, s);
+    hd == 128 ? launch<bf16_t, 128, TREE>(j, d.mode_p, mode_t, s) : launch<bf16_t, 64, TREE>(j, d.mode_p, mode_t, s);
   else
-    hd == 128 ? launch<float, 128, TREE>(j, d.mode_p, d.mode_t, s) : launch<float, 64, TREE>(j, d.mode_p, d.mode_t, s);
+    hd == 128 ? launch<float, 128, TREE>(j, d.mode_p, mode_t, s) : launch<float, 64, TREE>(j, d.mode_p, mode_t, s);
   return hipGetLastError();
 }
 
