@@ -156,7 +156,12 @@ struct Heads {
     b = pack(x + E);
   }
 
-  // heads h0, h0 + 1, .. of a row from `in` to `out` (null: not stored), `steps` steps
+  // Heads h0, h0 + 1, .. of a row from `in` to `out`, `steps` steps.  Rows that are
+  // rotated in memory are read past the caches (kOnce; 16 x 512 rows of 40 heads
+  // of 128: 35.6 us, 37.7 with plain loads).  An append's are not (51.8 against
+  // 48.9), and neither stores past them: 41 us by itself, but 4 more for the
+  // attention that reads the rows next than the 8 it saves.
+  template <bool kOnce>
   __device__ __forceinline__ void heads(const dllm_rotary& rot, const float* gain, const T* in, int64_t in_head, T* out,
                                         int64_t out_head, int h0, int n_heads, int steps) const {
     float g[2 * E];
@@ -176,9 +181,10 @@ struct Heads {
     for (int st = 0; st < steps; ++st) {
       const int h = h0 + st * HS + int(threadIdx.x & 63) / U, at = min(h, n_heads - 1);
       const T* src = in + at * in_head;
-      u32x4 a = *reinterpret_cast<const u32x4*>(src + e0), b = *reinterpret_cast<const u32x4*>(src + e1);
+      const u32x4 *pa = reinterpret_cast<const u32x4*>(src + e0), *pb = reinterpret_cast<const u32x4*>(src + e1);
+      u32x4 a = kOnce ? __builtin_nontemporal_load(pa) : *pa, b = kOnce ? __builtin_nontemporal_load(pb) : *pb;
       turn(a, b, rot, g);
-      if (h < n_heads && out) {
+      if (h < n_heads) {
         T* dst = out + h * out_head;
         *reinterpret_cast<u32x4*>(dst + e0) = a;
         *reinterpret_cast<u32x4*>(dst + e1) = b;
@@ -210,7 +216,7 @@ __device__ __forceinline__ void turn_row(const Rotation& r, const Append& w, int
   if (s0 < q_steps) {
     const T* in = static_cast<const T*>(r.q.p) + b * r.q.seq + i * r.q.row;
     T* out = static_cast<T*>(r.q_out.p) + b * r.q_out.seq + i * r.q_out.row;
-    lanes.heads(r.rot, r.rot.q_gain, in, r.q.head, out, r.q_out.head, s0 * H::HS, r.q_heads, min(s1, q_steps) - s0);
+    lanes.template heads<!kAppend>(r.rot, r.rot.q_gain, in, r.q.head, out, r.q_out.head, s0 * H::HS, r.q_heads, min(s1, q_steps) - s0);
   }
   if (s1 <= q_steps) return;
   const int k0 = max(s0 - q_steps, 0);
@@ -232,7 +238,7 @@ __device__ __forceinline__ void turn_row(const Rotation& r, const Append& w, int
     head = r.k_out.head;
     out = static_cast<T*>(r.k_out.p) + b * r.k_out.seq + i * r.k_out.row;
   }
-  lanes.heads(r.rot, r.rot.k_gain, in, r.k.head, out, head, k0 * H::HS, r.k_heads, s1 - q_steps - k0);
+  lanes.template heads<!kAppend>(r.rot, r.rot.k_gain, in, r.k.head, out, head, k0 * H::HS, r.k_heads, s1 - q_steps - k0);
 }
 
 template <typename T, int HD>
@@ -323,11 +329,14 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Rotation r, Append w) 
     typename Values<T, HD>::Shared values;
   } sh;
   const int x = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  if (x < w.turn_wgs) {
-    turn_row<T, HD, true>(r, w, x * kWaves + wave, sh.cs[wave]);
+  // the two kinds in even turns: with either first, the other's waits at the end
+  // are not covered (16 x 512 rows of 32 + 8 + 8 heads: 49.5 us, 51 with queries and keys first)
+  const int heads = w.p.n_kv_heads, values = w.tiles * heads * r.n, all = values + w.turn_wgs;
+  const int y = int(int64_t(x) * values / all);
+  if (y == int(int64_t(x + 1) * values / all)) {
+    turn_row<T, HD, true>(r, w, (x - y) * kWaves + wave, sh.cs[wave]);
     return;
   }
-  const int y = x - w.turn_wgs, heads = w.p.n_kv_heads;
   const int b = y / (heads * w.tiles), z = y % (heads * w.tiles);
   const int h = w.heads_first ? z % heads : z / w.tiles, tile = w.heads_first ? z / heads : z % w.tiles;
   Values<T, HD>::run(r, w, b, h, tile, sh.values);
