@@ -12,7 +12,7 @@ import ctypes as C
 
 import torch
 
-from . import _abi
+from . import _abi, _marshal
 from ._abi import (DllmError, ModelDesc, Weights, StatsC, KvCache, Probe, RpsParams, RpsPlan, RpsDecision,
                    DLLM_F32, DLLM_BF16, RPS_PIVOT_PAPER, RPS_PIVOT_BAND, DLLM_MAX_TOPK, RPS_MAX_BRANCH)
 
@@ -247,7 +247,7 @@ class KvPages:
         self._c = _abi.KvPagesC(k.data_ptr(), vt.data_ptr(), refs.data_ptr(), table.data_ptr(), len.data_ptr(), L,
                                 n_pages, heads, hd, page_len, table.shape[0], table.shape[1],
                                 DLLM_BF16 if k.dtype == torch.bfloat16 else DLLM_F32)
-        self._ref = C.byref(self._c)
+        self._ref, self._at = C.byref(self._c), C.addressof(self._c)
 
     @classmethod
     def empty(cls, n_layers: int, n_pages: int, n_kv_heads: int, page_len: int, head_dim: int, max_seqs: int,
@@ -429,58 +429,17 @@ class Rotary:
         self.head_dim, self.dim, self.amplitude = head_dim, dim, own if amplitude is None else amplitude
         self._c = _abi.RotaryC(self.freq.data_ptr(), _p(q_gain), _p(k_gain), head_dim, dim, _LAYOUTS[layout], int(norm),
                                self.amplitude, eps)
-        self._ref = C.byref(self._c)
+        self._at = C.addressof(self._c)
 
 
-def _positions(owner, t, n: int, rows: int):
-    """Address of an int32 list [entries, rows] beside the owner's arrays."""
-    if t is None:
-        return None
-    if t.dtype is not _I32 or t.get_device() != owner._index or t.shape != (n, rows) or not t.is_contiguous():
-        raise ValueError("positions and parents are contiguous int32 tensors [entries, rows], beside the other arrays")
-    return t.data_ptr()
-
-
-def _turned(owner, x, out, dtype, n: int, rows: int, name: str):
-    """x and out [n, rows, heads, head_dim] as heads and two dllm_rows; none without x."""
-    if x is None:
-        return 0, None, None
-    b, i, heads, hd = shape = x.shape
-    if b != n or i != rows or hd != owner.head_dim or out is None or out.shape != shape:
-        raise ValueError(f"{name} and its output are [entries, rows, heads, head_dim], of the same entries, rows and head_dim")
-    index = owner._index
-    seq, row, head, one = x.stride()
-    seq_o, row_o, head_o, one_o = out.stride()
-    if (one != 1 or one_o != 1 or x.dtype is not dtype or out.dtype is not dtype or x.get_device() != index
-            or out.get_device() != index):
-        raise ValueError(f"{name} must have contiguous rows, one type, and the device of the other arrays")
-    # a dimension of one has no stride to speak of
-    if n == 1:
-        seq = seq_o = 0
-    if rows == 1:
-        row = row_o = 0
-    if heads == 1:
-        head = head_o = 0
-    return heads, _Rows(x.data_ptr(), seq, row, head), _Rows(out.data_ptr(), seq_o, row_o, head_o)
-
-
-_DTYPES = {torch.bfloat16: DLLM_BF16, torch.float32: DLLM_F32}
-
+# These are called once a layer and token: _marshal reads the tensors natively
+# (types, devices, shapes and strides checked, ValueError where they do not fit).
 
 def rotary_rows(rot: Rotary, q, q_out, k=None, k_out=None, pos=None, pos_offset: int = 0, n_rows=None, stream=None):
     """q [entries, rows, heads, head_dim] (and k, with heads of its own) normed and rotated into q_out (and k_out);
     pos [entries, rows], or row i is at pos_offset + i.  The outputs may be the inputs."""
-    x = k if q is None else q
-    n, rows, _, _ = x.shape
-    t = x.dtype
-    dtype = _DTYPES.get(t)
-    if dtype is None:
-        raise ValueError("rows are bf16 or fp32")
-    hq, qi, qo = _turned(rot, q, q_out, t, n, rows, "q")
-    hk, ki, ko = _turned(rot, k, k_out, t, n, rows, "k")
-    status = lib().rotary_rows(rot._ref, dtype, None if pos is None else _positions(rot, pos, n, rows), pos_offset, n, rows,
-                               None if n_rows is None else _ids(rot, n_rows, n), hq, qi, qo, hk, ki, ko,
-                               _page_stream(rot, stream))
+    status = _marshal.rotary_rows(rot._at, rot._index, q, q_out, k, k_out, pos, pos_offset, n_rows,
+                                  None if stream is None else _page_stream(rot, stream))
     if status:
         _check(status)
 
@@ -489,46 +448,29 @@ def kv_pages_append(pages: KvPages, layer: int, seqs, k, v, rot: Rotary, q=None,
                     stream=None):
     """kv_pages_write with k normed and rotated on the way; q [entries, rows, heads, head_dim] likewise into q_out.
     pos [entries, rows]: positions of the rotation, by default those of the rows."""
-    n, rows, heads, hd = shape = k.shape
-    if v.shape != shape or heads != pages.n_kv_heads or hd != pages.head_dim:
-        raise ValueError("k and v need the pages' heads and head_dim and the same shape")
-    if rot._index != pages._index:
-        raise ValueError("the rotation is on another device than the pages")
-    hq, qi, qo = _turned(pages, q, q_out, pages.dtype, n, rows, "q")
-    _check(lib().kv_pages_append(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n), rot._ref,
-                                 _positions(pages, pos, n, rows), hq, qi, qo, _rows(pages, k, n, rows, heads, "k"),
-                                 _rows(pages, v, n, rows, heads, "v"), _page_stream(pages, stream)))
-
-
-def _mask(pages: KvPages, mask, n: int, rows: int):
-    if (mask.dtype is not _I32 or mask.get_device() != pages._index or mask.shape != (n, rows, (rows + 31) // 32)
-            or not mask.is_contiguous()):
-        raise ValueError("a mask is a contiguous int32 tensor [entries, rows, words of 32 rows] beside the pages")
-    return mask.data_ptr()
+    status = _marshal.kv_pages_append(pages._at, pages._index, layer, seqs, n_rows, rot._at, rot._index, pos, q, q_out,
+                                      k, v, None if stream is None else _page_stream(pages, stream))
+    if status:
+        _check(status)
 
 
 def kv_pages_tree(pages: KvPages, seqs, parent, mask, pos=None, n_rows=None, stream=None):
     """parent [entries, rows]: the row that each drafted row follows, or -1.  Written: mask [entries, rows,
     (rows + 31) // 32], the rows that each sees, as bits; pos [entries, rows], the rows' positions."""
-    n, rows = parent.shape
-    _check(lib().kv_pages_tree(pages._ref, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n),
-                               _positions(pages, parent, n, rows), _mask(pages, mask, n, rows),
-                               _positions(pages, pos, n, rows), _page_stream(pages, stream)))
+    status = _marshal.kv_pages_tree(pages._at, pages._index, seqs, n_rows, parent, mask, pos,
+                                    None if stream is None else _page_stream(pages, stream))
+    if status:
+        _check(status)
 
 
 def kv_pages_attention_tree(pages: KvPages, layer: int, seqs, q, out, mask, ws, n_rows=None, prefix_seq: int = 0,
                             shared_len: int = 0, max_len: int | None = None, scale: float | None = None, stream=None):
     """kv_pages_attention of the last rows of each sequence, which see what is before them and the rows in their mask."""
-    n, rows, heads, hd = shape = q.shape
-    if out.shape != shape or hd != pages.head_dim:
-        raise ValueError("q and out need the pages' head_dim and the same shape")
-    if max_len is None:
-        max_len = pages.table.shape[1] * pages.page_len
-    _check(lib().kv_pages_attention_tree(pages._ref, layer, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n), heads,
-                                         _rows(pages, q, n, rows, heads, "q"), _rows(pages, out, n, rows, heads, "out"),
-                                         _mask(pages, mask, n, rows), prefix_seq, shared_len, max_len,
-                                         pages._scale if scale is None else scale, *_scratch(pages, ws),
-                                         _page_stream(pages, stream)))
+    status = _marshal.kv_pages_attention_tree(pages._at, pages._index, layer, seqs, n_rows, q, out, mask, prefix_seq,
+                                              shared_len, max_len, scale, ws,
+                                              None if stream is None else _page_stream(pages, stream))
+    if status:
+        _check(status)
 
 
 def kv_pages_accept_workspace_bytes(pages: KvPages, n: int, max_path: int) -> int:
@@ -538,10 +480,10 @@ def kv_pages_accept_workspace_bytes(pages: KvPages, n: int, max_path: int) -> in
 def kv_pages_accept(pages: KvPages, seqs, path, n_path, status, ws, rows: int, n_rows=None, stream=None):
     """Of the last n_rows[i] (or `rows`) positions of seqs[i] those of the rows path[i][:n_path[i]], which ascend, are
     kept, in every layer, and the others given back."""
-    n, max_path = path.shape
-    _check(lib().kv_pages_accept(pages._ref, _ids(pages, seqs, n), n, rows, _ids(pages, n_rows, n),
-                                 _positions(pages, path, n, max_path), max_path, _ids(pages, n_path, n),
-                                 _ids(pages, status, 1), *_scratch(pages, ws), _page_stream(pages, stream)))
+    code = _marshal.kv_pages_accept(pages._at, pages._index, seqs, rows, n_rows, path, n_path, status, ws,
+                                    None if stream is None else _page_stream(pages, stream))
+    if code:
+        _check(code)
 
 
 def dllm_workspace_bytes_pages(handle, batch: int, seq: int, n_lm_pos: int) -> int:

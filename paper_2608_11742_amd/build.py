@@ -1,10 +1,12 @@
-"""Build libdllm_rps.so for gfx950 with hipcc (in-tree, next to this file)."""
+"""Build libdllm_rps.so for gfx950 with hipcc, and the module _marshal, which
+reads torch tensors for it, with g++ (in-tree, next to this file)."""
 from __future__ import annotations
 
 import os
 import re
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -13,6 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ = os.path.join(ROOT, "_build", "obj")
 LIB = os.path.join(HERE, "libdllm_rps.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -68,16 +71,41 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_marshal() -> list[str]:
+    """Object of marshal.cpp, and what it is linked with beside the library."""
+    import torch
+    from torch.utils import cpp_extension
+
+    rocm = os.path.dirname(os.path.dirname(HIPCC))
+    dirs = [INCLUDE, *cpp_extension.include_paths(), os.path.join(rocm, "include"), sysconfig.get_paths()["include"]]
+    obj = os.path.join(OBJ, "marshal.o")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *[f"-isystem{d}" for d in dirs], "-c", os.path.join(CSRC, "marshal.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed on marshal.cpp:\n{r.stderr}")
+    return [obj, f"-L{cpp_extension.library_paths()[0]}", "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10"]
+
+
 def build(jobs: int = 8) -> str:
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=jobs) as ex:
+        marshal = ex.submit(_compile_marshal)
         objs = list(ex.map(_compile, sources()))
+        marshal = marshal.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, LIB)
+    # torch's libraries are loaded before the module is; the library is beside it
+    cmd = ["g++", "-shared", "-o", MARSHAL + ".tmp", *marshal, f"-L{HERE}", "-l:libdllm_rps.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link of _marshal failed:\n{r.stderr}")
+    os.replace(MARSHAL + ".tmp", MARSHAL)
     return LIB
 
 
