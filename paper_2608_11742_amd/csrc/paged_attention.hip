@@ -302,11 +302,15 @@ __device__ __forceinline__ float quad_sum(float x) {
 // rows), of the tree those in its mask, none from `end` on
 __device__ __forceinline__ uint64_t seen_of(const PagedAttn& a, int b, int i, int root, int end, int k0) {
   const uint32_t* row = a.mask + (size_t(b) * a.max_rows + i) * a.words;
-  auto word = [&](int j) { return j < a.words ? row[j] : 0u; };
+  // (words past the mask's are read from inside it, so that no load waits behind a branch)
+  auto word = [&](int j) {
+    const uint32_t w = row[min(j, a.words - 1)];
+    return j < a.words ? w : 0u;
+  };
   const int t = k0 - root, j = max(t, 0) >> 5, shift = t & 31;
-  const uint64_t w = uint64_t(word(j + 1)) << 32 | word(j);
+  const uint64_t w = uint64_t(word(j + 1)) << 32 | word(j), next = word(j + 2);
   uint64_t bits;
-  if (t >= 0) bits = w >> shift | (shift ? uint64_t(word(j + 2)) << (64 - shift) : 0);
+  if (t >= 0) bits = w >> shift | (shift ? next << (64 - shift) : 0);
   else bits = t <= -64 ? ~uint64_t(0) : w << -t | ~(~uint64_t(0) << -t);
   const int left = end - k0;
   return left >= 64 ? bits : left <= 0 ? 0 : bits & ~(~uint64_t(0) << left);
@@ -591,15 +595,17 @@ struct Narrow {
         load_k(k0, id);
         constexpr bool kLate = !kHalf && NQB == 2;   // K and V together would spill
         if (!kLate) load_v(k0, id);
+        uint64_t seen[NQB];
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) seen[qb] = seen_of(a, at[qb].b, at[qb].i, root, end, k0);
         Scores sc;
         score(sc);
         if (kLate) load_v(k0, id);
 #pragma unroll
         for (int qb = 0; qb < NQB; ++qb) {
-          const uint64_t seen = seen_of(a, at[qb].b, at[qb].i, root, end, k0);
 #pragma unroll
           for (int kb = 0; kb < NB; ++kb) {
-            const uint32_t bits = uint32_t(seen >> key_of(kb, 4 * g));
+            const uint32_t bits = uint32_t(seen[qb] >> key_of(kb, 4 * g));
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (!(bits >> i & 1)) sc[kb][qb][i] = -INFINITY;
@@ -1029,6 +1035,7 @@ struct Wide {
         __syncthreads();
       }
       if (idle) continue;
+      const uint64_t seen = masked ? seen_of(a, at.b, at.i, root, lim, k0) : 0;
       // every K fragment is on its way before the first product waits for one,
       // half of the V fragments before the softmax
       u32x4 kf[2][L::QS], vf[2][L::NDB], pf[4];
@@ -1044,7 +1051,7 @@ struct Wide {
 #pragma unroll
         for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, st, db, lane);
       __builtin_amdgcn_sched_barrier(0);
-      if (masked) Rows32<HD>::hide(sc, seen_of(a, at.b, at.i, root, lim, k0));
+      if (masked) Rows32<HD>::hide(sc, seen);
       rows.softmax(sc, k0, masked ? INT_MAX : lim, j.scale_log2, pf);
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
@@ -1141,6 +1148,7 @@ struct Halves {
         __syncthreads();
       }
       const int keys = k0 + 32 * half;
+      const uint64_t seen = masked ? seen_of(a, at.b, at.i, root, w.k1, keys) : 0;
       u32x4 kf[1][L::QS], vf[2][L::NDB], pf[2];
       f32x16 sc[1];
 #pragma unroll
@@ -1151,7 +1159,7 @@ struct Halves {
         for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, 2 * half + st, db, lane);
       __builtin_amdgcn_sched_barrier(0);
       rows.scores(kf, sc);
-      if (masked) Rows32<HD>::hide(sc, seen_of(a, at.b, at.i, root, w.k1, keys));
+      if (masked) Rows32<HD>::hide(sc, seen);
       rows.softmax(sc, keys, masked ? INT_MAX : w.k1, j.scale_log2, pf);
 #pragma unroll
       for (int st = 0; st < 2; ++st)
@@ -1314,10 +1322,11 @@ struct Pairs {
           }
         }
       }
-      rows.scores(kf, sc);
       const bool masked = TREE && k0 + 32 > root;
+      const uint64_t seen = masked ? seen_of(a, b, i, root, limit, k0) : 0;
+      rows.scores(kf, sc);
       if (masked) {
-        Rows32<HD>::hide(sc, seen_of(a, b, i, root, limit, k0));
+        Rows32<HD>::hide(sc, seen);
         uint32_t wild = 0;
 #pragma unroll
         for (int st = 0; st < 2; ++st)

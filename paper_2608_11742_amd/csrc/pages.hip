@@ -352,15 +352,74 @@ __global__ __launch_bounds__(256) void free_apply_kernel(dllm_kv_pages p, const 
   for (int j = first + blockIdx.x * 256 + threadIdx.x; j < p.max_blocks; j += gridDim.x * 256) drop_entry(p, s, j);
 }
 
+// Rows of accepted paths to their places: a wave for an entry, layer and head, 8
+// rows of the path at a time.  Of the values 8 lanes take the rows of one dim
+// side by side, so that a load or store meets as few of the dims' lines as it
+// can; of the keys 16 bytes a lane.  A row's place is never behind where it comes
+// from and rows ascend: the rows of a step are read, in one instruction those of
+// a dim, before any is written, and no later step reads a place that is filled.
+// Bound by the values' lines: each moved row is 2 bytes in one of every dim of
+// every head and layer, which is read whole.  64 paths of up to 6 rows, 4 layers of
+// 32 heads of 128: 34 MB of rows, 214 MB read and 47 written, 55 us (4.8 TB/s).
+constexpr int kMoveThreads = 256;
+constexpr int kMoveRows = 8;
+template <typename T, int HD>
+__device__ __forceinline__ void move_rows(const dllm_kv_pages& p, int layer, int h, int s, int first, int m,
+                                          const int32_t* path, const int32_t* from) {
+  constexpr int E = 16 / int(sizeof(T)), CK = HD / E;     // elements of a chunk, chunks of a key
+  constexpr int KR = kWave / CK, NK = kMoveRows / KR;     // key rows of a load, loads of a step
+  constexpr int DV = kWave / kMoveRows, NV = HD / DV;     // dims of a load, loads of a step
+  const int lane = threadIdx.x & 63;
+  const int32_t* pages = p.table + size_t(s) * p.max_blocks;
+  // element 0 of the head in a page
+  auto head_of = [&](int page) { return ((size_t(layer) * p.n_pages + page) * p.n_kv_heads + h) * p.page_len * HD; };
+  for (int j0 = 0; j0 < m; j0 += kMoveRows) {
+    // row j0 + lane % 8 of the path: where it is, where it goes
+    const int j = min(j0 + lane % kMoveRows, m - 1);
+    const int r = path[j], a = from[j], c = pages[(first + j) / p.page_len];
+    const bool move = j0 + lane % kMoveRows < m && r != j && a >= 0 && a < p.n_pages && c >= 0 && c < p.n_pages;
+    if (!__any(move)) continue;
+    const int src = (first + r) & (p.page_len - 1), dst = (first + j) & (p.page_len - 1);
+    T* values = static_cast<T*>(p.vt);
+    const size_t v0 = head_of(max(a, 0)) + src, v1 = head_of(max(c, 0)) + dst, dim = size_t(lane / kMoveRows) * p.page_len;
+    T y[NV];
+    if (move) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) y[i] = values[v0 + dim + size_t(i) * DV * p.page_len];
+    }
+    u32x4 x[NK];
+    T* keys = static_cast<T*>(p.k);
+    size_t to[NK];
+    bool key_moves[NK];
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int u = i * KR + lane / CK, e = lane % CK * E;   // row of the step
+      key_moves[i] = __shfl(int(move), u, kWave);
+      const size_t k0 = head_of(max(__shfl(a, u, kWave), 0)) + size_t(__shfl(src, u, kWave)) * HD + e;
+      to[i] = head_of(max(__shfl(c, u, kWave), 0)) + size_t(__shfl(dst, u, kWave)) * HD + e;
+      if (key_moves[i]) x[i] = *reinterpret_cast<const u32x4*>(keys + k0);
+    }
+    if (move) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) values[v1 + dim + size_t(i) * DV * p.page_len] = y[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+      if (key_moves[i]) *reinterpret_cast<u32x4*>(keys + to[i]) = x[i];
+  }
+}
+
 // Acceptance plan: checks, the pages of the rows that are kept (`from`, [n][max_path])
-// before the tables are cut; accept_kernel moves the rows.  Paths and their pages
-// are gone through by all threads together.
+// before the tables are cut; accept_kernel moves the rows, or with `move_here`
+// the plan's waves before that.  Paths and their pages are gone through by all
+// threads together.
+template <typename T, int HD>
 __global__ __launch_bounds__(kPlanThreads) void pages_accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs,
                                                                     int n, int max_rows,
                                                                     const int32_t* __restrict__ n_rows,
                                                                     const int32_t* __restrict__ path, int max_path,
                                                                     const int32_t* __restrict__ n_path, int32_t* from,
-                                                                    int32_t* status, bool drop_here) {
+                                                                    int32_t* status, bool drop_here, bool move_here) {
   __shared__ PlanShared sh;
   __shared__ int rows_of[KV_MAX_SEQS];
   const int tid = threadIdx.x;
@@ -403,6 +462,15 @@ __global__ __launch_bounds__(kPlanThreads) void pages_accept_kernel(dllm_kv_page
     err = plan_error(err, sh);
   }
   if (err == kNoError) {
+    if (move_here) {
+      const int heads = p.n_kv_heads;
+      for (int t = __builtin_amdgcn_readfirstlane(tid >> 6); t < n * p.n_layers * heads; t += kPlanWaves) {
+        const int i = t / heads / p.n_layers;
+        move_rows<T, HD>(p, t / heads % p.n_layers, t % heads, sh.seq[i], sh.first[i], sh.off[i],
+                         path + size_t(i) * max_path, from + size_t(i) * max_path);
+      }
+      __syncthreads();   // the tables have been read
+    }
     if (tid < n) p.len[s] = first + m;
     if (drop_here)
       for (int t = tid; t < n * p.max_blocks; t += kPlanThreads) {
@@ -411,6 +479,21 @@ __global__ __launch_bounds__(kPlanThreads) void pages_accept_kernel(dllm_kv_page
       }
   }
   if (tid == 0) *status = err == kNoError ? KV_PAGES_OK : err;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(kMoveThreads) void accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs, int n,
+                                                              const int32_t* __restrict__ path, int max_path,
+                                                              const int32_t* __restrict__ n_path,
+                                                              const int32_t* __restrict__ from,
+                                                              const int32_t* __restrict__ status) {
+  const int heads = p.n_kv_heads;
+  const int item = blockIdx.x * (kMoveThreads / kWave) + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int b = item / heads / p.n_layers;
+  if (b >= n || *status != KV_PAGES_OK) return;
+  const int m = n_path[b], s = seqs[b];
+  move_rows<T, HD>(p, item / heads % p.n_layers, item % heads, s, p.len[s] - m, m, path + size_t(b) * max_path,
+                   from + size_t(b) * max_path);   // (the length is the new one)
 }
 
 // Compaction plan in the workspace: [0] pages moved, then their new ids by
@@ -484,67 +567,6 @@ __global__ __launch_bounds__(kCopyThreads) void compact_apply_kernel(dllm_kv_pag
   for (int64_t t = blockIdx.x; t < int64_t(moved) * units; t += gridDim.x) {
     const int r = int(t / units);
     copy_unit(p, page_bytes, parts, int(t % units), c.from[r], c.to[r]);
-  }
-}
-
-// Rows of accepted paths to their places: a wave for an entry, layer and head, 8
-// rows of the path at a time.  Of the values 8 lanes take the rows of one dim
-// side by side, so that a load or store meets as few of the dims' lines as it
-// can; of the keys 16 bytes a lane.  A row's place is never behind where it comes
-// from and rows ascend: the rows of a step are read, in one instruction those of
-// a dim, before any is written, and no later step reads a place that is filled.
-constexpr int kMoveThreads = 256;
-constexpr int kMoveRows = 8;
-template <typename T, int HD>
-__global__ __launch_bounds__(kMoveThreads) void accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs, int n,
-                                                              const int32_t* __restrict__ path, int max_path,
-                                                              const int32_t* __restrict__ n_path,
-                                                              const int32_t* __restrict__ from,
-                                                              const int32_t* __restrict__ status) {
-  constexpr int E = 16 / int(sizeof(T)), CK = HD / E;     // elements of a chunk, chunks of a key
-  constexpr int KR = kWave / CK, NK = kMoveRows / KR;     // key rows of a load, loads of a step
-  constexpr int DV = kWave / kMoveRows, NV = HD / DV;     // dims of a load, loads of a step
-  const int lane = threadIdx.x & 63, heads = p.n_kv_heads;
-  const int item = blockIdx.x * (kMoveThreads / kWave) + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  const int h = item % heads, layer = item / heads % p.n_layers, b = item / heads / p.n_layers;
-  if (b >= n || *status != KV_PAGES_OK) return;
-  const int m = n_path[b], s = seqs[b], first = p.len[s] - m;   // the length is the new one
-  const int32_t* pages = p.table + size_t(s) * p.max_blocks;
-  // element 0 of the head in a page
-  auto head_of = [&](int page) { return ((size_t(layer) * p.n_pages + page) * heads + h) * p.page_len * HD; };
-  for (int j0 = 0; j0 < m; j0 += kMoveRows) {
-    // row j0 + lane % 8 of the path: where it is, where it goes
-    const int j = min(j0 + lane % kMoveRows, m - 1), at = b * max_path + j;
-    const int r = path[at], a = from[at], c = pages[(first + j) / p.page_len];
-    const bool move = j0 + lane % kMoveRows < m && r != j && a >= 0 && a < p.n_pages && c >= 0 && c < p.n_pages;
-    if (!__any(move)) continue;
-    const int src = (first + r) & (p.page_len - 1), dst = (first + j) & (p.page_len - 1);
-    T* values = static_cast<T*>(p.vt);
-    const size_t v0 = head_of(max(a, 0)) + src, v1 = head_of(max(c, 0)) + dst, dim = size_t(lane / kMoveRows) * p.page_len;
-    T y[NV];
-    if (move) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) y[i] = values[v0 + dim + size_t(i) * DV * p.page_len];
-    }
-    u32x4 x[NK];
-    T* keys = static_cast<T*>(p.k);
-    size_t to[NK];
-    bool key_moves[NK];
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int u = i * KR + lane / CK, e = lane % CK * E;   // row of the step
-      key_moves[i] = __shfl(int(move), u, kWave);
-      const size_t k0 = head_of(max(__shfl(a, u, kWave), 0)) + size_t(__shfl(src, u, kWave)) * HD + e;
-      to[i] = head_of(max(__shfl(c, u, kWave), 0)) + size_t(__shfl(dst, u, kWave)) * HD + e;
-      if (key_moves[i]) x[i] = *reinterpret_cast<const u32x4*>(keys + k0);
-    }
-    if (move) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) values[v1 + dim + size_t(i) * DV * p.page_len] = y[i];
-    }
-#pragma unroll
-    for (int i = 0; i < NK; ++i)
-      if (key_moves[i]) *reinterpret_cast<u32x4*>(keys + to[i]) = x[i];
   }
 }
 
@@ -682,6 +704,7 @@ size_t page_bytes_of(const dllm_kv_pages& p) {
 
 constexpr int kCopyWgs = 2048;        // 8 workgroups of a copy on every CU
 constexpr int kDropHere = 32 * 1024;  // table entries one workgroup clears by itself
+constexpr int kMoveHere = 64;         // an acceptance's waves that its plan takes itself, 16 at a time
 
 }  // namespace
 
@@ -722,20 +745,25 @@ hipError_t pages_accept(const dllm_kv_pages& p, const int32_t* seqs, int n, int 
                         const int32_t* path, int max_path, const int32_t* n_path, int32_t* status, void* ws,
                         hipStream_t s) {
   int32_t* from = static_cast<int32_t*>(ws);
-  const bool here = int64_t(n) * p.max_blocks <= kDropHere;
-  hipLaunchKernelGGL(pages_accept_kernel, dim3(1), dim3(kPlanThreads), 0, s, p, seqs, n, max_rows, n_rows, path, max_path,
-                     n_path, from, status, here);
-  if (!here)
-    hipLaunchKernelGGL(free_apply_kernel, dim3(std::min(cdiv(p.max_blocks, 256), 64), n), dim3(256), 0, s, p, seqs,
-                       status);
-  auto launch = [&](auto kernel) {
-    const int64_t waves = int64_t(n) * p.n_layers * p.n_kv_heads, per = kMoveThreads / kWave;
-    hipLaunchKernelGGL(kernel, dim3(uint32_t((waves + per - 1) / per)), dim3(kMoveThreads), 0, s, p, seqs, n, path, max_path,
-                       n_path, from, status);
+  const bool drop_here = int64_t(n) * p.max_blocks <= kDropHere;
+  const int64_t waves = int64_t(n) * p.n_layers * p.n_kv_heads, per = kMoveThreads / kWave;
+  const bool move_here = waves <= kMoveHere;
+  auto launch = [&](auto plan, auto move) {
+    hipLaunchKernelGGL(plan, dim3(1), dim3(kPlanThreads), 0, s, p, seqs, n, max_rows, n_rows, path, max_path, n_path, from,
+                       status, drop_here, move_here);
+    if (!drop_here)
+      hipLaunchKernelGGL(free_apply_kernel, dim3(std::min(cdiv(p.max_blocks, 256), 64), n), dim3(256), 0, s, p, seqs,
+                         status);
+    if (!move_here)
+      hipLaunchKernelGGL(move, dim3(uint32_t((waves + per - 1) / per)), dim3(kMoveThreads), 0, s, p, seqs, n, path,
+                         max_path, n_path, from, status);
     return hipGetLastError();
   };
-  if (p.dtype == DLLM_BF16) return p.head_dim == 128 ? launch(accept_kernel<bf16_t, 128>) : launch(accept_kernel<bf16_t, 64>);
-  return p.head_dim == 128 ? launch(accept_kernel<float, 128>) : launch(accept_kernel<float, 64>);
+  if (p.dtype == DLLM_BF16)
+    return p.head_dim == 128 ? launch(pages_accept_kernel<bf16_t, 128>, accept_kernel<bf16_t, 128>)
+                             : launch(pages_accept_kernel<bf16_t, 64>, accept_kernel<bf16_t, 64>);
+  return p.head_dim == 128 ? launch(pages_accept_kernel<float, 128>, accept_kernel<float, 128>)
+                           : launch(pages_accept_kernel<float, 64>, accept_kernel<float, 64>);
 }
 
 size_t pages_compact_workspace(int n_pages) { return (16 + 3 * size_t(n_pages)) * sizeof(int32_t); }

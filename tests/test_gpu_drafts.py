@@ -497,6 +497,9 @@ class Drafts(Both):
     (2, dict(layers=1, heads=1, pages=1100, seqs=40, blocks=70)),
     (3, dict(page=256, heads=3, pages=9, blocks=3, hd=128)),
     (4, dict(pages=2500, seqs=600, blocks=60, heads=1, layers=1)),    # tables past what one workgroup clears
+    (5, dict(layers=3, heads=8, hd=128)),                             # rows past what one workgroup moves
+    (6, dict(layers=4, heads=9, hd=128, dtype=torch.float32)),
+    (7, dict(layers=4, heads=7, dtype=torch.float32)),
 ])
 def test_random_acceptances(seed, kw):
     rng = random.Random(seed)
@@ -549,8 +552,8 @@ def test_acceptance_errors_change_nothing():
 
 def test_long_paths():
     """Paths of many batches of rows, over pages and back by one."""
-    for dtype, hd in ((BF16, 128), (F32, 64)):
-        both = Drafts(pages=160, page=16, seqs=3, blocks=70, dtype=dtype, hd=hd)
+    for dtype, hd, heads in ((BF16, 128, 2), (F32, 64, 2), (BF16, 64, 11), (F32, 128, 11)):
+        both = Drafts(pages=160, page=16, seqs=3, blocks=70, dtype=dtype, hd=hd, heads=heads)
         assert both.call("grow", [0, 1, 2], [1040, 1030, 17]) == OK
         rng = random.Random(2)
         paths = [list(range(1, 1024)), sorted(rng.sample(range(1024), 500)), [16]]
