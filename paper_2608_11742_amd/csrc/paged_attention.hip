@@ -50,6 +50,7 @@
 // rounded, narrow before.
 #include <algorithm>
 #include <climits>
+#include <utility>
 
 #include "common.h"
 #include "kernels.h"
@@ -726,6 +727,16 @@ struct Narrow {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 
+template <class F, int... I>
+__device__ __forceinline__ void static_for_each(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+// f(0) .. f(N - 1), each with a constant
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for_each(std::make_integer_sequence<int, N>{}, f);
+}
+
 // 16 bytes per lane from global memory straight into LDS (lane l: lds + 16 l)
 __device__ __forceinline__ void copy16(const void* src, uint32_t lds) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src),
@@ -755,6 +766,15 @@ struct Tile {
   // key within its 32 of MFMA row r
   __device__ __forceinline__ static int key_of(int r) { return (r & 0x13) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
+  // page ids of a tile's 16-key groups
+  struct Ids {
+    int a, b, c, d;
+    template <int i>
+    __device__ __forceinline__ int of() const {
+      return i == 0 ? a : i == 1 ? b : i == 2 ? c : d;
+    }
+  };
+
   // one wave's part (`wave` of four) of copying a tile
   struct Copier {
     static constexpr int IC = KB / 1024 / kWaves;   // copies the wave issues for K, and for V
@@ -778,30 +798,33 @@ struct Tile {
     __device__ __forceinline__ int in_pool(int p) const { return min(max(p, 0), n_pages - 1); }
     // table entries of the tile's 16-key groups (past the last key: its page
     // again), brought into the pool where they are used: loads do not wait here
-    __device__ __forceinline__ void pages_at(const Share& w, int k0, int (&id)[4]) const {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) id[i] = w.page(k0 + 16 * i, shift, last_block);
+    __device__ __forceinline__ Ids pages_at(const Share& w, int k0) const {
+      return Ids{w.page(k0, shift, last_block), w.page(k0 + 16, shift, last_block), w.page(k0 + 32, shift, last_block),
+                 w.page(k0 + 48, shift, last_block)};
     }
-    __device__ __forceinline__ void issue(int k0, const int (&id)[4], uint32_t dst) const {
-      const int pmask = page_len - 1, kr = lane / CK, vd = lane >> 3, vc = (lane & 7) ^ vswz(8 * wave + vd);
-#pragma unroll
-      for (int i = 0; i < IC; ++i) {
-        const int grp = i * kWaves + wave, r = grp * KROWS + kr;
-        // a copy's rows share a 16-key group, one of C over the waves
-        constexpr int C = kWaves * KROWS / 16;
-        const int u = wave * KROWS / 16, sub = i * C + u;
-        const int even = id[i * C], odd = id[i * C + C - 1];
-        const int page = in_pool(u ? odd : even);
-        const uint8_t* src = K + page * page_bytes + ((k0 + sub * 16) & pmask) * RB;
-        copy16(src + (r & 15) * RB + ((lane % CK) ^ kswz(r)) * 16, dst + grp * 1024);
-      }
-      const int page = in_pool(vc < 4 ? (vc < 2 ? id[0] : id[1]) : (vc < 6 ? id[2] : id[3]));
+    // the i-th of IC copies of keys, and of values
+    template <int i>
+    __device__ __forceinline__ void issue_keys(int k0, Ids id, uint32_t dst) const {
+      const int pmask = page_len - 1, kr = lane / CK;
+      const int grp = i * kWaves + wave, r = grp * KROWS + kr;
+      // a copy's rows share a 16-key group, one of C over the waves
+      constexpr int C = kWaves * KROWS / 16;
+      const int u = wave * KROWS / 16, sub = i * C + u;
+      const int page = in_pool(u ? id.template of<i * C + C - 1>() : id.template of<i * C>());
+      const uint8_t* src = K + page * page_bytes + ((k0 + sub * 16) & pmask) * RB;
+      copy16(src + (r & 15) * RB + ((lane % CK) ^ kswz(r)) * 16, dst + grp * 1024);
+    }
+    template <int i>
+    __device__ __forceinline__ void issue_values(int k0, Ids id, uint32_t dst) const {
+      const int pmask = page_len - 1, vd = lane >> 3, vc = (lane & 7) ^ vswz(8 * wave + vd);
+      const int page = in_pool(vc < 4 ? (vc < 2 ? id.a : id.b) : (vc < 6 ? id.c : id.d));
       const uint8_t* src = V + page * page_bytes + size_t(vd) * (page_len * 2) + ((k0 + 8 * vc) & pmask) * 2;
-#pragma unroll
-      for (int i = 0; i < IC; ++i) {
-        const int grp = i * kWaves + wave;
-        copy16(src + size_t(grp) * 8 * (page_len * 2), dst + KB + grp * 1024);
-      }
+      const int grp = i * kWaves + wave;
+      copy16(src + size_t(grp) * 8 * (page_len * 2), dst + KB + grp * 1024);
+    }
+    __device__ __forceinline__ void issue(int k0, Ids id, uint32_t dst) const {
+      static_for<IC>([&](auto i) { issue_keys<i>(k0, id, dst); });
+      static_for<IC>([&](auto i) { issue_values<i>(k0, id, dst); });
     }
   };
 
@@ -867,16 +890,22 @@ struct Rows32 {
   }
   template <int H>
   __device__ __forceinline__ void scores(const u32x4 (&kf)[H][L::QS], f32x16 (&sc)[H]) const {
+    scores(kf, sc, [](auto) {});
+  }
+  // step(st) after the products of step st
+  template <int H, class F>
+  __device__ __forceinline__ void scores(const u32x4 (&kf)[H][L::QS], f32x16 (&sc)[H], F&& step) const {
 #pragma unroll
     for (int h = 0; h < H; ++h)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[h][i] = 0.f;
-#pragma unroll
-    for (int st = 0; st < L::QS; ++st)
+    static_for<L::QS>([&](auto st) {
 #pragma unroll
       for (int h = 0; h < H; ++h)
         sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[h][st]),
                                                         __builtin_bit_cast(bf16x8, qf[st]), sc[h], 0, 0, 0);
+      step(st);
+    });
   }
   // scores of keys k0 .. into probabilities (binary16 pairs); keys from lim on are not seen
   template <int H>
@@ -1010,10 +1039,9 @@ struct Wide {
     const int lim_row = limit_of(a, entry, at.i), lim = min(lim_row, w.k1);
     const int root = TREE ? __builtin_amdgcn_readfirstlane(entry.held - entry.rows) : 0;   // the tree's first position
 
-    int id[4];
-    copier.pages_at(w, w.k0, id);
+    typename L::Ids id = copier.pages_at(w, w.k0);
     if (w.k0 < w.k1) copier.issue(w.k0, id, lds0);
-    copier.pages_at(w, w.k0 + kTile, id);
+    id = copier.pages_at(w, w.k0 + kTile);
     int slot = 0;
     bool any_wild = false;
     for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
@@ -1024,17 +1052,22 @@ struct Wide {
       if (k0 + kTile > w.k1) {
         L::zero_values(sv, tid, kThreads, w.k1 - k0);
         barrier_lds();
-      } else if (k0 + kTile < w.k1) {
-        copier.issue(k0 + kTile, id, lds0 + (slot ^ 1) * L::BYTES);
-        copier.pages_at(w, k0 + 2 * kTile, id);
       }
+      const bool more = k0 + kTile < w.k1;
+      const uint32_t next = lds0 + (slot ^ 1) * L::BYTES;
       const bool masked = TREE && k0 + kTile > root;
       if (masked && __syncthreads_or(L::wild_values(sv, tid, kThreads))) {
         any_wild = true;
         L::tame_values(sv, tid, kThreads);
         __syncthreads();
       }
-      if (idle) continue;
+      if (idle) {
+        if (more) {
+          copier.issue(k0 + kTile, id, next);
+          id = copier.pages_at(w, k0 + 2 * kTile);
+        }
+        continue;
+      }
       const uint64_t seen = masked ? seen_of(a, at.b, at.i, root, lim, k0) : 0;
       // every K fragment is on its way before the first product waits for one,
       // half of the V fragments before the softmax
@@ -1045,7 +1078,17 @@ struct Wide {
 #pragma unroll
         for (int h = 0; h < 2; ++h) kf[h][st] = L::key_chunk(sk, h, st, lane);
       __builtin_amdgcn_sched_barrier(0);
-      rows.scores(kf, sc);
+      if (more) {
+        rows.scores(kf, sc, [&](auto st) {
+          static_assert(2 * Copier::IC == L::QS, "a copy a step");
+          if constexpr (st < Copier::IC) copier.template issue_keys<st>(k0 + kTile, id, next);
+          else copier.template issue_values<st - Copier::IC>(k0 + kTile, id, next);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        id = copier.pages_at(w, k0 + 2 * kTile);
+      } else {
+        rows.scores(kf, sc);
+      }
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
@@ -1115,10 +1158,9 @@ struct Halves {
     const int fr = lane & 31, f = lane >> 5, block = wave & 1, half = wave >> 1;
     const uint32_t lds0 = lds_address(smem);
     const Copier copier(a, w.head, wave, w.k1);
-    int id[4];
-    copier.pages_at(w, w.k0, id);
+    typename L::Ids id = copier.pages_at(w, w.k0);
     if (w.k0 < w.k1) copier.issue(w.k0, id, lds0);
-    copier.pages_at(w, w.k0 + kTile, id);
+    id = copier.pages_at(w, w.k0 + kTile);
 
     const RowAt at = row_at(j, min(w.row0 + 32 * block + fr, w.row_end - 1));
     Rows32<HD> rows;
@@ -1139,7 +1181,7 @@ struct Halves {
         barrier_lds();
       } else if (k0 + kTile < w.k1) {
         copier.issue(k0 + kTile, id, lds0 + (slot ^ 1) * L::BYTES);
-        copier.pages_at(w, k0 + 2 * kTile, id);
+        id = copier.pages_at(w, k0 + 2 * kTile);
       }
       const bool masked = k0 + kTile > root;
       if (masked && __syncthreads_or(L::wild_values(sv, tid, kThreads))) {
@@ -1250,10 +1292,9 @@ struct Pairs {
     const typename L::Copier copier(a, head, wave & 3, s), own_keys(a, head, 0, e.held);
     const int first = kTile * tile;   // of this wave's tile in a step
     const uint32_t lds0 = lds_address(smem) + tile * L::BYTES;
-    int id[4];
-    copier.pages_at(prefix, first, id);
+    typename L::Ids id = copier.pages_at(prefix, first);
     if (s > 0) copier.issue(first, id, lds0);
-    copier.pages_at(prefix, first + kKeys, id);
+    id = copier.pages_at(prefix, first + kKeys);
 
     const int row = min(r0 + fr, per - 1), i = row / j.group, g = row % j.group;
     Rows32<HD> rows;
@@ -1272,7 +1313,7 @@ struct Pairs {
         __syncthreads();
       } else if (k0 + kKeys < s) {
         copier.issue(k0 + kKeys + first, id, lds0 + (slot ^ 1) * (2 * L::BYTES));
-        copier.pages_at(prefix, k0 + 2 * kKeys + first, id);
+        id = copier.pages_at(prefix, k0 + 2 * kKeys + first);
       }
       if (k0 >= own_from) continue;   // the entry ends in this step, or before it
       const int h = way & 1, keys = k0 + 32 * way;
