@@ -298,23 +298,36 @@ __device__ __forceinline__ float quad_sum(float x) {
 // products with the masks in place of the weights count per row and dim those
 // that are +inf or NaN and those that are -inf or NaN.
 
-// bits of the keys k0 .. k0 + 63 that row i of entry b sees: those before the
-// tree's first position `root` (negative where the sequence is shorter than its
-// rows), of the tree those in its mask, none from `end` on
-__device__ __forceinline__ uint64_t seen_of(const PagedAttn& a, int b, int i, int root, int end, int k0) {
+// the words of row i's mask that hold the tree's keys among k0 .. k0 + 63; `root`:
+// the tree's first position, negative where the sequence is shorter than its rows
+struct MaskWords {
+  uint32_t w[3];
+};
+__device__ __forceinline__ MaskWords mask_words(const PagedAttn& a, int b, int i, int root, int k0) {
   const uint32_t* row = a.mask + (size_t(b) * a.max_rows + i) * a.words;
+  const int j = max(k0 - root, 0) >> 5;
+  MaskWords m;
   // (words past the mask's are read from inside it, so that no load waits behind a branch)
-  auto word = [&](int j) {
-    const uint32_t w = row[min(j, a.words - 1)];
-    return j < a.words ? w : 0u;
-  };
-  const int t = k0 - root, j = max(t, 0) >> 5, shift = t & 31;
-  const uint64_t w = uint64_t(word(j + 1)) << 32 | word(j), next = word(j + 2);
+#pragma unroll
+  for (int u = 0; u < 3; ++u) {
+    const uint32_t w = row[min(j + u, a.words - 1)];
+    m.w[u] = j + u < a.words ? w : 0u;
+  }
+  return m;
+}
+// bits of the keys k0 .. k0 + 63 that the row sees: those before the tree, of the
+// tree those in its mask, none from `end` on
+__device__ __forceinline__ uint64_t seen_in(const MaskWords& m, int root, int end, int k0) {
+  const int t = k0 - root, shift = t & 31;
+  const uint64_t w = uint64_t(m.w[1]) << 32 | m.w[0];
   uint64_t bits;
-  if (t >= 0) bits = w >> shift | (shift ? next << (64 - shift) : 0);
+  if (t >= 0) bits = w >> shift | (shift ? uint64_t(m.w[2]) << (64 - shift) : 0);
   else bits = t <= -64 ? ~uint64_t(0) : w << -t | ~(~uint64_t(0) << -t);
   const int left = end - k0;
   return left >= 64 ? bits : left <= 0 ? 0 : bits & ~(~uint64_t(0) << left);
+}
+__device__ __forceinline__ uint64_t seen_of(const PagedAttn& a, int b, int i, int root, int end, int k0) {
+  return seen_in(mask_words(a, b, i, root, k0), root, end, k0);
 }
 
 // of a word of values: 1 in the places of those that are +inf or NaN (up), -inf or NaN (down)
@@ -822,6 +835,14 @@ struct Tile {
       const int grp = i * kWaves + wave;
       copy16(src + size_t(grp) * 8 * (page_len * 2), dst + KB + grp * 1024);
     }
+    // the c-th of all 2 IC, one after each step over head_dim of the products
+    template <int c>
+    __device__ __forceinline__ void issue_one(int k0, Ids id, uint32_t dst) const {
+      static_assert(2 * IC == QS, "a copy a step");
+      if constexpr (c < IC) issue_keys<c>(k0, id, dst);
+      else issue_values<c - IC>(k0, id, dst);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     __device__ __forceinline__ void issue(int k0, Ids id, uint32_t dst) const {
       static_for<IC>([&](auto i) { issue_keys<i>(k0, id, dst); });
       static_for<IC>([&](auto i) { issue_values<i>(k0, id, dst); });
@@ -840,13 +861,29 @@ struct Tile {
       *p = x;
     }
   }
-  // whether any of the tile's values is infinite or no number, as one thread of `threads` finds it
-  __device__ __forceinline__ static bool wild_values(const uint8_t* sv, int t, int threads) {
-    uint32_t wild = 0;
-    for (int c = t; c < HD * 8; c += threads) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(sv + 16 * c);
+  // zero_values, and whether any other of the tile's values is infinite or no
+  // number, as this one of kThreads threads finds it
+  __device__ __forceinline__ static bool tidy_values(uint8_t* sv, int t, int left) {
+    constexpr int N = HD * 8 / kThreads;
+    u32x4 x[N];
+    auto at = [&](int i) {
+      const int c = t + i * kThreads, d = c >> 3;
+      return reinterpret_cast<u32x4*>(sv + d * 128 + (((c & 7) ^ vswz(d)) << 4));
+    };
 #pragma unroll
-      for (int i = 0; i < 4; ++i) wild |= wild_bits<true>(x[i]);
+    for (int i = 0; i < N; ++i) x[i] = *at(i);
+    const int n = left - 8 * (t & 7);   // kThreads is a multiple of 8: all of a thread's chunks are of the same keys
+    uint32_t wild = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        x[i][u] &= n > 2 * u + 1 ? ~0u : n > 2 * u ? 0xffffu : 0u;
+        wild |= wild_bits<true>(x[i][u]);
+      }
+    if (n < 8) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) *at(i) = x[i];
     }
     return wild != 0;
   }
@@ -1045,22 +1082,26 @@ struct Wide {
     int slot = 0;
     bool any_wild = false;
     for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
+      const bool masked = TREE && k0 + kTile > root;
+      MaskWords words{};
+      if (masked) words = mask_words(a, at.b, at.i, root, k0);
       wait_vmcnt<0>();
       barrier_lds();   // tile k0 has landed; the other slot has been read
       const uint8_t* sk = smem + slot * L::BYTES;
       uint8_t* sv = smem + slot * L::BYTES + L::KB;
-      if (k0 + kTile > w.k1) {
+      if (masked) {
+        if (__syncthreads_or(L::tidy_values(sv, tid, w.k1 - k0))) {
+          any_wild = true;
+          L::tame_values(sv, tid, kThreads);
+          __syncthreads();
+        }
+      } else if (k0 + kTile > w.k1) {
         L::zero_values(sv, tid, kThreads, w.k1 - k0);
         barrier_lds();
       }
       const bool more = k0 + kTile < w.k1;
       const uint32_t next = lds0 + (slot ^ 1) * L::BYTES;
-      const bool masked = TREE && k0 + kTile > root;
-      if (masked && __syncthreads_or(L::wild_values(sv, tid, kThreads))) {
-        any_wild = true;
-        L::tame_values(sv, tid, kThreads);
-        __syncthreads();
-      }
+      const uint64_t seen = masked ? seen_in(words, root, lim, k0) : 0;
       if (idle) {
         if (more) {
           copier.issue(k0 + kTile, id, next);
@@ -1068,7 +1109,6 @@ struct Wide {
         }
         continue;
       }
-      const uint64_t seen = masked ? seen_of(a, at.b, at.i, root, lim, k0) : 0;
       // every K fragment is on its way before the first product waits for one,
       // half of the V fragments before the softmax
       u32x4 kf[2][L::QS], vf[2][L::NDB], pf[4];
@@ -1079,12 +1119,7 @@ struct Wide {
         for (int h = 0; h < 2; ++h) kf[h][st] = L::key_chunk(sk, h, st, lane);
       __builtin_amdgcn_sched_barrier(0);
       if (more) {
-        rows.scores(kf, sc, [&](auto st) {
-          static_assert(2 * Copier::IC == L::QS, "a copy a step");
-          if constexpr (st < Copier::IC) copier.template issue_keys<st>(k0 + kTile, id, next);
-          else copier.template issue_values<st - Copier::IC>(k0 + kTile, id, next);
-          __builtin_amdgcn_sched_barrier(0);
-        });
+        rows.scores(kf, sc, [&](auto st) { copier.template issue_one<st>(k0 + kTile, id, next); });
         id = copier.pages_at(w, k0 + 2 * kTile);
       } else {
         rows.scores(kf, sc);
@@ -1172,25 +1207,26 @@ struct Halves {
     int slot = 0;
     bool any_wild = false;
     for (int k0 = w.k0; k0 < w.k1; k0 += kTile, slot ^= 1) {
+      const int keys = k0 + 32 * half;
+      const bool masked = k0 + kTile > root;
+      MaskWords words{};
+      if (masked) words = mask_words(a, at.b, at.i, root, keys);
       wait_vmcnt<0>();
       barrier_lds();   // tile k0 has landed; the other slot has been read
       const uint8_t* sk = smem + slot * L::BYTES;
       uint8_t* sv = smem + slot * L::BYTES + L::KB;
-      if (k0 + kTile > w.k1) {
+      if (masked) {
+        if (__syncthreads_or(L::tidy_values(sv, tid, w.k1 - k0))) {
+          any_wild = true;
+          L::tame_values(sv, tid, kThreads);
+          __syncthreads();
+        }
+      } else if (k0 + kTile > w.k1) {
         L::zero_values(sv, tid, kThreads, w.k1 - k0);
         barrier_lds();
-      } else if (k0 + kTile < w.k1) {
-        copier.issue(k0 + kTile, id, lds0 + (slot ^ 1) * L::BYTES);
-        id = copier.pages_at(w, k0 + 2 * kTile);
       }
-      const bool masked = k0 + kTile > root;
-      if (masked && __syncthreads_or(L::wild_values(sv, tid, kThreads))) {
-        any_wild = true;
-        L::tame_values(sv, tid, kThreads);
-        __syncthreads();
-      }
-      const int keys = k0 + 32 * half;
-      const uint64_t seen = masked ? seen_of(a, at.b, at.i, root, w.k1, keys) : 0;
+      const bool more = k0 + kTile < w.k1;
+      const uint32_t next = lds0 + (slot ^ 1) * L::BYTES;
       u32x4 kf[1][L::QS], vf[2][L::NDB], pf[2];
       f32x16 sc[1];
 #pragma unroll
@@ -1200,8 +1236,13 @@ struct Halves {
 #pragma unroll
         for (int db = 0; db < L::NDB; ++db) vf[st][db] = L::value_chunk(sv, 2 * half + st, db, lane);
       __builtin_amdgcn_sched_barrier(0);
-      rows.scores(kf, sc);
-      if (masked) Rows32<HD>::hide(sc, seen);
+      if (more) {
+        rows.scores(kf, sc, [&](auto st) { copier.template issue_one<st>(k0 + kTile, id, next); });
+        id = copier.pages_at(w, k0 + 2 * kTile);
+      } else {
+        rows.scores(kf, sc);
+      }
+      if (masked) Rows32<HD>::hide(sc, seen_in(words, root, w.k1, keys));
       rows.softmax(sc, keys, masked ? INT_MAX : w.k1, j.scale_log2, pf);
 #pragma unroll
       for (int st = 0; st < 2; ++st)
