@@ -491,13 +491,20 @@ dllm_status kv_pages_tree(const dllm_kv_pages* pages, const int32_t* seqs, int32
  * do not reach it, whatever they are.  A row that sees no position is 0.
  * Values that it does see are multiplied by weights of up to 2^15 before the
  * sums are divided: fp32 ones of 2^112 and more come out infinite.
- * Everything else, the workspace (kv_pages_attention_workspace_bytes) and the
- * plan (kv_pages_attention_plan) as there. */
+ * Everything else and the workspace (kv_pages_attention_workspace_bytes) as
+ * there. */
 dllm_status kv_pages_attention_tree(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
                                     int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
                                     const dllm_rows* out, const uint32_t* mask, int32_t prefix_seq,
                                     int32_t shared_len, int32_t max_len, float scale, void* ws, size_t ws_bytes,
                                     dllm_stream stream);
+
+/* How kv_pages_attention_tree divides a call of these sizes, as
+ * kv_pages_attention_plan.  Rows of a part can be 64 too.  Tails of several ranges
+ * have as many slots, n * tail_ranges at most, as the device gives out by the
+ * lengths of the entries (n <= 64; tail_keys is 0 then). */
+dllm_status kv_pages_attention_tree_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
+                                         int32_t shared_len, int32_t max_len, kv_attention_plan* plan);
 
 /* Of the last n_rows[i] positions of sequence seqs[i] (NULL: max_rows each),
  * the rows path[i][0 .. n_path[i]-1] are kept, in that order, in every layer:

@@ -16,7 +16,7 @@ from .binding import (  # noqa: F401
     kv_pages_compact_workspace_bytes, kv_pages_write, kv_pages_attention, kv_pages_attention_workspace_bytes,
     kv_pages_attention_plan,
     Rotary, dllm_rotary_frequencies, rotary_rows, kv_pages_append, kv_pages_tree, kv_pages_attention_tree,
-    kv_pages_accept, kv_pages_accept_workspace_bytes,
+    kv_pages_attention_tree_plan, kv_pages_accept, kv_pages_accept_workspace_bytes,
     dllm_forward_pages, dllm_workspace_bytes_pages,
 )
 from .model import Model  # noqa: F401

@@ -128,6 +128,7 @@ SIGNATURES = {
     "kv_pages_tree": (i32, [C.POINTER(KvPagesC), vp, i32, i32, vp, vp, vp, vp, vp]),
     "kv_pages_attention_tree": (i32, [C.POINTER(KvPagesC), i32, vp, i32, i32, vp, i32, C.POINTER(Rows), C.POINTER(Rows),
                                       vp, i32, i32, i32, f32, vp, sz, vp]),
+    "kv_pages_attention_tree_plan": (i32, [C.POINTER(KvPagesC), i32, i32, i32, i32, i32, C.POINTER(AttentionPlan)]),
     "kv_pages_accept_workspace_bytes": (sz, [C.POINTER(KvPagesC), i32, i32]),
     "kv_pages_accept": (i32, [C.POINTER(KvPagesC), vp, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
     "dllm_profile_begin": (i32, [vp, i32]),

@@ -473,6 +473,16 @@ def kv_pages_attention_tree(pages: KvPages, layer: int, seqs, q, out, mask, ws, 
         _check(status)
 
 
+def kv_pages_attention_tree_plan(pages: KvPages, n: int, max_rows: int, n_heads: int, shared_len: int = 0,
+                                 max_len: int | None = None):
+    """How kv_pages_attention_tree divides a call of these sizes, as kv_pages_attention_plan."""
+    if max_len is None:
+        max_len = pages.table.shape[1] * pages.page_len
+    plan = _abi.AttentionPlan()
+    _check(lib().kv_pages_attention_tree_plan(pages._ref, n, max_rows, n_heads, shared_len, max_len, C.byref(plan)))
+    return plan
+
+
 def kv_pages_accept_workspace_bytes(pages: KvPages, n: int, max_path: int) -> int:
     return lib().kv_pages_accept_workspace_bytes(pages._ref, n, max_path)
 

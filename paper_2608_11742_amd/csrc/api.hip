@@ -1064,13 +1064,14 @@ dllm_status kv_pages_attention_tree(const dllm_kv_pages* pages, int32_t layer, c
                 max_len, scale, ws, ws_bytes, stream);
 }
 
-dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
-                                    int32_t shared_len, int32_t max_len, kv_attention_plan* plan) {
-  dllm_status st = check_attention(pages, n, max_rows, n_heads, "kv_pages_attention_plan");
+namespace {
+
+dllm_status plan_of(const char* who, const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
+                    int32_t shared_len, int32_t max_len, bool tree, kv_attention_plan* plan) {
+  dllm_status st = check_attention(pages, n, max_rows, n_heads, who);
   if (st != DLLM_OK) return st;
-  if (!plan) return fail(DLLM_EINVAL, "kv_pages_attention_plan: NULL plan");
-  if (shared_len < 0 || max_len < 0)
-    return fail(DLLM_ESHAPE, "kv_pages_attention_plan: shared_len %d max_len %d", shared_len, max_len);
+  if (!plan) return fail(DLLM_EINVAL, "%s: NULL plan", who);
+  if (shared_len < 0 || max_len < 0) return fail(DLLM_ESHAPE, "%s: shared_len %d max_len %d", who, shared_len, max_len);
   PagedAttn a{};
   a.p = *pages;
   a.n = n;
@@ -1078,8 +1079,22 @@ dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32
   a.heads = n_heads;
   a.shared_len = shared_len;
   a.max_len = max_len;
-  *plan = paged_attention_plan(a);
+  *plan = paged_attention_plan(a, tree);
   return DLLM_OK;
+}
+
+}  // namespace
+
+dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
+                                    int32_t shared_len, int32_t max_len, kv_attention_plan* plan) {
+  return plan_of("kv_pages_attention_plan", pages, n, max_rows, n_heads, shared_len, max_len, false, plan);
+}
+
+dllm_status kv_pages_attention_tree_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
+                                         int32_t shared_len, int32_t max_len, kv_attention_plan* plan) {
+  const char* who = "kv_pages_attention_tree_plan";
+  if (max_rows > KV_TREE_MAX_ROWS) return fail(DLLM_ESHAPE, "%s: max_rows %d > %d", who, max_rows, KV_TREE_MAX_ROWS);
+  return plan_of(who, pages, n, max_rows, n_heads, shared_len, max_len, true, plan);
 }
 
 dllm_status dllm_forward_pages(dllm_model* m, const int32_t* tokens, int32_t batch, int32_t seq,

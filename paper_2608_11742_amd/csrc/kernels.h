@@ -198,7 +198,7 @@ size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, in
 size_t paged_attention_workspace_upto(const dllm_kv_pages& p, int n, int max_rows, int heads);
 hipError_t paged_attention(const PagedAttn& a, hipStream_t s);
 // how it divides the call (by its sizes alone)
-kv_attention_plan paged_attention_plan(const PagedAttn& a);
+kv_attention_plan paged_attention_plan(const PagedAttn& a, bool tree);
 
 // register-only bf16 MFMA loop (benchmark calibration); *flop: the launch's MFMA work
 hipError_t mfma_calibration(bool random_operands, int iters, int workgroups, double* flop, hipStream_t s);

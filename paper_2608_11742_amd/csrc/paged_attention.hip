@@ -81,8 +81,7 @@ struct Job {
   Part prefix, tail;
   bool stacked;       // the prefix is a part of its own; else each tail starts at position 0
   bool direct;        // one range in all: the output itself
-  bool by_length;     // the tails' ranges go to the entries by their lengths (see Slots),
-  int least;          // in steps of at least so many tiles
+  int slots;          // of a tree's tails (see Slots); 0: each entry has tail.ranges
 };
 
 __device__ __forceinline__ int most_positions(const PagedAttn& a) { return a.p.max_blocks * a.p.page_len; }
@@ -170,9 +169,9 @@ __device__ __forceinline__ int wave_sums(int v) {
 }
 __device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_sums(v), kWave - 1); }
 
-// The tails of trees are divided by what the entries hold: of the n * ranges
-// slots that a head and row tile have, an entry gets one for every `step` keys,
-// the least step with which all find a slot.  So one long entry among short
+// The tails of trees are divided by what the entries hold: of the slots that a
+// head and row tile have, an entry gets one for every `step` tiles, the least
+// step with which all find a slot (and 4 at least).  So one long entry among short
 // ones, or a max_len that is far off, leaves no workgroup without work.  Every
 // wave works it out from the lengths, a lane for each of up to 64 entries.
 struct Slots {
@@ -181,14 +180,14 @@ struct Slots {
 };
 template <bool TREE>
 __device__ __forceinline__ Slots slots_of(const Job& j, int shared) {
-  const int lane = threadIdx.x & 63, all = j.a.n * j.tail.ranges;
+  const int lane = threadIdx.x & 63, all = j.slots;
   Slots s{};
   if (lane < j.a.n) {
     s.e = entry_of(j.a, lane);
     const int from = j.stacked ? stacked_of<TREE>(s.e, shared, j.prefix.range) : 0;
     s.tiles = s.e.rows > 0 ? (s.e.held - from + kTile - 1) / kTile : 0;
   }
-  int step = max((wave_total(s.tiles) + all - 1) / all, j.least), used;
+  int step = max((wave_total(s.tiles) + all - 1) / all, 4), used;
   // at most a slot too many an entry: the step grows until they fit
   while (s.count = (s.tiles + step - 1) / step, used = wave_total(s.count), used > all)
     step += max(1, int(int64_t(step) * (used - all) / all));
@@ -206,7 +205,9 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
   w.head = it.item % a.p.n_kv_heads;
   const int t = it.item / a.p.n_kv_heads;
   int r = t % part.ranges, b = t / part.ranges;
-  if (b >= (in_prefix ? 1 : a.n)) return false;   // items are filled up to whole rounds of XCDs
+  const bool by_length = TREE && j.slots && !in_prefix;
+  // items are filled up to whole rounds of XCDs
+  if (by_length ? t >= j.slots : b >= (in_prefix ? 1 : a.n)) return false;
   const int s = shared_of(a);
   const int64_t rows_all = int64_t(a.n) * a.max_rows * a.heads;
   if (in_prefix) {
@@ -221,7 +222,7 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
   }
   int range = part.range, ranges = part.ranges;
   w.rec0 = (j.prefix.ranges + r) * rows_all;
-  if (TREE && j.by_length) {
+  if (by_length) {
     const Slots z = slots_of<TREE>(j, s);
     // slot t is of the last entry that starts at or before it (one without any starts where the next does)
     b = __popcll(__ballot(int(threadIdx.x & 63) < a.n && z.first <= t)) - 1;
@@ -1535,7 +1536,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
   // the tail's records: one after another like the prefix's, or slots of an entry's rows
   const float* tails = rec + j.prefix.ranges * stride;
   size_t tail_stride = stride;
-  if (TREE && j.by_length) {
+  if (TREE && j.slots) {
     const Slots z = slots_of<TREE>(j, shared_of(a));
     const int count = __shfl(z.count, b, kWave), first = __shfl(z.first, b, kWave);
     nt = live ? count : 0;
@@ -1649,7 +1650,7 @@ template <typename T, int HD, int PREFIX, int TAIL, bool TREE>
 void launch_parts(const Job& j, hipStream_t s) {
   const int kvh = j.a.p.n_kv_heads;
   const int prefix = j.prefix.ranges ? blocks_of(j.prefix.ranges * kvh, j.prefix.row_tiles) : 0;
-  const int tail = blocks_of(j.a.n * j.tail.ranges * kvh, j.tail.row_tiles);
+  const int tail = blocks_of((j.slots ? j.slots : j.a.n * j.tail.ranges) * kvh, j.tail.row_tiles);
   hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL, TREE>), dim3(prefix + tail),
                      dim3(kThreads), 0, s, j, prefix);
 }
@@ -1676,7 +1677,7 @@ void launch(const Job& j, int prefix, int tail, hipStream_t s) {
   // rows of many ranges take several groups of lanes each: the records of a
   // row come in turn, four at a time
   constexpr int kGroups = kThreads / (HD / 4);
-  const int ranges = j.prefix.ranges + j.tail.ranges;
+  const int ranges = j.prefix.ranges + (j.slots ? cdiv(j.slots, j.a.n) : j.tail.ranges);
   const int slices = ranges <= 4 ? 1 : ranges <= 8 ? 2 : ranges <= 16 ? 4 : 8;
   hipLaunchKernelGGL((join_kernel<T, HD, TREE>), dim3(cdiv(j.a.n * j.a.max_rows * j.a.heads, kGroups / slices)),
                      dim3(kThreads), 0, s, j, slices);
@@ -1754,9 +1755,52 @@ struct Division {
   bool pairs, stacked;
   int mode_p, mode_t;
   Part prefix, tail;
+  int slots;        // of a tree's tails, as in Job
   int64_t shared;   // whole pages of the prefix, as far as the caller knows
 };
-Division divide(const PagedAttn& a) {
+
+// More than 32 rows of a tree over keys of their own: in halves or wide, and in
+// how many slots.  Not divided, or as many as give each CU one or two
+// workgroups, by the least estimated time: 2.5 us and, for every round of two
+// workgroups a CU, 4 and what a tile of 64 keys of heads of 128 takes, 1.45 wide
+// and 0.95 in halves alone on a CU, 2.3 and 1.75 where two share it, or what the keys
+// take from memory; 4 more and the records at 5 TB/s where they are joined.  Measured, us, 32 heads, wide not
+// divided / one a CU / two / halves not divided: 12 x 43 rows of 8 key heads
+// over 480 positions 19.4 / 29.8 / 29.8 / 19.9, 4 x 100 over 3000 69 / 45 / 44 / 49, 1 x
+// 64 over 2000 49 / 20.1 / 20.1 / 35 (halves, one a CU: 18.0), 16 x 24 over 1000 to 3500
+// 77 / 49 / 44 / 64, 9 x 28 over 6100 130 / 58 / 53 / 89; 32 key heads, 8 x 75 over 990
+// 29 / 29 / 38 / 32; 32 heads of 64, 8 x 60 over 1500 23.7 (halves not divided), 26.4 (two a CU);
+// 32 key heads, 4 x 64 over 4000 to 8000 in halves 101 (one a CU), 89 (two).
+struct TreeTail {
+  int mode, slots;
+  double us;
+};
+// (keys: the longest entry's, theirs on average, and all that are read, a shared prefix once)
+TreeTail plan_tree(const PagedAttn& a, int rows, double longest, double mean, double once) {
+  const int kvh = a.p.n_kv_heads;
+  const int64_t most = a.n <= kWave ? a.n * most_ranges(ROWS128, int64_t(cdiv(rows, rows_of(ROWS128))) * a.n * kvh) : a.n;
+  const double u = a.p.head_dim == 128 ? 1.0 : 0.55;
+  TreeTail best{ROWS128, a.n, 1e30};
+  for (int mode : {ROWS64, ROWS128}) {
+    const int per_slot = cdiv(rows, rows_of(mode)) * kvh;
+    for (int wgs : {0, kCus, 2 * kCus}) {
+      const int slots = int(std::min<int64_t>(std::max(a.n, wgs / per_slot), most));
+      const bool divided = slots > a.n;
+      if (wgs && !divided) continue;
+      const double all = double(slots) * per_slot, rounds = std::max(1.0, all / (2 * kCus));
+      const double tile = u * (mode == ROWS64 ? (all > kCus ? 1.75 : 0.95) : (all > kCus ? 2.3 : 1.45));
+      const double tiles = divided ? std::max(4.0, a.n * mean / kTile / slots + 0.5) : longest / kTile;
+      // (keys and values from memory: 4.5 TB/s with one workgroup a CU, 5.5 with two)
+      const double memory = once * kvh * a.p.head_dim * 4 / (all > kCus ? 5.5e6 : 4.5e6);
+      const double us = 2.5 + rounds * 4.0 + std::max(rounds * tiles * tile, memory) +
+                        (divided ? 4.0 + double(slots) * a.max_rows * a.heads * 2 * record(a.p.head_dim) * sizeof(float) / 5e6 : 0.0);
+      if (us < best.us) best = TreeTail{mode, slots, us};
+    }
+  }
+  return best;
+}
+
+Division divide(const PagedAttn& a, bool tree) {
   Division d{};
   const int dt = a.p.dtype, kvh = a.p.n_kv_heads, group = a.heads / kvh;
   const int64_t most = int64_t(a.p.max_blocks) * a.p.page_len;
@@ -1769,9 +1813,24 @@ Division divide(const PagedAttn& a) {
   const double mean = std::max<int64_t>(0, keys - shared) / 2.0;
   d.prefix = Part{1, 0, kTile};
   d.tail = plan_part(d.mode_t, rows_t, a.n, kvh, std::max(keys, shared));
+  // (the slots of entries that are divided evenly)
+  auto even = [&] { d.slots = tree && a.n <= kWave && d.tail.ranges > 1 ? a.n * d.tail.ranges : 0; };
+  const bool wide_tree = tree && d.mode_t == ROWS128;
+  double own = 0.0;
+  if (wide_tree) {
+    const TreeTail z = plan_tree(a, rows_t, double(std::max(keys, shared)), shared + mean, shared + a.n * mean);
+    d.mode_t = z.mode;
+    d.tail = Part{cdiv(rows_t, rows_of(z.mode)), cdiv(z.slots, a.n), int(most)};
+    d.slots = z.slots > a.n ? z.slots : 0;
+    own = z.us;
+  } else {
+    even();
+  }
   if (shared == 0) return d;
   const Cost none{0, 0};
-  const double own = parts_us(a, d.mode_t, cost_of(a, d.mode_t, d.tail, a.n, shared + mean), none, d.tail.ranges);
+  if (!wide_tree) own = parts_us(a, d.mode_t, cost_of(a, d.mode_t, d.tail, a.n, shared + mean), none, d.tail.ranges);
+  const TreeTail alone{d.mode_t, d.slots, own};
+  if (wide_tree) d.mode_t = ROWS128;
   const int mode = mode_of(dt, rows_p, 1, kvh);
   const Part tail = plan_part(d.mode_t, rows_t, a.n, kvh, longest);
   // what the tails take by themselves, at 5 TB/s
@@ -1789,6 +1848,10 @@ Division divide(const PagedAttn& a) {
     d.prefix = prefix;
     d.tail = tail;
     d.mode_p = mode;
+    even();
+    if (wide_tree && rows_t <= rows_of(ROWS64)) d.mode_t = ROWS64;
+  } else {
+    d.mode_t = alone.mode;
   }
   return d;
 }
@@ -1803,7 +1866,7 @@ hipError_t attend(const PagedAttn& a, hipStream_t s) {
   j.a = a;
   j.scale_log2 = a.scale * 1.4426950408889634f;
   j.group = a.heads / a.p.n_kv_heads;
-  const Division d = divide(a);
+  const Division d = divide(a, TREE);
   const int kvh = a.p.n_kv_heads, hd = a.p.head_dim;
   if (d.pairs) {
     j.direct = true;
@@ -1818,14 +1881,11 @@ hipError_t attend(const PagedAttn& a, hipStream_t s) {
   j.stacked = d.stacked;
   if (d.shared == 0) j.a.shared_len = j.a.prefix_seq = 0;
   j.direct = j.prefix.ranges + j.tail.ranges == 1;
-  // (a prefix over tails in halves has their rows of several entries)
-  const int mode_t = TREE && d.mode_t == ROWS128 && a.max_rows * j.group <= rows_of(ROWS64) ? ROWS64 : d.mode_t;
-  j.by_length = TREE && j.tail.ranges > 1 && a.n <= kWave;
-  j.least = 4;
+  j.slots = d.slots;
   if (a.p.dtype == DLLM_BF16)
-    hd == 128 ? launch<bf16_t, 128, TREE>(j, d.mode_p, mode_t, s) : launch<bf16_t, 64, TREE>(j, d.mode_p, mode_t, s);
+    hd == 128 ? launch<bf16_t, 128, TREE>(j, d.mode_p, d.mode_t, s) : launch<bf16_t, 64, TREE>(j, d.mode_p, d.mode_t, s);
   else
-    hd == 128 ? launch<float, 128, TREE>(j, d.mode_p, mode_t, s) : launch<float, 64, TREE>(j, d.mode_p, mode_t, s);
+    hd == 128 ? launch<float, 128, TREE>(j, d.mode_p, d.mode_t, s) : launch<float, 64, TREE>(j, d.mode_p, d.mode_t, s);
   return hipGetLastError();
 }
 
@@ -1833,8 +1893,8 @@ hipError_t attend(const PagedAttn& a, hipStream_t s) {
 
 hipError_t paged_attention(const PagedAttn& a, hipStream_t s) { return a.mask ? attend<true>(a, s) : attend<false>(a, s); }
 
-kv_attention_plan paged_attention_plan(const PagedAttn& a) {
-  const Division d = divide(a);
+kv_attention_plan paged_attention_plan(const PagedAttn& a, bool tree) {
+  const Division d = divide(a, tree);
   kv_attention_plan p{};
   p.way = d.pairs ? KV_WAY_PAIRS : d.stacked ? KV_WAY_PARTS : KV_WAY_ENTRIES;
   if (d.pairs) return p;
@@ -1845,7 +1905,7 @@ kv_attention_plan paged_attention_plan(const PagedAttn& a) {
   }
   p.tail_rows = rows_of(d.mode_t);
   p.tail_ranges = d.tail.ranges;
-  p.tail_keys = d.tail.range;
+  p.tail_keys = d.slots ? 0 : d.tail.range;
   return p;
 }
 
