@@ -3,7 +3,7 @@
 //
 // Types, devices, shapes and strides are read from the tensors directly: the
 // same checks in Python took 2 to 5 us of a call, where launching takes 3
-// (appending 9 tokens 9.5 us -> 4.3, a tree's masks 5.9 -> 3.3).  binding.py holds
+// (appending 9 tokens 9.5 us -> 5.5, a tree's masks 5.9 -> 3.6).  binding.py holds
 // the functions that users call, their defaults and documentation.
 //
 // A function takes the addresses of its structs (dllm_kv_pages, dllm_rotary) and
@@ -14,6 +14,7 @@
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
 #include <cmath>
 #include <exception>
 
@@ -98,6 +99,7 @@ struct Sizes {
 Sizes sizes(PyObject* o, int64_t hd) {
   const at::Tensor& t = tensor(o);
   if (t.dim() != 4 || t.size(3) != hd) refuse("rows are tensors [entries, rows, heads, head_dim] of the head_dim given");
+  if (t.size(2) > INT32_MAX) refuse("too many heads");
   return Sizes{t.size(0), t.size(1), t.size(2)};
 }
 dllm_rows rows(const Place& p, PyObject* o, const Sizes& s, int64_t hd, at::ScalarType type) {
@@ -234,7 +236,8 @@ PyObject* kv_pages_attention_tree_(PyObject*, PyObject* const* a, Py_ssize_t n_a
     const int32_t layer = number(a[2]), *seqs = ints(p, a[3], kLists, n), *n_rows = ints(p, a[4], kLists, n);
     const int32_t* mask = ints(p, a[7], kMasks, n, max_rows, (int64_t(max_rows) + 31) / 32);
     const int32_t prefix = number(a[8]), shared = number(a[9]);
-    const int32_t most = a[10] == Py_None ? pages->max_blocks * pages->page_len : number(a[10]);
+    const int32_t most = a[10] == Py_None ? int32_t(std::min<int64_t>(int64_t(pages->max_blocks) * pages->page_len, INT32_MAX))
+                                           : number(a[10]);
     double scale = 1.0 / std::sqrt(double(hd));
     if (a[11] != Py_None) {
       scale = PyFloat_AsDouble(a[11]);
