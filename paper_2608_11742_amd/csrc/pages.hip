@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256) void free_apply_kernel(dllm_kv_pages p, const 
 // Bound by the values' lines: each moved row is 2 bytes in one of every dim of
 // every head and layer, which is read whole.  64 paths of up to 6 rows, 4 layers of
 // 32 heads of 128: 34 MB of rows, 214 MB read and 47 written, 55 us (4.8 TB/s).
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 256, kMoveWaves = kMoveThreads / kWave;
 constexpr int kMoveRows = 8;
 template <typename T, int HD>
 __device__ __forceinline__ void move_rows(const dllm_kv_pages& p, int layer, int h, int s, int first, int m,
@@ -482,18 +482,18 @@ __global__ __launch_bounds__(kPlanThreads) void pages_accept_kernel(dllm_kv_page
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kMoveThreads) void accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs, int n,
+__global__ __launch_bounds__(kMoveThreads) void accept_kernel(dllm_kv_pages p, const int32_t* __restrict__ seqs,
                                                               const int32_t* __restrict__ path, int max_path,
                                                               const int32_t* __restrict__ n_path,
                                                               const int32_t* __restrict__ from,
                                                               const int32_t* __restrict__ status) {
-  const int heads = p.n_kv_heads;
-  const int item = blockIdx.x * (kMoveThreads / kWave) + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  const int b = item / heads / p.n_layers;
-  if (b >= n || *status != KV_PAGES_OK) return;
-  const int m = n_path[b], s = seqs[b];
-  move_rows<T, HD>(p, item / heads % p.n_layers, item % heads, s, p.len[s] - m, m, path + size_t(b) * max_path,
-                   from + size_t(b) * max_path);   // (the length is the new one)
+  const int heads = p.n_kv_heads, b = blockIdx.y;
+  if (*status != KV_PAGES_OK) return;
+  const int m = n_path[b], s = seqs[b], first = p.len[s] - m;   // (the length is the new one)
+  if (m == 0) return;
+  int item = blockIdx.x * kMoveWaves + __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  for (; item < p.n_layers * heads; item += gridDim.x * kMoveWaves)
+    move_rows<T, HD>(p, item / heads, item % heads, s, first, m, path + size_t(b) * max_path, from + size_t(b) * max_path);
 }
 
 // Compaction plan in the workspace: [0] pages moved, then their new ids by
@@ -705,6 +705,7 @@ size_t page_bytes_of(const dllm_kv_pages& p) {
 constexpr int kCopyWgs = 2048;        // 8 workgroups of a copy on every CU
 constexpr int kDropHere = 32 * 1024;  // table entries one workgroup clears by itself
 constexpr int kMoveHere = 64;         // an acceptance's waves that its plan takes itself, 16 at a time
+constexpr int kMoveWgs = 4096;        // workgroups of an entry's moves, at most
 
 }  // namespace
 
@@ -746,8 +747,8 @@ hipError_t pages_accept(const dllm_kv_pages& p, const int32_t* seqs, int n, int 
                         hipStream_t s) {
   int32_t* from = static_cast<int32_t*>(ws);
   const bool drop_here = int64_t(n) * p.max_blocks <= kDropHere;
-  const int64_t waves = int64_t(n) * p.n_layers * p.n_kv_heads, per = kMoveThreads / kWave;
-  const bool move_here = waves <= kMoveHere;
+  const int waves = p.n_layers * p.n_kv_heads;   // of an entry
+  const bool move_here = int64_t(n) * waves <= kMoveHere;
   auto launch = [&](auto plan, auto move) {
     hipLaunchKernelGGL(plan, dim3(1), dim3(kPlanThreads), 0, s, p, seqs, n, max_rows, n_rows, path, max_path, n_path, from,
                        status, drop_here, move_here);
@@ -755,7 +756,7 @@ hipError_t pages_accept(const dllm_kv_pages& p, const int32_t* seqs, int n, int 
       hipLaunchKernelGGL(free_apply_kernel, dim3(std::min(cdiv(p.max_blocks, 256), 64), n), dim3(256), 0, s, p, seqs,
                          status);
     if (!move_here)
-      hipLaunchKernelGGL(move, dim3(uint32_t((waves + per - 1) / per)), dim3(kMoveThreads), 0, s, p, seqs, n, path,
+      hipLaunchKernelGGL(move, dim3(std::min(cdiv(waves, kMoveWaves), kMoveWgs), n), dim3(kMoveThreads), 0, s, p, seqs, path,
                          max_path, n_path, from, status);
     return hipGetLastError();
   };

@@ -241,11 +241,19 @@ __device__ __forceinline__ void turn_row(const Rotation& r, const Append& w, int
   lanes.template heads<!kAppend>(r.rot, r.rot.k_gain, in, r.k.head, out, head, k0 * H::HS, r.k_heads, s1 - q_steps - k0);
 }
 
+// Grids of two dimensions: the most rows there may be are 2^24 workgroups, 2^32
+// threads, one more than a dimension can have.
+dim3 grid_of(int64_t wgs) {
+  const int64_t most = 1 << 22;
+  return dim3(uint32_t(std::min(wgs, most)), uint32_t((wgs + most - 1) / most));
+}
+__device__ __forceinline__ int workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 template <typename T, int HD>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotation r) {
   __shared__ __attribute__((aligned(16))) float2 cs[kWaves][HD / 2];
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-  turn_row<T, HD, false>(r, Append{}, blockIdx.x * kWaves + wave, cs[wave]);
+  turn_row<T, HD, false>(r, Append{}, workgroup() * kWaves + wave, cs[wave]);
 }
 
 constexpr int kTile = 64;   // positions of a workgroup's values, from a multiple of 64: pages are cut there too
@@ -328,10 +336,11 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Rotation r, Append w) 
     __attribute__((aligned(16))) float2 cs[kWaves][HD / 2];
     typename Values<T, HD>::Shared values;
   } sh;
-  const int x = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int x = workgroup(), wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
   // the two kinds in even turns: with either first, the other's waits at the end
   // are not covered (16 x 512 rows of 32 + 8 + 8 heads: 49.5 us, 51 with queries and keys first)
   const int heads = w.p.n_kv_heads, values = w.tiles * heads * r.n, all = values + w.turn_wgs;
+  if (x >= all) return;
   const int y = int(int64_t(x) * values / all);
   if (y == int(int64_t(x + 1) * values / all)) {
     turn_row<T, HD, true>(r, w, (x - y) * kWaves + wave, sh.cs[wave]);
@@ -375,7 +384,7 @@ template <typename T, int HD>
 hipError_t launch_rows(Rotation r, hipStream_t s) {
   divide<T, HD>(r);
   const int64_t items = int64_t(r.n) * r.max_rows * r.parts;
-  hipLaunchKernelGGL((rotary_kernel<T, HD>), dim3(uint32_t((items + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, r);
+  hipLaunchKernelGGL((rotary_kernel<T, HD>), grid_of((items + kWaves - 1) / kWaves), dim3(kThreads), 0, s, r);
   return hipGetLastError();
 }
 
@@ -386,7 +395,8 @@ hipError_t launch_append(Rotation r, Append w, hipStream_t s) {
   w.turn_wgs = int((items + kWaves - 1) / kWaves);
   w.tiles = (r.max_rows + kTile - 2) / kTile + 1;
   w.heads_first = w.tiles == 2;
-  hipLaunchKernelGGL((append_kernel<T, HD>), dim3(w.turn_wgs + w.tiles * w.p.n_kv_heads * r.n), dim3(kThreads), 0, s, r, w);
+  const int64_t all = w.turn_wgs + int64_t(w.tiles) * w.p.n_kv_heads * r.n;
+  hipLaunchKernelGGL((append_kernel<T, HD>), grid_of(all), dim3(kThreads), 0, s, r, w);
   return hipGetLastError();
 }
 
