@@ -1760,11 +1760,12 @@ struct Division {
 };
 
 // More than 32 rows of a tree over keys of their own: in halves or wide, and in
-// how many slots.  Not divided, or as many as give each CU one or two
+// how many slots.  Not divided, or as many as give each CU one to four
 // workgroups, by the least estimated time: 2.5 us and, for every round of two
 // workgroups a CU, 4 and what a tile of 64 keys of heads of 128 takes, 1.45 wide
 // and 0.95 in halves alone on a CU, 2.3 and 1.75 where two share it, or what the keys
-// take from memory; 4 more and the records at 5 TB/s where they are joined.  Measured, us, 32 heads, wide not
+// take from memory; 4 more and the records at 5 TB/s where they are joined.  (A slot
+// is of one entry, so that on average half a slot of each is left out.)  Measured, us, 32 heads, wide not
 // divided / one a CU / two / halves not divided: 12 x 43 rows of 8 key heads
 // over 480 positions 19.4 / 29.8 / 29.8 / 19.9, 4 x 100 over 3000 69 / 45 / 44 / 49, 1 x
 // 64 over 2000 49 / 20.1 / 20.1 / 35 (halves, one a CU: 18.0), 16 x 24 over 1000 to 3500
@@ -1783,13 +1784,13 @@ TreeTail plan_tree(const PagedAttn& a, int rows, double longest, double mean, do
   TreeTail best{ROWS128, a.n, 1e30};
   for (int mode : {ROWS64, ROWS128}) {
     const int per_slot = cdiv(rows, rows_of(mode)) * kvh;
-    for (int wgs : {0, kCus, 2 * kCus}) {
+    for (int wgs : {0, kCus, 2 * kCus, 3 * kCus, 4 * kCus}) {
       const int slots = int(std::min<int64_t>(std::max(a.n, wgs / per_slot), most));
       const bool divided = slots > a.n;
       if (wgs && !divided) continue;
       const double all = double(slots) * per_slot, rounds = std::max(1.0, all / (2 * kCus));
       const double tile = u * (mode == ROWS64 ? (all > kCus ? 1.75 : 0.95) : (all > kCus ? 2.3 : 1.45));
-      const double tiles = divided ? std::max(4.0, a.n * mean / kTile / slots + 0.5) : longest / kTile;
+      const double tiles = divided ? std::max(4.0, a.n * mean / kTile / (slots - 0.5 * a.n)) : longest / kTile;
       // (keys and values from memory: 4.5 TB/s with one workgroup a CU, 5.5 with two)
       const double memory = once * kvh * a.p.head_dim * 4 / (all > kCus ? 5.5e6 : 4.5e6);
       const double us = 2.5 + rounds * 4.0 + std::max(rounds * tiles * tile, memory) +
