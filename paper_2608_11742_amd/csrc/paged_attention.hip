@@ -19,7 +19,7 @@
 // each of them costs less than a join: then every entry's range starts at
 // position 0 and takes its pages from the prefix's table first.
 //
-// Three kernels, by the number of stacked rows (MI355X; floors by the rates of
+// Four kernels, by the number of stacked rows (MI355X; floors by the rates of
 // a large copy, 4.9 TB/s, and a large bf16 product, 1190 TFLOP/s):
 //   narrow   up to 32 rows: bound by the keys and values it streams.  The
 //            waves share the rows and take the key steps in turn; a step's
@@ -29,11 +29,15 @@
 //            end.  Single tokens of 4 sequences up to 120000 long, 8 key heads
 //            of 128: 217 us, 5.7 TB/s.
 //   wide     128 rows, 32 a wave (bf16).  Tiles of 64 keys go through a
-//            two-slot LDS ring, copied one tile ahead, on 32 x 32 MFMAs.  16 x
-//            32 rows of 32 heads over 30011 positions: 318 us, 0.80 PFLOP/s,
-//            floor 213.  Matrix units are busy 43% of it and vector ALUs 37%:
-//            products and softmax alone take 177 us, fragment reads from LDS
-//            add 50, the copies 85 and the join of the ranges 15.
+//            two-slot LDS ring, copied one tile ahead, on 32 x 32 MFMAs; a
+//            wave issues one copy after each step of the score products (all of
+//            them before the products: 318 us).  16 x 32 rows of 32 heads over
+//            30011 positions: 303 us, 0.84 PFLOP/s, floor 213.  Matrix units are
+//            busy 44% of it: products and softmax alone take 177 us, and
+//            fragment reads from LDS, the copies and the join of the ranges
+//            (15) are covered in part.
+//   halves   33 to 64 rows of a tree (bf16): the wide kernel with two waves on
+//            each block of 32 rows, which take half the keys of a tile each.
 //   pairs    two entries' 32 rows each (bf16): prefix and own tails in one
 //            launch that writes the output.  16 x 32 rows over 1024: 21 us, of
 //            which 7 are spent before and after the keys, 1.4 on every 128
@@ -1177,7 +1181,10 @@ struct Wide {
 
 // 33 to 64 rows of a tree over one range of keys: wave w takes block w % 2 of 32
 // rows and half w / 2 of every tile's keys, so that no wave is without rows; the
-// two states of a block are joined through LDS.
+// two states of a block are joined through LDS.  Bound as wide is, by a wave's
+// products, softmax and fragment reads in turn: a tile takes 0.95 us alone on a
+// CU where wide takes 1.45 (32 heads on 8 key heads of 128, 16 x 16 rows over 100
+// to 1500 positions: 25.1 us, 27.2 wide).
 template <int HD>
 struct Halves {
   using L = Tile<HD>;
@@ -1760,7 +1767,7 @@ struct Division {
 };
 
 // More than 32 rows of a tree over keys of their own: in halves or wide, and in
-// how many slots.  Not divided, or as many as give each CU one to four
+// how many slots.  Not divided, or as many as give each CU one or two
 // workgroups, by the least estimated time: 2.5 us and, for every round of two
 // workgroups a CU, 4 and what a tile of 64 keys of heads of 128 takes, 1.45 wide
 // and 0.95 in halves alone on a CU, 2.3 and 1.75 where two share it, or what the keys
@@ -1784,7 +1791,7 @@ TreeTail plan_tree(const PagedAttn& a, int rows, double longest, double mean, do
   TreeTail best{ROWS128, a.n, 1e30};
   for (int mode : {ROWS64, ROWS128}) {
     const int per_slot = cdiv(rows, rows_of(mode)) * kvh;
-    for (int wgs : {0, kCus, 2 * kCus, 3 * kCus, 4 * kCus}) {
+    for (int wgs : {0, kCus, 2 * kCus}) {
       const int slots = int(std::min<int64_t>(std::max(a.n, wgs / per_slot), most));
       const bool divided = slots > a.n;
       if (wgs && !divided) continue;

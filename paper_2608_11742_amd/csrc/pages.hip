@@ -359,8 +359,10 @@ __global__ __launch_bounds__(256) void free_apply_kernel(dllm_kv_pages p, const 
 // from and rows ascend: the rows of a step are read, in one instruction those of
 // a dim, before any is written, and no later step reads a place that is filled.
 // Bound by the values' lines: each moved row is 2 bytes in one of every dim of
-// every head and layer, which is read whole.  64 paths of up to 6 rows, 4 layers of
-// 32 heads of 128: 34 MB of rows, 214 MB read and 47 written, 55 us (4.8 TB/s).
+// every head and layer, which is read whole, and a line that is written in part
+// costs what a whole one does (stored whole, 64 or 128 bytes, the same time).  64
+// paths of up to 6 rows, 4 layers of 32 heads of 128: 34 MB of rows, 209 MB read
+// and 47 written in 134 MB of lines, 87 us, 55 where they are in the last-level cache.
 constexpr int kMoveThreads = 256, kMoveWaves = kMoveThreads / kWave;
 constexpr int kMoveRows = 8;
 template <typename T, int HD>
@@ -704,7 +706,10 @@ size_t page_bytes_of(const dllm_kv_pages& p) {
 
 constexpr int kCopyWgs = 2048;        // 8 workgroups of a copy on every CU
 constexpr int kDropHere = 32 * 1024;  // table entries one workgroup clears by itself
-constexpr int kMoveHere = 64;         // an acceptance's waves that its plan takes itself, 16 at a time
+// Waves of an acceptance, times head_dim, that its plan moves itself, 16 waves at a
+// time on one CU (heads of 64, 24 waves: 8.1 us, 11.5 with a launch of their own; 32
+// 11.6 and 11.1, 64 16.6 and 11.5; of 128, 16 waves 11.7 and 10.9, 64 31.4 and 11.0).
+constexpr int kMoveHere = 1536;
 constexpr int kMoveWgs = 4096;        // workgroups of an entry's moves, at most
 
 }  // namespace
@@ -748,7 +753,7 @@ hipError_t pages_accept(const dllm_kv_pages& p, const int32_t* seqs, int n, int 
   int32_t* from = static_cast<int32_t*>(ws);
   const bool drop_here = int64_t(n) * p.max_blocks <= kDropHere;
   const int waves = p.n_layers * p.n_kv_heads;   // of an entry
-  const bool move_here = int64_t(n) * waves <= kMoveHere;
+  const bool move_here = int64_t(n) * waves * p.head_dim <= kMoveHere;
   auto launch = [&](auto plan, auto move) {
     hipLaunchKernelGGL(plan, dim3(1), dim3(kPlanThreads), 0, s, p, seqs, n, max_rows, n_rows, path, max_path, n_path, from,
                        status, drop_here, move_here);

@@ -11,6 +11,12 @@
 //
 // Values of an append are transposed through LDS in tiles of 64 positions by
 // workgroups of their own in the same launch.
+//
+// Bound by memory.  16 x 512 rows of 32 + 8 heads of 128, normed: 168 MB read and
+// written in 30.3 us, the rate of a large copy (34 us) passed a little because
+// what was written before is partly in the last-level cache; with values into
+// pages 201 MB in 48.5 us (floor 41), 33 where the rows are in that cache.  9 single
+// tokens take 5.7 us, a launch and its dependent loads.
 #include <algorithm>
 
 #include "common.h"

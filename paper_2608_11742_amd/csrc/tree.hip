@@ -3,7 +3,8 @@
 //
 // A thread takes a row and one word of its mask and walks up the tree until it
 // is past the word; the thread of word 0 walks to the root and counts.  Parents
-// are in LDS.  Bound by that walk's dependent reads, as many as the tree is deep.
+// are in LDS.  Bound by that walk's dependent reads, as many as the tree is deep,
+// behind a launch: 64 trees of 200 rows 3.2 us, one of 5 1.6, calls of 3.3 to 4.
 #include "common.h"
 #include "kernels.h"
 
