@@ -389,6 +389,8 @@ _LAYOUTS = {"halves": _abi.ROTARY_HALVES, "pairs": _abi.ROTARY_PAIRS}
 def dllm_rotary_frequencies(dim: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
                             original_len: float = 4096.0, slow: float = 1.0, fast: float = 32.0):
     """(frequencies in radians a position, amplitude) of a rotation of dim elements; scaling "linear", "base" or "ramp"."""
+    if scaling not in _SCALINGS:
+        raise ValueError("scaling is None, linear, base or ramp")
     freq, amplitude = (C.c_double * max(1, dim // 2))(), C.c_float()
     _check(lib().dllm_rotary_frequencies(dim, base, _SCALINGS[scaling], factor, original_len, slow, fast, freq,
                                          C.byref(amplitude)))

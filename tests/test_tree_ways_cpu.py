@@ -76,3 +76,11 @@ def test_plan_refusals(abi):
     assert ask(shared=-1) == 2 and ask(most=-1) == 2
     p.dtype = 2
     assert ask() == 3
+
+
+def test_scalings_have_names(abi):
+    import paper_2608_11742_amd as P
+    with pytest.raises(ValueError):
+        P.dllm_rotary_frequencies(64, scaling="log")
+    with pytest.raises(P.binding.DllmError):
+        P.dllm_rotary_frequencies(-2)
