@@ -1816,6 +1816,12 @@ Division divide(const PagedAttn& a, bool tree) {
   const int rows_t = a.max_rows * group, rows_p = a.n * rows_t;
   const int64_t keys = std::max<int64_t>(1, std::min<int64_t>(a.max_len, most));
   d.mode_p = d.mode_t = mode_of(dt, rows_t, a.n, kvh);
+  // fp32 rows of trees that leave much of the last 32 empty are taken 16 at a time: the
+  // products bound them (16 key heads of 64, 26 x 72 rows over 97 positions 31.5 us, 32
+  // at a time 36.9; 32 key heads, 12 x 48 over 1100 82.7 and 93.5; 16 x 33 over 1060 54
+  // and 55; but 32 x 32 over 400 37.6 and 30.8)
+  if (tree && dt == DLLM_F32 && d.mode_t == ROWS32 && cdiv(rows_t, 16) * 16 * 1.1 < cdiv(rows_t, 32) * 32)
+    d.mode_p = d.mode_t = ROWS16;
   // lengths of the tails: the longest, and half of it on average
   const int64_t longest = std::max<int64_t>(1, keys - shared);
   const double mean = std::max<int64_t>(0, keys - shared) / 2.0;
