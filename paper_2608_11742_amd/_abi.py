@@ -10,6 +10,7 @@ import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdllm_rps.so")
+MARSHAL_PATH = os.path.join(HERE, "_marshal.so")
 
 DLLM_MAX_TOPK = 16
 RPS_MAX_PIVOTS = 16
@@ -155,10 +156,15 @@ ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_RAMP = 0, 1, 2, 3
 
 
+def require(*paths: str):
+    for path in paths:
+        if not os.path.exists(path):
+            raise ImportError(f"{path} is missing: the HIP library must be built first "
+                              "(python -c 'import __graft_entry__ as g; g.build()')")
+
+
 def load(path: str = LIB_PATH):
-    if not os.path.exists(path):
-        raise ImportError(f"{path} is missing: the HIP library must be built first "
-                          "(python -c 'import __graft_entry__ as g; g.build()')")
+    require(path)
     lib = C.CDLL(path)
     for name, (res, args) in SIGNATURES.items():
         fn = getattr(lib, name)

@@ -12,9 +12,11 @@ import ctypes as C
 
 import torch
 
-from . import _abi, _marshal
+from . import _abi
+_abi.require(_abi.LIB_PATH, _abi.MARSHAL_PATH)   # _marshal is linked with the library
+from . import _marshal  # noqa: E402
 from ._abi import (DllmError, ModelDesc, Weights, StatsC, KvCache, Probe, RpsParams, RpsPlan, RpsDecision,
-                   DLLM_F32, DLLM_BF16, RPS_PIVOT_PAPER, RPS_PIVOT_BAND, DLLM_MAX_TOPK, RPS_MAX_BRANCH)
+                   DLLM_F32, DLLM_BF16, RPS_PIVOT_PAPER, RPS_PIVOT_BAND, DLLM_MAX_TOPK, RPS_MAX_BRANCH)  # noqa: E402
 
 _LIB = None
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
