@@ -371,7 +371,10 @@ dllm_status kv_pages_write(const dllm_kv_pages* pages, int32_t layer, const int3
  * A row that sees no position is 0, and so are the rows of a sequence outside
  * 0 .. max_seqs-1.  Table entries outside the pool are clamped.  Positions past
  * a sequence's last are never used, whatever they hold; with causal, a row
- * gives those after its own the weight 0, so their values are to be finite. */
+ * gives those after its own the weight 0, so their values are to be finite.
+ * fp32 values up to 2^127 give a finite row (a mean of larger ones may round to
+ * infinity); those below 2^-118 times the positions that a sequence can have,
+ * max_blocks * page_len, are not taken to their last bit. */
 size_t kv_pages_attention_workspace_bytes(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads);
 dllm_status kv_pages_attention(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,
                                int32_t max_rows, const int32_t* n_rows, int32_t n_heads, const dllm_rows* q,
@@ -489,8 +492,6 @@ dllm_status kv_pages_tree(const dllm_kv_pages* pages, const int32_t* seqs, int32
  * names (laid out as by kv_pages_tree, of any pattern; bits from n_rows[b] on
  * are not looked at); max_rows <= KV_TREE_MAX_ROWS.  Values that a row does not see
  * do not reach it, whatever they are.  A row that sees no position is 0.
- * Values that it does see are multiplied by weights of up to 2^15 before the
- * sums are divided: fp32 ones of 2^112 and more come out infinite.
  * Everything else and the workspace (kv_pages_attention_workspace_bytes) as
  * there. */
 dllm_status kv_pages_attention_tree(const dllm_kv_pages* pages, int32_t layer, const int32_t* seqs, int32_t n,

@@ -51,7 +51,14 @@
 // 2^-22 of the row's largest, and off by 2^-33 of it at most below, so that a
 // million keys that weigh 2^-25 each are not lost beside one that weighs 1.  The
 // sums l and products o are held in 32 bits; wide and pairs sum the weights as
-// rounded, narrow before.
+// rounded, narrow before.  fp32 needs no such room above a rounding.  There the
+// reference is the largest score itself when it moves, where the exponent of the
+// largest weights is near 0 and its own rounding smallest, and stands up to 2^7;
+// and every weight is divided by 2^8 times the positions that a sequence can
+// have, so that all of a row's weights sum up to less than 1 and no sum of
+// products passes the largest value: finite values give a finite output, as a mean
+// has to be.  At the other end, products of values below 2^-118 times those
+// positions lose bits.
 #include <algorithm>
 #include <climits>
 #include <utility>
@@ -69,6 +76,7 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 64;       // keys of a wide tile; ranges are whole tiles
 constexpr int kNarrowRows = 32;
 constexpr float kFirst = 8.f, kMost = 15.f;   // log2 of a row's largest weight when its reference moves, and ever
+constexpr float kFirst32 = 0.f, kMost32 = 7.f;   // fp32: before Job::weight
 // floats per record: HD output values, m, l, padding to 16 bytes
 constexpr int record(int hd) { return hd + 4; }
 
@@ -81,6 +89,7 @@ struct Part {
 struct Job {
   PagedAttn a;
   float scale_log2;   // scale * log2(e)
+  float weight;       // fp32: what every weight is multiplied by, a power of two
   int group;          // query heads per key head
   Part prefix, tail;
   bool stacked;       // the prefix is a part of its own; else each tail starts at position 0
@@ -392,6 +401,7 @@ __device__ __forceinline__ u32x4 ones_of(uint32_t x) {
 template <typename T, int HD, int NQB, bool TREE>
 struct Narrow {
   static constexpr bool kHalf = sizeof(T) == 2;
+  static constexpr float FIRST = kHalf ? kFirst : kFirst32, MOST = kHalf ? kMost : kMost32;
   static constexpr int E = 16 / int(sizeof(T));             // elements per chunk
   static constexpr int CK = HD / E;                         // chunks per key row
   // a step's K takes 64 registers at most, its V as many; half of that beside the state of two row blocks
@@ -508,7 +518,7 @@ struct Narrow {
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[kb][qb][i]);
         top = quad_max(top) * j.scale_log2;
-        const float mn = top > m[qb] + kMost ? top - kFirst : m[qb];
+        const float mn = top > m[qb] + MOST ? top - FIRST : m[qb];
         const float ref = mn == -INFINITY ? 0.f : mn;   // a row that has seen no key yet: exponents 2^-inf
         alpha[qb] = __builtin_amdgcn_exp2f(m[qb] - ref);
         moved = moved || mn != m[qb];
@@ -519,6 +529,7 @@ struct Narrow {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             sc[kb][qb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][qb][i], j.scale_log2, -ref));
+            if constexpr (!kHalf) sc[kb][qb][i] *= j.weight;
             sum += sc[kb][qb][i];
           }
         l[qb] = l[qb] * alpha[qb] + sum;
@@ -1879,6 +1890,9 @@ hipError_t attend(const PagedAttn& a, hipStream_t s) {
   Job j{};
   j.a = a;
   j.scale_log2 = a.scale * 1.4426950408889634f;
+  // positions of a sequence: up to 2^30
+  j.weight = 0x1p-8f;
+  for (int64_t most = 1; most < int64_t(a.p.max_blocks) * a.p.page_len; most *= 2) j.weight *= 0.5f;
   j.group = a.heads / a.p.n_kv_heads;
   const Division d = divide(a, TREE);
   const int kvh = a.p.n_kv_heads, hd = a.p.head_dim;
