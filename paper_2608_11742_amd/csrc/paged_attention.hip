@@ -1845,7 +1845,9 @@ Division divide(const PagedAttn& a, bool tree) {
   if (wide_tree) {
     const TreeTail z = plan_tree(a, rows_t, double(std::max(keys, shared)), shared + mean, shared + a.n * mean);
     d.mode_t = z.mode;
-    d.tail = Part{cdiv(rows_t, rows_of(z.mode)), cdiv(z.slots, a.n), int(most)};
+    // (slots have lengths of their own)
+    d.tail = Part{cdiv(rows_t, rows_of(z.mode)), cdiv(z.slots, a.n),
+                  int((std::max(keys, shared) + kTile - 1) / kTile) * kTile};
     d.slots = z.slots > a.n ? z.slots : 0;
     own = z.us;
   } else {

@@ -84,3 +84,16 @@ def test_scalings_have_names(abi):
         P.dllm_rotary_frequencies(64, scaling="log")
     with pytest.raises(P.binding.DllmError):
         P.dllm_rotary_frequencies(-2)
+
+
+def test_undivided_tails_are_as_long_as_the_call_says(abi):
+    """Tails of one range hold the longest sequence there is said to be, in tiles
+    of 64, as in the attention without trees, whatever the cache could hold."""
+    rng = random.Random(5)
+    for _ in range(4000):
+        dtype, hd, kv = rng.choice(["f32", "bf16"]), rng.choice([64, 128]), rng.choice([1, 2, 8, 32])
+        n, rows, most = int(2 ** rng.uniform(0, 8)), int(2 ** rng.uniform(0, 9)), int(2 ** rng.uniform(0, 17))
+        plan, _ = plan_of(abi, dtype, hd, 16, kv * rng.choice([1, 4]), kv, n, rows, 0, most)
+        assert plan.way == ENTRIES
+        if plan.tail_ranges == 1:
+            assert plan.tail_keys == -(-most // 64) * 64
