@@ -277,7 +277,7 @@ dllm_status vocab_entropy_topk_noalloc(const void* hidden, const void* w_lm, int
 #define KV_MAX_HEADS 1024
 #define KV_MAX_LAYERS 65536
 #define KV_MAX_ROWS (1 << 20)         /* rows of one entry of a batch */
-#define KV_MAX_HEAD_ROWS (1 << 26)    /* entries * rows * query heads of an attention */
+#define KV_MAX_HEAD_ROWS (1 << 26)    /* entries * rows * query heads of an attention, or heads of a rotation */
 #define KV_TREE_MAX_ROWS 1024         /* rows of a tree of drafted tokens, and of a path through it */
 enum {
     KV_PAGES_OK = 0,
@@ -459,7 +459,8 @@ dllm_status rotary_rows(const dllm_rotary* rot, int32_t dtype, const int32_t* po
                         dllm_stream stream);
 
 /* kv_pages_write of keys that are normed and rotated on the way, and of values
- * as they are; n, max_rows and n_rows as there, and the same rows are written.
+ * as they are; n, max_rows and n_rows as there, but n * max_rows * (n_heads +
+ * n_kv_heads) <= KV_MAX_HEAD_ROWS, and the same rows are written.
  *   pos      [n][max_rows] positions of the rotation, NULL: those of the rows,
  *            len - n_rows[b] + i (a row of a tree has its depth's, kv_pages_tree).
  *   q, q_out   nullable (n_heads 0): queries of n_heads heads at the same

@@ -451,7 +451,8 @@ def rotary_rows(rot: Rotary, q, q_out, k=None, k_out=None, pos=None, pos_offset:
 def kv_pages_append(pages: KvPages, layer: int, seqs, k, v, rot: Rotary, q=None, q_out=None, pos=None, n_rows=None,
                     stream=None):
     """kv_pages_write with k normed and rotated on the way; q [entries, rows, heads, head_dim] likewise into q_out.
-    pos [entries, rows]: positions of the rotation, by default those of the rows."""
+    pos [entries, rows]: positions of the rotation, by default those of the rows.  entries * rows * (heads + key heads)
+    is KV_MAX_HEAD_ROWS at most."""
     status = _marshal.kv_pages_append(pages._at, pages._index, layer, seqs, n_rows, rot._at, rot._index, pos, q, q_out,
                                       k, v, None if stream is None else _page_stream(pages, stream))
     if status:

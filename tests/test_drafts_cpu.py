@@ -250,3 +250,18 @@ def test_host_acceptance_keeps_the_tables_sound():
             if m % 16:
                 assert h.refs[h.table[s][m // 16]] == 1
     assert codes == {OK, ESEQ, ELEN, ESHARED, EPATH}
+
+
+@needs_lib
+def test_appended_rows_of_all_heads_are_limited(abi):
+    """KV_MAX_HEAD_ROWS counts query and key heads (sizes are looked at before rows: with NULL ones, those that fit are EINVAL)."""
+    _abi, lib = abi
+    most = _abi.KV_MAX_HEAD_ROWS
+    rot = C.byref(rotary(_abi))
+    for n, rows, heads, kv in [(64, 32768, 32, 8), (64, 32768, 24, 8), (1, 1 << 20, 32, 32), (1024, 1 << 16, 0, 1),
+                               (1024, 1 << 16, 0, 2), (1, 1 << 20, 0, 64), (1, 1 << 20, 1, 64), (1024, 1 << 20, 1024, 1024)]:
+        p = C.byref(pages(_abi, n_kv_heads=kv))
+        status = lib.kv_pages_append(p, 0, FAKE, n, rows, None, rot, None, heads, None, None, None, None, None)
+        assert status == (1 if n * rows * (heads + kv) <= most else 2), (n, rows, heads, kv)
+        if status == 2:
+            assert b"rows of" in lib.dllm_last_error()
