@@ -403,8 +403,8 @@ class Rotary:
     """Rotation of heads to their positions, after a norm by head (dllm_rotary).
 
     dim: rotated elements of a head (default all), layout "halves" or "pairs",
-    scaling as in dllm_rotary_frequencies; freq [dim / 2] gives other
-    frequencies, amplitude another factor.  norm: heads are normed first, with
+    scaling as in dllm_rotary_frequencies; freq [dim / 2] stands for base and
+    scaling (with amplitude 1), amplitude gives another factor.  norm: heads are normed first, with
     gains q_gain and k_gain [head_dim] where given."""
 
     def __init__(self, head_dim: int, dim: int | None = None, base: float = 10000.0, layout: str = "halves",
@@ -421,9 +421,10 @@ class Rotary:
         own = 1.0
         if freq is None and dim:
             freq, own = dllm_rotary_frequencies(dim, base, scaling, factor, original_len, slow, fast)
-        if freq is not None and len(freq) != dim // 2:
+        freq = torch.as_tensor([] if freq is None else freq, dtype=torch.float64)
+        if tuple(freq.shape) != (dim // 2,):
             raise ValueError("one frequency for every pair of rotated elements")
-        self.freq = torch.as_tensor(freq if dim else [0.0], dtype=torch.float64).to(device).contiguous()
+        self.freq = (freq if dim else torch.zeros(1, dtype=torch.float64)).to(device).contiguous()
         self.device, self._index = self.freq.device, self.freq.get_device()
         self.q_gain, self.k_gain = q_gain, k_gain
         for g in (q_gain, k_gain):

@@ -265,3 +265,21 @@ def test_appended_rows_of_all_heads_are_limited(abi):
         assert status == (1 if n * rows * (heads + kv) <= most else 2), (n, rows, heads, kv)
         if status == 2:
             assert b"rows of" in lib.dllm_last_error()
+
+
+@needs_lib
+def test_frequencies_of_their_own_are_one_a_pair(abi):
+    """Frequencies in a grid would be read row after row, those of the wrong pairs."""
+    import torch
+
+    import paper_2608_11742_amd as P
+    f = torch.arange(32, dtype=torch.float32)
+    for freq in (f, f.numpy(), f.tolist(), f.double()):
+        rot = P.Rotary(64, freq=freq, device="cpu")
+        assert rot.freq.tolist() == f.tolist() and rot.freq.dtype == torch.float64 and rot.amplitude == 1.0
+    for freq in (f[:31], f[:, None], f[:, None].expand(32, 2), [[x, 0.0] for x in f.tolist()], []):
+        with pytest.raises(ValueError):
+            P.Rotary(64, freq=freq, device="cpu")
+    with pytest.raises(ValueError):
+        P.Rotary(64, dim=0, freq=f, device="cpu")
+    assert P.Rotary(64, dim=0, device="cpu").dim == 0
