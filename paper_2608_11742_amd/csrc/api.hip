@@ -1036,7 +1036,6 @@ dllm_status attend(const char* who, const dllm_kv_pages* pages, int32_t layer, c
   a.max_len = max_len;
   a.causal = causal;
   a.mask = mask;
-  a.words = (max_rows + 31) / 32;
   a.scale = scale;
   a.part = static_cast<float*>(ws);
   return hip_check(paged_attention(a, static_cast<hipStream_t>(stream)), who);

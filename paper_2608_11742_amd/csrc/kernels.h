@@ -181,17 +181,15 @@ hipError_t pages_append(const dllm_kv_pages& p, int layer, const int32_t* seqs, 
 // attention over the pages of one layer (paged_attention.hip)
 struct PagedAttn {
   dllm_kv_pages p;
-  int layer;
   const int32_t* seqs;
   const int32_t* n_rows;   // nullable: max_rows each
-  int n, max_rows, heads;
+  const uint32_t* mask;    // nullable: which of an entry's rows each of them sees, a bit a row in words of 32
+  float* part;             // workspace of paged_attention_workspace bytes
   dllm_rows q, out;
+  int layer, n, max_rows, heads;
   int prefix_seq, shared_len, max_len;
   bool causal;
-  const uint32_t* mask;    // nullable: which of an entry's rows each of them sees, `words` a row
-  int words;
   float scale;
-  float* part;             // workspace of paged_attention_workspace bytes
 };
 size_t paged_attention_workspace(const dllm_kv_pages& p, int n, int max_rows, int heads);
 // enough for every call of no more entries and rows

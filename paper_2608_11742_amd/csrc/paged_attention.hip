@@ -95,7 +95,11 @@ struct Job {
   bool stacked;       // the prefix is a part of its own; else each tail starts at position 0
   bool direct;        // one range in all: the output itself
   int slots;          // of a tree's tails (see Slots); 0: each entry has tail.ranges
+  int slices;         // groups of lanes that a row of the join has
 };
+// Kernels take it by value: arguments past 256 bytes cost each launch 0.3 us (24
+// single tokens of 32 heads of 64 over 530 positions 11.75 -> 12.06 us)
+static_assert(sizeof(Job) <= 256, "arguments of a launch");
 
 __device__ __forceinline__ int most_positions(const PagedAttn& a) { return a.p.max_blocks * a.p.page_len; }
 
@@ -144,8 +148,9 @@ __device__ __forceinline__ table_t table_row(const PagedAttn& a, int seq) {
 // Pages of positions before `split` are `before`'s, then `after`'s.
 struct Share {
   int row0, row_end, head, k0, k1, split;
-  int64_t rec0;   // of the share's records: that of row 0 of all entries would be here
-  Entry e;        // of a tail
+  int part;    // of the share's records (see record_of)
+  int slots;   // how far a slot of a tree's tails is past its entry's number; 0 without slots
+  Entry e;     // of a tail of a tree
   table_t before, after;
   __device__ __forceinline__ int page(int pos, int shift, int last_block) const {
     return (pos < split ? before : after)[min(pos >> shift, last_block)];
@@ -163,7 +168,11 @@ struct Item {
 __device__ __forceinline__ Item item_of(int x, int row_tiles) {
   return Item{x / (8 * row_tiles) * 8 + x % 8, x / 8 % row_tiles};
 }
-int blocks_of(int items, int row_tiles) { return cdiv(items, 8) * 8 * row_tiles; }
+__host__ __device__ __forceinline__ int blocks_of(int items, int row_tiles) { return (items + 7) / 8 * 8 * row_tiles; }
+// workgroups of the prefix
+__host__ __device__ __forceinline__ int prefix_blocks(const Job& j) {
+  return blocks_of(j.prefix.ranges * j.a.p.n_kv_heads, j.prefix.row_tiles);
+}
 
 // v of the lane that `CTRL` moves here (0 where the rows of ROWS do not take part)
 template <int CTRL, int ROWS = 0xf>
@@ -222,19 +231,19 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
   // items are filled up to whole rounds of XCDs
   if (by_length ? t >= j.slots : b >= (in_prefix ? 1 : a.n)) return false;
   const int s = shared_of(a);
-  const int64_t rows_all = int64_t(a.n) * a.max_rows * a.heads;
+  w.slots = 0;
   if (in_prefix) {
     w.row0 = it.tile * tile_rows;
     w.row_end = a.n * per;
     w.k0 = r * part.range;
     w.k1 = min(w.k0 + part.range, s);
-    w.rec0 = r * rows_all;
+    w.part = r;
     w.split = 0;
     w.before = w.after = table_row(a, a.prefix_seq);
     return w.k0 < w.k1;
   }
   int range = part.range, ranges = part.ranges;
-  w.rec0 = (j.prefix.ranges + r) * rows_all;
+  w.part = j.prefix.ranges + r;
   if (by_length) {
     const Slots z = slots_of<TREE>(j, s);
     // slot t is of the last entry that starts at or before it (one without any starts where the next does)
@@ -244,7 +253,8 @@ __device__ __forceinline__ bool share_of(const Job& j, int x, bool in_prefix, in
     if (r >= ranges) return false;
     const int tiles = __builtin_amdgcn_readlane(z.tiles, b);
     range = (tiles + ranges - 1) / ranges * kTile;   // even
-    w.rec0 = j.prefix.ranges * rows_all + int64_t(t - b) * a.max_rows * a.heads;
+    w.part = j.prefix.ranges;
+    w.slots = t - b;
     w.e = Entry{__builtin_amdgcn_readlane(z.e.seq, b), __builtin_amdgcn_readlane(z.e.held, b),
                 __builtin_amdgcn_readlane(z.e.rows, b)};
   } else {
@@ -275,9 +285,11 @@ __device__ __forceinline__ RowAt row_at(const Job& j, int row) {
   return r;
 }
 
-__device__ __forceinline__ float* record_of(const Job& j, int64_t rec0, const RowAt& r, int kvh, int hd) {
-  const int64_t row = (int64_t(r.b) * j.a.max_rows + r.i) * j.a.heads + kvh * j.group + r.g;
-  return j.a.part + (rec0 + row) * record(hd);
+// A part has a record for every row of all entries; the slots of a tree's tails,
+// with the rows of one entry each, follow one another from their first part on.
+__device__ __forceinline__ float* record_of(const Job& j, const Share& w, const RowAt& r, int kvh, int hd) {
+  const int64_t row = (int64_t(r.b + w.slots) * j.a.max_rows + r.i) * j.a.heads + kvh * j.group + r.g;
+  return j.a.part + (int64_t(w.part) * j.a.n * j.a.max_rows * j.a.heads + row) * record(hd);
 }
 
 // lane l's value of lanes l, l ^ 32 joined
@@ -318,14 +330,15 @@ struct MaskWords {
   uint32_t w[3];
 };
 __device__ __forceinline__ MaskWords mask_words(const PagedAttn& a, int b, int i, int root, int k0) {
-  const uint32_t* row = a.mask + (size_t(b) * a.max_rows + i) * a.words;
+  const int words = (a.max_rows + 31) / 32;
+  const uint32_t* row = a.mask + (size_t(b) * a.max_rows + i) * words;
   const int j = max(k0 - root, 0) >> 5;
   MaskWords m;
   // (words past the mask's are read from inside it, so that no load waits behind a branch)
 #pragma unroll
   for (int u = 0; u < 3; ++u) {
-    const uint32_t w = row[min(j + u, a.words - 1)];
-    m.w[u] = j + u < a.words ? w : 0u;
+    const uint32_t w = row[min(j + u, words - 1)];
+    m.w[u] = j + u < words ? w : 0u;
   }
   return m;
 }
@@ -727,7 +740,7 @@ struct Narrow {
       const float inv = any ? 1.f / sum : 0.f;
       T* out = static_cast<T*>(a.out.p) + at[qb].b * a.out.seq + at[qb].i * a.out.row +
                (kvh * j.group + at[qb].g) * a.out.head;
-      float* rec = record_of(j, w.rec0, at[qb], kvh, HD);
+      float* rec = record_of(j, w, at[qb], kvh, HD);
       for (int db = wave; db < NDB; db += kWaves) {
         f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -1173,7 +1186,7 @@ struct Wide {
         for (int i = 0; i < 16; ++i)
           store_f(out + 32 * db + 8 * (i >> 2) + 4 * f + (i & 3), any ? rows.o[db][i] * inv : 0.f);
     } else {
-      float* rec = record_of(j, w.rec0, at, w.head, HD);
+      float* rec = record_of(j, w, at, w.head, HD);
 #pragma unroll
       for (int db = 0; db < L::NDB; ++db)
 #pragma unroll
@@ -1288,7 +1301,7 @@ struct Halves {
     const float l = lsum * w0 + other[(STATE - 1) * kWave] * w1, inv = 1.f / l;
     if (w.row0 + 32 * block + fr >= w.row_end || at.i >= w.e.rows) return;
     bf16_t* out = static_cast<bf16_t*>(a.out.p) + at.b * a.out.seq + at.i * a.out.row + (w.head * j.group + at.g) * a.out.head;
-    float* rec = record_of(j, w.rec0, at, w.head, HD);
+    float* rec = record_of(j, w, at, w.head, HD);
 #pragma unroll
     for (int c = 0; c < OWN * 16; c += 4) {
       f32x4 y;
@@ -1517,16 +1530,16 @@ template <int HD> struct Taker<bf16_t, HD, ROWS64, true> : Halves<HD> {};
 
 // both parts in one launch: prefix workgroups, then the tails' (trees are in those alone)
 template <typename T, int HD, int PREFIX, int TAIL, bool TREE>
-__global__ __launch_bounds__(kThreads, 2) void attention_kernel(Job j, int prefix_blocks) {
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(Job j) {
   using P = Taker<T, HD, PREFIX, false>;
   using U = Taker<T, HD, TAIL, TREE>;
   __shared__ __attribute__((aligned(16))) uint8_t smem[P::SMEM > U::SMEM ? P::SMEM : U::SMEM];
   Share w;
-  const int x = blockIdx.x;
-  if (x < prefix_blocks) {
+  const int x = blockIdx.x, prefix = prefix_blocks(j);
+  if (x < prefix) {
     if (share_of<TREE>(j, x, true, rows_of(PREFIX), w)) P::run(j, w, smem);
   } else {
-    if (share_of<TREE>(j, x - prefix_blocks, false, rows_of(TAIL), w)) U::run(j, w, smem);
+    if (share_of<TREE>(j, x - prefix, false, rows_of(TAIL), w)) U::run(j, w, smem);
   }
 }
 
@@ -1536,11 +1549,11 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Job j, int prefi
 // hold positions the row sees; HD / 4 lanes a row and slice, slice c takes the
 // ranges c, c + slices, .., and the slices are joined in order.
 template <typename T, int HD, bool TREE>
-__global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
+__global__ __launch_bounds__(kThreads) void join_kernel(Job j) {
   constexpr int kLanes = HD / 4;
   __shared__ __attribute__((aligned(16))) float part[kThreads / kLanes][HD + 4];
   const PagedAttn& a = j.a;
-  const int group = int(threadIdx.x) / kLanes, c = int(threadIdx.x) % kLanes * 4, slice = group % slices;
+  const int slices = j.slices, group = int(threadIdx.x) / kLanes, c = int(threadIdx.x) % kLanes * 4, slice = group % slices;
   const int rows = kThreads / kLanes / slices, row = blockIdx.x * rows + group / slices;
   const bool in = row < a.n * a.max_rows * a.heads;
   const int h = row % a.heads, t = row / a.heads, b = in ? t / a.max_rows : 0, i = t % a.max_rows;
@@ -1577,7 +1590,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Job j, int slices) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int r = min(r0 + u * slices, np + nt - 1);
-      const float* x = r < np ? rec + r * stride : tails + (r - np) * tail_stride;
+      const float* x = !TREE ? rec + (r < np ? r : j.prefix.ranges + r - np) * stride
+                             : r < np ? rec + r * stride : tails + (r - np) * tail_stride;
       mr[u] = x[HD];
       lr[u] = x[HD + 1];
       v[u] = *reinterpret_cast<const f32x4*>(x + c);
@@ -1667,10 +1681,8 @@ Part plan_part(int mode, int rows, int64_t groups, int kv_heads, int64_t keys, d
 template <typename T, int HD, int PREFIX, int TAIL, bool TREE>
 void launch_parts(const Job& j, hipStream_t s) {
   const int kvh = j.a.p.n_kv_heads;
-  const int prefix = j.prefix.ranges ? blocks_of(j.prefix.ranges * kvh, j.prefix.row_tiles) : 0;
   const int tail = blocks_of((j.slots ? j.slots : j.a.n * j.tail.ranges) * kvh, j.tail.row_tiles);
-  hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL, TREE>), dim3(prefix + tail),
-                     dim3(kThreads), 0, s, j, prefix);
+  hipLaunchKernelGGL((attention_kernel<T, HD, PREFIX, TAIL, TREE>), dim3(prefix_blocks(j) + tail), dim3(kThreads), 0, s, j);
 }
 
 // (a prefix never takes fewer rows than the tails, see divide)
@@ -1689,16 +1701,16 @@ void launch_modes(const Job& j, int prefix, int tail, hipStream_t s) {
 }
 
 template <typename T, int HD, bool TREE>
-void launch(const Job& j, int prefix, int tail, hipStream_t s) {
+void launch(Job& j, int prefix, int tail, hipStream_t s) {
   launch_modes<T, HD, TREE>(j, prefix, tail, s);
   if (j.direct) return;
   // rows of many ranges take several groups of lanes each: the records of a
   // row come in turn, four at a time
   constexpr int kGroups = kThreads / (HD / 4);
   const int ranges = j.prefix.ranges + (j.slots ? cdiv(j.slots, j.a.n) : j.tail.ranges);
-  const int slices = ranges <= 4 ? 1 : ranges <= 8 ? 2 : ranges <= 16 ? 4 : 8;
-  hipLaunchKernelGGL((join_kernel<T, HD, TREE>), dim3(cdiv(j.a.n * j.a.max_rows * j.a.heads, kGroups / slices)),
-                     dim3(kThreads), 0, s, j, slices);
+  j.slices = ranges <= 4 ? 1 : ranges <= 8 ? 2 : ranges <= 16 ? 4 : 8;
+  hipLaunchKernelGGL((join_kernel<T, HD, TREE>), dim3(cdiv(j.a.n * j.a.max_rows * j.a.heads, kGroups / j.slices)),
+                     dim3(kThreads), 0, s, j);
 }
 
 }  // namespace
