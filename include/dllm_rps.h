@@ -401,9 +401,10 @@ dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32
 
 /* ------------------------------------------------- rotary positions, drafts
  *
- * Models whose queries and keys are normed by head, rotated in part, in pairs
- * or at scaled frequencies, and tokens that are drafted as a tree and verified
- * over the paged cache in one forward:
+ * For a program's own forward of models whose queries and keys are normed by
+ * head, rotated in part, in pairs or at scaled frequencies, and of tokens that are
+ * drafted as a tree and verified together over the paged cache (dllm_forward_pages
+ * takes neither trees nor these rotations):
  *   kv_pages_grow          the tree's rows after what a sequence holds
  *   kv_pages_tree          what each row sees of the tree, and its position
  *   kv_pages_append        a layer's rotated keys and values into the pages
@@ -415,7 +416,8 @@ dllm_status kv_pages_attention_plan(const dllm_kv_pages* pages, int32_t n, int32
  *   (y_a, y_b) -> amplitude (cos(t) y_a - sin(t) y_b, sin(t) y_a + cos(t) y_b)
  * with t = p * freq[j] for pair j < dim / 2: elements (j, j + dim / 2), or with
  * DLLM_ROTARY_PAIRS (2 j, 2 j + 1).  Elements from dim on are not rotated.
- * Angles are reduced in 64 bits, the rest is computed in 32 and rounded once.
+ * Angles are reduced in 64 bits (off by 2^-51 of t at most), the rest, the
+ * squares of a norm among it, is computed in 32 and rounded once.
  *   freq     device [dim / 2], radians a position; may be NULL with dim 0.
  *   q_gain, k_gain   device [head_dim], 16-byte aligned, NULL: ones; read with
  *            norm only.
@@ -437,7 +439,9 @@ typedef struct {
  *   DLLM_ROTARY_RAMP    by turns r within original_len positions: those of r >=
  *                       fast stand, those of r <= slow are divided by factor,
  *                       between them both are mixed by (r - slow) / (fast - slow)
- *                       (YaRN; 0 <= slow < fast)
+ *                       (YaRN as its paper defines it, 0 <= slow < fast;
+ *                       checkpoints whose ramp runs over the pair's index instead
+ *                       need frequencies of their own)
  * amplitude receives 1, and for the ramp 0.1 ln(factor) + 1, that method's
  * factor on the rotated queries and keys.  A host function. */
 typedef enum { DLLM_ROTARY_PLAIN = 0, DLLM_ROTARY_LINEAR = 1, DLLM_ROTARY_BASE = 2, DLLM_ROTARY_RAMP = 3 } dllm_rotary_scaling;
@@ -504,7 +508,9 @@ dllm_status kv_pages_attention_tree(const dllm_kv_pages* pages, int32_t layer, c
 /* How kv_pages_attention_tree divides a call of these sizes, as
  * kv_pages_attention_plan.  Rows of a part can be 64 too.  Tails of several ranges
  * have as many slots, n * tail_ranges at most, as the device gives out by the
- * lengths of the entries (n <= 64; tail_keys is 0 then). */
+ * lengths of the entries (n <= 64; tail_keys is 0 then).  More entries have even
+ * ranges, and those of more than 32 bf16 rows a key head one each, unless the
+ * prefix is a part. */
 dllm_status kv_pages_attention_tree_plan(const dllm_kv_pages* pages, int32_t n, int32_t max_rows, int32_t n_heads,
                                          int32_t shared_len, int32_t max_len, kv_attention_plan* plan);
 

@@ -30,9 +30,10 @@
 //            of 128: 217 us, 5.7 TB/s.
 //   wide     128 rows, 32 a wave (bf16).  Tiles of 64 keys go through a
 //            two-slot LDS ring, copied one tile ahead, on 32 x 32 MFMAs; a
-//            wave issues one copy after each step of the score products (all of
-//            them before the products: 318 us).  16 x 32 rows of 32 heads over
-//            30011 positions: 303 us, 0.84 PFLOP/s, floor 213.  Matrix units are
+//            wave issues one copy after each step of the score products (2%
+//            faster than all of them before the products).  16 x 32 rows of 32
+//            heads over 30011 positions: 299-316 us by device, 0.80-0.85 PFLOP/s,
+//            floor 213.  Matrix units are
 //            busy 44% of it: products and softmax alone take 177 us, and
 //            fragment reads from LDS, the copies and the join of the ranges
 //            (15) are covered in part.
@@ -49,7 +50,10 @@
 // pass 2^15, so o is rescaled rarely.  Weights of bf16 models are rounded to
 // binary16 for the product with binary16 values: 11 significant bits down to
 // 2^-22 of the row's largest, and off by 2^-33 of it at most below, so that a
-// million keys that weigh 2^-25 each are not lost beside one that weighs 1.  The
+// million keys that weigh 2^-25 each are not lost beside one that weighs 1.  Such
+// an output is 1.67e-3 off 64 bits (root mean square, the rounding to bf16), with
+// weights in 32 bits 1.66e-3; the two differ by 8e-4, where the rounding to bf16
+// falls the other way.  The
 // sums l and products o are held in 32 bits; wide and pairs sum the weights as
 // rounded, narrow before.  fp32 needs no such room above a rounding.  There the
 // reference is the largest score itself when it moves, where the exponent of the
@@ -195,7 +199,8 @@ __device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readl
 // head and row tile have, an entry gets one for every `step` tiles, the least
 // step with which all find a slot (and 4 at least).  So one long entry among short
 // ones, or a max_len that is far off, leaves no workgroup without work.  Every
-// wave works it out from the lengths, a lane for each of up to 64 entries.
+// wave works it out from the lengths, a lane for each of up to 64 entries; more
+// have even ranges, and more than 32 bf16 rows of each of them one (see plan_tree).
 struct Slots {
   Entry e;                   // of this lane
   int count, first, tiles;   // its slots, and the tiles in them
@@ -1078,7 +1083,7 @@ struct Rows32 {
 
 // 128 rows, 32 a wave, over one range of keys; two tiles in LDS, so that two
 // workgroups share a CU.  Measured equal (16 x 32 rows, 32 heads, over 30011
-// positions: 320 us, 0.79 PFLOP/s): eight waves and 256 rows with three tiles on
+// positions, as it was then: 320 us, 0.79 PFLOP/s): eight waves and 256 rows with three tiles on
 // their way, whose copies are half as many a row; the same in two groups that
 // take turns at matrix and vector work.  64 rows a wave, alone on its SIMD with
 // products and softmax in one stream, took 350.

@@ -711,7 +711,7 @@ size_t page_bytes_of(const dllm_kv_pages& p) {
 constexpr int kCopyWgs = 2048;        // 8 workgroups of a copy on every CU
 constexpr int kDropHere = 32 * 1024;  // table entries one workgroup clears by itself
 // Waves of an acceptance, times head_dim, that its plan moves itself, 16 waves at a
-// time on one CU (heads of 64, 24 waves: 8.1 us, 11.5 with a launch of their own; 32
+// time on one CU (paths of a few rows, heads of 64, 24 waves: 8.1 us, 11.5 with a launch of their own; 32
 // 11.6 and 11.1, 64 16.6 and 11.5; of 128, 16 waves 11.7 and 10.9, 64 31.4 and 11.0).
 constexpr int kMoveHere = 1536;
 constexpr int kMoveWgs = 4096;        // workgroups of an entry's moves, at most
