@@ -66,3 +66,29 @@ def test_many_keys(hd, rows, length, equal):
     poison(kp)
     check_attention(kp, 1, [0], torch.ones_like(q), None, scale=1.0, max_len=length)
     drafts.check_tree(kp, 1, [0], torch.ones_like(q), None, see, scale=1.0, max_len=length)
+
+
+@pytest.mark.parametrize("power", [-80, 126])
+@pytest.mark.parametrize("case", smallest(TREE_WAYS, lambda c: (c[1], *c[9:])), ids=str)
+def test_powers_of_two(case, power):
+    """Values a power of two larger or smaller give outputs that are, bit for bit:
+    no weight is rounded otherwise for them and none of the products, of weights
+    down to 2^-40 here, leaves the normal numbers."""
+    hd, page, heads, kv, n, rows, prefix, tail = case[1:9]
+    kp, seqs, lens = batch(case)
+    g = torch.Generator(device=kp.device).manual_seed(4)
+    kp.vt.uniform_(1.0, 2.0, generator=g)
+    kp.vt[..., 1::2, :] *= -1
+    q, see = queries(n, rows, heads, hd, F32), drafts.masks(random.Random(n), n, rows, "tree")
+    kw = dict(prefix_seq=0, shared_len=prefix, max_len=max(lens))
+    ws = torch.empty(P.kv_pages_attention_workspace_bytes(kp, n, rows, heads), dtype=torch.uint8, device=kp.device)
+
+    def both():
+        out = torch.empty_like(q)
+        P.kv_pages_attention(kp, 1, torch.tensor(seqs, dtype=torch.int32, device=kp.device), q, out, ws, **kw)
+        return out, drafts.run_tree(kp, 1, seqs, q, None, see, **kw)
+
+    before = both()
+    kp.vt *= 2.0 ** power
+    for a, b in zip(before, both()):
+        assert bool(torch.isfinite(b).all()) and torch.equal(a.double() * 2.0 ** power, b.double())
